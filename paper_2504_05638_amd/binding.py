@@ -27,11 +27,17 @@ TAGC_DECODE_PEEL, TAGC_DECODE_PEEL_ESTIMATE, TAGC_DECODE_ESTIMATE = 0, 1, 2
 TAGC_CELL_F32, TAGC_CELL_BF16 = 0, 1
 TAGC_FLAG_OVERFLOW = 2
 TAGC_STATIC_WORKSPACE_BYTES = 16 << 20
+TAGC_MOMENT_BLOCK, TAGC_MAX_GROUPS = 256, 16
+TAGC_ACT_NONE, TAGC_ACT_RELU, TAGC_ACT_GELU, TAGC_ACT_GELU_TANH, TAGC_ACT_SILU = 0, 1, 2, 3, 4
 
 EXPORTS = ["tagc_plan", "tagc_plan_destroy", "tagc_plan_sizes",
            "tagc_plan_upload", "tagc_compress", "tagc_compress_ranks", "tagc_compress_static", "tagc_feedback_apply", "tagc_aggregate",
            "tagc_decompress", "tagc_reduce_decompress", "tagc_profile_enable", "tagc_profile_read",
-           "tagc_hash_host", "tagc_dense_pieces_host", "tagc_strerror"]
+           "tagc_hash_host", "tagc_dense_pieces_host", "tagc_strerror",
+           "tagc_optim_plan", "tagc_optim_destroy", "tagc_optim_plan_sizes", "tagc_optim_upload",
+           "tagc_grad_norm", "tagc_adamw_step", "tagc_adamw_unpack",
+           "tagc_linear_forward_workspace", "tagc_linear_backward_workspace",
+           "tagc_linear_forward", "tagc_linear_backward"]
 
 
 class tagc_segment(C.Structure):
@@ -81,6 +87,52 @@ class tagc_shared_buffers(C.Structure):
                 ("sketch", C.c_void_p), ("header", C.c_void_p),
                 ("bounds", C.c_void_p), ("workspace", C.c_void_p),
                 ("status", C.c_void_p)]
+
+
+class tagc_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("bases", C.c_void_p), ("copy", C.c_void_p), ("length", C.c_uint64),
+                ("param_type", C.c_uint32), ("grad_type", C.c_uint32), ("group", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
+class tagc_optim_config(C.Structure):
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_double), ("max_norm", C.c_double), ("seed", C.c_uint64),
+                ("moment_bits", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tagc_group(C.Structure):
+    _fields_ = [("lr", C.c_double), ("weight_decay", C.c_double)]
+
+
+class tagc_optim_control(C.Structure):
+    _fields_ = [("step", C.c_uint32), ("skipped", C.c_uint32), ("apply", C.c_uint32),
+                ("norm", C.c_float), ("factor", C.c_float), ("lr_scale", C.c_float),
+                ("reserved", C.c_uint32 * 2), ("bias1", C.c_double), ("bias2", C.c_double),
+                ("reserved2", C.c_uint32 * 4)]
+
+
+class tagc_optim_sizes(C.Structure):
+    _fields_ = [("table_bytes", C.c_uint64), ("n_elems", C.c_uint64), ("n_blocks", C.c_uint64),
+                ("n_chunks", C.c_uint64)]
+
+
+class tagc_linear(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("in_", C.c_uint64), ("out", C.c_uint64),
+                ("dtype", C.c_uint32), ("activation", C.c_uint32),
+                ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("ldw", C.c_uint64),
+                ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_uint64),
+                ("y", C.c_void_p), ("ldy", C.c_uint64), ("pre", C.c_void_p), ("ldp", C.c_uint64)]
+
+
+class tagc_linear_grad(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("in_", C.c_uint64), ("out", C.c_uint64),
+                ("dtype", C.c_uint32), ("activation", C.c_uint32),
+                ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("ldw", C.c_uint64),
+                ("pre", C.c_void_p), ("ldp", C.c_uint64), ("dy", C.c_void_p), ("lddy", C.c_uint64),
+                ("dx", C.c_void_p), ("lddx", C.c_uint64), ("dw", C.c_void_p), ("lddw", C.c_uint64),
+                ("db", C.c_void_p), ("accumulate", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class TagcError(RuntimeError):
@@ -155,6 +207,30 @@ def lib():
         L.tagc_dense_pieces_host.restype = C.c_uint32
         L.tagc_dense_pieces_host.argtypes = [C.c_uint32, C.c_uint32, C.POINTER(C.c_uint32),
                                              C.POINTER(C.c_uint32), C.c_uint32]
+        L.tagc_optim_plan.restype = C.c_int
+        L.tagc_optim_plan.argtypes = [C.POINTER(tagc_optim_config), C.POINTER(tagc_tensor),
+                                      C.c_uint32, C.POINTER(vp)]
+        L.tagc_optim_destroy.restype = None
+        L.tagc_optim_destroy.argtypes = [vp]
+        L.tagc_optim_plan_sizes.restype = C.c_int
+        L.tagc_optim_plan_sizes.argtypes = [vp, C.POINTER(tagc_optim_sizes)]
+        L.tagc_optim_upload.restype = C.c_int
+        L.tagc_optim_upload.argtypes = [vp, vp, vp]
+        L.tagc_grad_norm.restype = C.c_int
+        L.tagc_grad_norm.argtypes = [vp, vp, vp, vp]
+        L.tagc_adamw_step.restype = C.c_int
+        L.tagc_adamw_step.argtypes = [vp, vp, C.POINTER(tagc_group), C.c_uint32, C.c_uint32, vp, vp]
+        L.tagc_adamw_unpack.restype = C.c_int
+        L.tagc_adamw_unpack.argtypes = [vp, vp, vp, vp, vp]
+        L.tagc_linear_forward_workspace.restype = C.c_int
+        L.tagc_linear_forward_workspace.argtypes = [C.POINTER(tagc_linear), C.POINTER(C.c_uint64)]
+        L.tagc_linear_backward_workspace.restype = C.c_int
+        L.tagc_linear_backward_workspace.argtypes = [C.POINTER(tagc_linear_grad),
+                                                     C.POINTER(C.c_uint64)]
+        L.tagc_linear_forward.restype = C.c_int
+        L.tagc_linear_forward.argtypes = [C.POINTER(tagc_linear), vp, vp]
+        L.tagc_linear_backward.restype = C.c_int
+        L.tagc_linear_backward.argtypes = [C.POINTER(tagc_linear_grad), vp, vp]
         L.tagc_strerror.restype = C.c_char_p
         L.tagc_strerror.argtypes = [C.c_int]
         _lib = L
@@ -284,3 +360,65 @@ def tagc_dense_pieces_host(lo, hi, cap=256):
     at, n = (C.c_uint32 * cap)(), (C.c_uint32 * cap)()
     k = lib().tagc_dense_pieces_host(lo, hi, at, n, cap)
     return list(zip(at[:k], n[:k])) if k <= cap else None
+
+
+# ------------------------------------------------- include/tagc_train.h
+
+
+def tagc_optim_plan(config: tagc_optim_config, tensors) -> C.c_void_p:
+    """tensors: a list (or C array) of tagc_tensor."""
+    n = len(tensors)
+    arr = tensors if isinstance(tensors, C.Array) else (tagc_tensor * max(n, 1))(*tensors)
+    out = C.c_void_p()
+    _check(lib().tagc_optim_plan(C.byref(config), arr, n, C.byref(out)), "tagc_optim_plan")
+    return out
+
+
+def tagc_optim_destroy(plan):
+    lib().tagc_optim_destroy(plan)
+
+
+def tagc_optim_plan_sizes(plan) -> tagc_optim_sizes:
+    z = tagc_optim_sizes()
+    _check(lib().tagc_optim_plan_sizes(plan, C.byref(z)), "tagc_optim_plan_sizes")
+    return z
+
+
+def tagc_optim_upload(plan, table_dev: int, stream: int = 0):
+    _check(lib().tagc_optim_upload(plan, table_dev, stream), "tagc_optim_upload")
+
+
+def tagc_grad_norm(plan, table_dev: int, control_dev: int, stream: int = 0):
+    _check(lib().tagc_grad_norm(plan, table_dev, control_dev, stream), "tagc_grad_norm")
+
+
+def tagc_adamw_step(plan, table_dev: int, groups, step: int = 0, control_dev=None, stream: int = 0):
+    """groups: a C array of tagc_group (or a list of (lr, weight_decay))."""
+    arr = groups if isinstance(groups, C.Array) else (tagc_group * max(len(groups), 1))(*groups)
+    _check(lib().tagc_adamw_step(plan, table_dev, arr, len(groups), step, control_dev, stream),
+           "tagc_adamw_step")
+
+
+def tagc_adamw_unpack(plan, table_dev: int, m_out, v_out, stream: int = 0):
+    _check(lib().tagc_adamw_unpack(plan, table_dev, m_out, v_out, stream), "tagc_adamw_unpack")
+
+
+def tagc_linear_forward_workspace(l: tagc_linear) -> int:
+    n = C.c_uint64()
+    _check(lib().tagc_linear_forward_workspace(C.byref(l), C.byref(n)), "tagc_linear_forward_workspace")
+    return int(n.value)
+
+
+def tagc_linear_backward_workspace(l: tagc_linear_grad) -> int:
+    n = C.c_uint64()
+    _check(lib().tagc_linear_backward_workspace(C.byref(l), C.byref(n)),
+           "tagc_linear_backward_workspace")
+    return int(n.value)
+
+
+def tagc_linear_forward(l: tagc_linear, workspace=None, stream: int = 0):
+    _check(lib().tagc_linear_forward(C.byref(l), workspace, stream), "tagc_linear_forward")
+
+
+def tagc_linear_backward(l: tagc_linear_grad, workspace=None, stream: int = 0):
+    _check(lib().tagc_linear_backward(C.byref(l), workspace, stream), "tagc_linear_backward")

@@ -13,7 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtagc.so")
 SOURCES = ["plan.cpp", "profile.cpp", "sparsify.hip", "index.hip", "sketch.hip",
-           "decode.hip"]
+           "decode.hip", "optim.hip", "linear.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]

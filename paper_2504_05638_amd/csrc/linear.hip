@@ -10,6 +10,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "device_utils.h"
 #include "tagc_internal.h"
 #include "tagc_train.h"
@@ -19,12 +21,14 @@ namespace tagc {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kSlab = 64;        // k's of a stage in local memory: 128 bytes of a row
 constexpr uint32_t kPackTile = 64;
 constexpr uint32_t kPlanes = 3;       // bfloat16 numbers that a float32 is taken apart into
 constexpr uint32_t kFewRows = 4;      // rows up to which the weights are streamed past the rows instead
+
+constexpr uint64_t kMaxSide = 1u << 22;  // rows, features and direct strides are fewer
 
 inline uint64_t up(uint64_t a, uint64_t b) { return (a + b - 1) / b * b; }
 
@@ -291,16 +295,28 @@ struct Product {
 __device__ inline uint32_t term_p(uint32_t t) { return (0x001102u >> (4 * t)) & 3; }
 __device__ inline uint32_t term_q(uint32_t t) { return (0x010120u >> (4 * t)) & 3; }
 
-// A wave computes RM by RN tiles of 32 by 32, WM by WN waves a workgroup's tile.  Q's rows go in as the matrix
+// A wave computes RM by RN tiles of 16 by 16, WM by WN waves a workgroup's tile.  Q's rows go in as the matrix
 // instruction's first operand, so that a lane ends up with neighbours of a row of C.
+//
+// Slabs of 64 k's pass through two stages of local memory, which global memory is read into directly.  A slab is four parts:
+// two steps of 32 k's by two halves of P's rows, and what a part multiplies is read into registers during the part
+// before, so that a wave waits for local memory only where the waves meet.  That is before a slab's last
+// part: by then all have read the slab's last pieces, its stage is free for the slab after the next, and
+// the next one has come.
+//
+// Bound by the matrix units, and by the power they draw: at 8192 by 8192 by 8192 they are busy for 72 % of the cycles,
+// and the clock falls to some 1.6 GHz.  What was measured on the way (TFLOP/s there): products in the order the compiler
+// found 1113, woven with the reads 1196; 32 x 32 x 16 instructions, which move their sums twice as often, 1196, 16 x 16 x 32 1236;
+// four waves of 128 by 128 1163; eight waves in two groups that take turns at reading and multiplying 1041; slabs
+// of 32 in a ring of four stages, whose loads take half a cache line, 1172.
 template <typename T, int WM, int WN, int RM, int RN>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
 {
-    constexpr uint32_t kThreads = WM * WN * 64, TM = WM * RM * 32, TN = WN * RN * 32;
+    constexpr uint32_t kThreads = WM * WN * 64, TM = WM * RM * 16, TN = WN * RN * 16;
     constexpr uint32_t terms = sizeof(T) == 2 ? 1 : 6;
     constexpr uint32_t kStage = (TM + TN) * kSlab * 2;
     constexpr uint32_t kLoadsP = TM * 8 / kThreads, kLoadsQ = TN * 8 / kThreads;
-    constexpr uint32_t kRow = RN * 32 + 4;  // floats of a row of a wave's strip
+    constexpr uint32_t kRow = RN * 16 + 4;  // floats of a row of a wave's strip
     static_assert(WM * WN * 32 * kRow * 4 <= 2 * kStage, "the strips fit");
     __shared__ __attribute__((aligned(1024))) char stage0[kStage];
     __shared__ __attribute__((aligned(1024))) char stage1[kStage];
@@ -309,7 +325,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     uint32_t b = blockIdx.x;
     const uint32_t tiles = a.tiles_m * a.tiles_n, part = b / tiles;
     b %= tiles;
-    const uint32_t m0 = b % a.tiles_m * TM, n0 = b / a.tiles_m * TN;
+    // Workgroups go to the eight XCDs in turn.  Each XCD gets neighbouring tiles, and goes through them in groups of
+    // eight rows of tiles, so that what its L2 holds is used again.
+    const uint32_t xcd = b % 8, extra = tiles % 8;
+    b = xcd * (tiles / 8) + min(xcd, extra) + b / 8;
+    const uint32_t group = b / (8 * a.tiles_n), left = min(a.tiles_m - group * 8, 8u), in = b - group * 8 * a.tiles_n;
+    const uint32_t m0 = (group * 8 + in % left) * TM, n0 = in / left * TN;
 
     // Where this lane's 16 bytes of each load come from.  A row's eight pieces lie in the stage in an order
     // turned by the row's number, so that lanes that read the same piece of 16 rows meet no
@@ -318,11 +339,11 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     const uint32_t sub = threadIdx.x >> 3, piece = (threadIdx.x & 7) ^ ((sub >> 1) & 7);
 #pragma unroll
     for (uint32_t i = 0; i < kLoadsP; ++i)
-        off_p[i] = min(m0 + sub + i * (kThreads / 8), a.m - 1) - m0;
+        off_p[i] = (min(m0 + sub + i * (kThreads / 8), a.m - 1) - m0) * uint32_t(a.ldp * 2) + piece * 16;
 #pragma unroll
     for (uint32_t i = 0; i < kLoadsQ; ++i)
-        off_q[i] = min(n0 + sub + i * (kThreads / 8), a.n - 1) - n0;
-    const uint16_t *p0 = a.p + uint64_t(m0) * a.ldp, *q0 = a.q + uint64_t(n0) * a.ldq;
+        off_q[i] = (min(n0 + sub + i * (kThreads / 8), a.n - 1) - n0) * uint32_t(a.ldq * 2) + piece * 16;
+    const char *p0 = reinterpret_cast<const char *>(a.p + uint64_t(m0) * a.ldp), *q0 = reinterpret_cast<const char *>(a.q + uint64_t(n0) * a.ldq);
 
     const uint32_t first = part * a.slabs, all = a.k / kSlab * terms;
     const uint32_t count = min(a.slabs, all - first);
@@ -333,98 +354,124 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
             ks = s / terms;
             t = s % terms;
         }
-        const uint16_t *p = p0 + ks * kSlab, *q = q0 + ks * kSlab;
+        const char *p = p0 + ks * (kSlab * 2), *q = q0 + ks * (kSlab * 2);
         if constexpr (terms > 1) {
-            p += term_p(t) * a.plane_p;
-            q += term_q(t) * a.plane_q;
+            p += term_p(t) * a.plane_p * 2;
+            q += term_q(t) * a.plane_q * 2;
         }
 #pragma unroll
         for (uint32_t i = 0; i < kLoadsP; ++i)
             __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void *)(p + uint64_t(off_p[i]) * a.ldp + piece * 8),
+                (const __attribute__((address_space(1))) void *)(p + off_p[i]),
                 (__attribute__((address_space(3))) void *)(stage + (i * kThreads + wave * 64) * 16), 16, 0, 0);
 #pragma unroll
         for (uint32_t i = 0; i < kLoadsQ; ++i)
             __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void *)(q + uint64_t(off_q[i]) * a.ldq + piece * 8),
+                (const __attribute__((address_space(1))) void *)(q + off_q[i]),
                 (__attribute__((address_space(3))) void *)(stage + TM * 128 + (i * kThreads + wave * 64) * 16), 16, 0, 0);
     };
 
-    f32x16 acc[RM][RN];
+    f32x4 acc[RM][RN];
 #pragma unroll
     for (int i = 0; i < RM; ++i)
 #pragma unroll
         for (int j = 0; j < RN; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
 
-    bf16x8 fp[2][RM], fq[2][RN];
-    const uint32_t row_p = wm * RM * 32 + (lane & 31), row_q = wn * RN * 32 + (lane & 31);
-    // (rows 32 further on are turned the same way)
-    auto read = [&](const char *stage, uint32_t step, int to) {
-        const uint32_t c = step * 2 + (lane >> 5);
+    constexpr int H = RM / 2;
+    bf16x8 fp[2][H], fq[2][RN];
+    const uint32_t row_p = wm * RM * 16 + (lane & 15), row_q = wn * RN * 16 + (lane & 15);
+    // (rows 16 further on are turned the same way)
+    auto read_q = [&](const char *stage, uint32_t step) {
+        const uint32_t c = step * 4 + (lane >> 4);
 #pragma unroll
         for (int j = 0; j < RN; ++j)
-            fq[to][j] = *reinterpret_cast<const bf16x8 *>(stage + TM * 128 + (row_q + 32 * j) * 128 + ((c ^ ((row_q >> 1) & 7)) << 4));
-#pragma unroll
-        for (int i = 0; i < RM; ++i)
-            fp[to][i] = *reinterpret_cast<const bf16x8 *>(stage + (row_p + 32 * i) * 128 + ((c ^ ((row_p >> 1) & 7)) << 4));
+            fq[step][j] = *reinterpret_cast<const bf16x8 *>(stage + TM * 128 + (row_q + 16 * j) * 128 + ((c ^ ((row_q >> 1) & 7)) << 4));
     };
-    auto multiply = [&](int from) {
+    auto read_p = [&](const char *stage, uint32_t step, int half) {
+        const uint32_t c = step * 4 + (lane >> 4);
 #pragma unroll
-        for (int i = 0; i < RM; ++i)
+        for (int i = 0; i < H; ++i)
+            fp[half][i] = *reinterpret_cast<const bf16x8 *>(stage + (row_p + 16 * (half * H + i)) * 128 + ((c ^ ((row_p >> 1) & 7)) << 4));
+    };
+    auto multiply = [&](int step, int half) {
+#pragma unroll
+        for (int i = 0; i < H; ++i)
 #pragma unroll
             for (int j = 0; j < RN; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[from][j], fp[from][i], acc[i][j], 0, 0, 0);
+                acc[half * H + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fq[step][j], fp[half][i], acc[half * H + i][j], 0, 0, 0);
+    };
+    // The next pieces are read while the products of the last ones run, one read behind each of the first products.
+    auto woven = [&](auto reads) {
+#pragma unroll
+        for (int i = 0; i < H * RN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i < decltype(reads)::value) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
     };
     // What this wave has asked for has come, then what the others have.
     auto arrived = [&]() {
         wait_own_memory_ops();
         __syncthreads();
     };
-    // One slab: its first pieces are in registers, the next slab is on its way to `next`.  Before the last
-    // products everything of this slab has been read, so that its stage can be filled anew.
+    // One slab: its first pieces are in registers, the next slab is on its way to `next`.  (Behind the last slab the
+    // last one is fetched again, and never used: a branch here would cost the registers that the loop lacks.)
     auto slab = [&](uint32_t s, char *now, char *next) {
-        read(now, 1, 1);
-        multiply(0);
-        read(now, 2, 0);
-        multiply(1);
-        read(now, 3, 1);
-        multiply(0);
+        read_p(now, 0, 1);
+        multiply(0, 0);
+        woven(std::integral_constant<int, H>());
+        read_q(now, 1);
+        read_p(now, 1, 0);
+        multiply(0, 1);
+        woven(std::integral_constant<int, H + RN>());
+        read_p(now, 1, 1);
+        multiply(1, 0);
+        woven(std::integral_constant<int, H>());
+        // (from here to the next meeting a wave goes before those that have not got here)
+        __builtin_amdgcn_s_setprio(0);
         arrived();
-        if (s + 2 < count) fetch(first + s + 2, now);
-        if (s + 1 < count) read(next, 0, 0);
-        multiply(1);
+        __builtin_amdgcn_s_setprio(1);
+        fetch(first + min(s + 2, count - 1), now);
+        read_q(next, 0);
+        read_p(next, 0, 0);
+        multiply(1, 1);
+#pragma unroll
+        for (int i = 0; i < H * RN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i < H + RN) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (i % (H * RN / (kLoadsP + kLoadsQ)) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
     };
 
     fetch(first, stage0);
-    if (count > 1) fetch(first + 1, stage1);
+    fetch(first + min(1u, count - 1), stage1);
     arrived();
-    read(stage0, 0, 0);
+    read_q(stage0, 0);
+    read_p(stage0, 0, 0);
     for (uint32_t s = 0; s < count; s += 2) {
         slab(s, stage0, stage1);
         if (s + 1 < count) slab(s + 1, stage1, stage0);
     }
-    __syncthreads();
+    arrived();
 
     // Results go through the wave's own strip of local memory, 32 rows at a time, so that a row's neighbours
     // are written together.
     float *strip = reinterpret_cast<float *>(wave * 32 * kRow * 4 + 32 * kRow * 4 <= kStage ? stage0 + wave * 32 * kRow * 4
                                                                                             : stage1 + (wave - kStage / (32 * kRow * 4)) * 32 * kRow * 4);
 #pragma unroll
-    for (int i = 0; i < RM; ++i) {
+    for (int i = 0; i < RM; i += 2) {
 #pragma unroll
-        for (int j = 0; j < RN; ++j)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *reinterpret_cast<float4 *>(strip + (lane & 31) * kRow + 32 * j + 8 * e + 4 * (lane >> 5)) =
-                    make_float4(acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]);
+            for (int j = 0; j < RN; ++j)
+                *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[i + h][j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        constexpr uint32_t across = RN * 4, rows = 64 / across;
+        constexpr uint32_t across = RN * 2, rows = 64 / across;
 #pragma unroll 1
         for (uint32_t r = 0; r < 32; r += rows) {
             const uint32_t lr = r + lane / across, ln = lane % across * 8;
-            const uint32_t m = m0 + (wm * RM + i) * 32 + lr, n = n0 + wn * RN * 32 + ln;
+            const uint32_t m = m0 + (wm * RM + i) * 16 + lr, n = n0 + wn * RN * 16 + ln;
             float z[8];
 #pragma unroll
             for (int h = 0; h < 8; h += 4) {
@@ -577,7 +624,7 @@ struct Operand {
 // whether rows of k elements can be read as they lie
 bool as_it_lies(uint32_t dtype, const void *p, uint64_t ld, uint64_t k)
 {
-    return dtype == TAGC_BF16 && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && k % kSlab == 0;
+    return dtype == TAGC_BF16 && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && ld < kMaxSide && k % kSlab == 0;
 }
 
 uint32_t planes_of(uint32_t dtype) { return dtype == TAGC_F32 ? kPlanes : 1; }
@@ -620,8 +667,8 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     const uint32_t grid = f.tiles_m * f.tiles_n * f.splits;
     if (grid) {
         ProfileScope prof("linear_product", s);
-        if (f.large) product_kernel<T, 2, 4, 4, 2><<<grid, 512, 0, s>>>(a);
-        else product_kernel<T, 2, 2, 2, 2><<<grid, 256, 0, s>>>(a);
+        if (f.large) product_kernel<T, 2, 4, 8, 4><<<grid, 512, 0, s>>>(a);
+        else product_kernel<T, 2, 2, 4, 4><<<grid, 256, 0, s>>>(a);
     }
     if (f.splits != 1) {
         ProfileScope prof("linear_join", s);
@@ -645,7 +692,8 @@ bool good(const void *p, uint64_t ld, uint64_t cols, uint64_t bytes) { return !p
 int check_sizes(uint64_t rows, uint64_t in, uint64_t out, uint32_t dtype, uint32_t act)
 {
     if (dtype > TAGC_BF16 || act > TAGC_ACT_SILU) return TAGC_EINVAL;
-    if (rows >= (1ull << 26) || in >= (1ull << 26) || out >= (1ull << 26)) return TAGC_ESIZE;
+    // a tile's 256 rows span fewer than 2^32 bytes
+    if (rows >= kMaxSide || in >= kMaxSide || out >= kMaxSide) return TAGC_ESIZE;
     // a launch has fewer than 2^32 threads: at most a workgroup of 256 for a tile of 64 by 64
     const uint64_t r = up(rows, 64) / 64, i = up(in, 64) / 64, o = up(out, 64) / 64;
     if (r * i >= (1ull << 24) || r * o >= (1ull << 24) || i * o >= (1ull << 24)) return TAGC_ESIZE;

@@ -11,6 +11,8 @@ marshalling only; all arithmetic is the library's (include/tagc_train.h).
 """
 from __future__ import annotations
 
+import math
+
 import torch
 
 from . import binding as B
@@ -26,52 +28,66 @@ def _need(condition, what):
         raise ValueError(what)
 
 
-def _rows_of(t, name, shape, like):
-    """(address, elements from row to row) of a matrix; None for None."""
+# (the address of the device's current stream, without the object around it where torch offers that: a
+# third of what a small call costs the host)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(stream, device):
+    if stream is None and _raw_stream is not None and device.index is not None:
+        return _raw_stream(device.index)
+    return _stream_ptr(stream)
+
+
+def _rows_of(t, name, rows, cols, dtype, device):
+    """(address, elements from row to row) of a [rows, cols] matrix; (None, 0) for None."""
     if t is None:
         return None, 0
-    _need(t.dtype == like.dtype and t.device == like.device, "%s: a %s on %s is wanted" % (name, like.dtype, like.device))
-    _need(tuple(t.shape) == tuple(shape), "%s has shape %s, %s is wanted" % (name, tuple(t.shape), tuple(shape)))
-    rows, cols = shape
-    _need(cols <= 1 or rows == 0 or t.stride(1) == 1, "%s: a row's elements must be neighbours" % name)
-    # (of a single row the stride says nothing; of no elements neither does the address)
-    ld = t.stride(0) if rows > 1 and cols > 0 else cols
-    _need(ld >= cols, "%s: rows must not overlap" % name)
-    return t.data_ptr() if t.numel() else None, ld
+    if t.dtype != dtype or t.device != device:
+        raise ValueError("%s: a %s on %s is wanted" % (name, dtype, device))
+    if t.shape != (rows, cols):
+        raise ValueError("%s has shape %s, %s is wanted" % (name, tuple(t.shape), (rows, cols)))
+    ld, step = t.stride()
+    if rows <= 1 or cols == 0:  # (of a single row the stride says nothing; of no elements neither does the address)
+        ld = cols
+    if (step != 1 and cols > 1 and rows > 0) or ld < cols:
+        raise ValueError("%s: a row's elements must be neighbours, and rows must not overlap" % name)
+    return t.data_ptr() or None, ld
 
 
-def _vector(t, name, n, like):
+def _vector(t, name, n, dtype, device):
     if t is None:
         return None
-    _need(t.dtype == like.dtype and t.device == like.device, "%s: a %s on %s is wanted" % (name, like.dtype, like.device))
-    _need(tuple(t.shape) == (n,) and (n <= 1 or t.stride(0) == 1), "%s: a contiguous vector of %d is wanted" % (name, n))
-    return t.data_ptr() if n else None
+    if t.dtype != dtype or t.device != device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s: a contiguous vector of %d, %s on %s, is wanted" % (name, n, dtype, device))
+    return t.data_ptr() or None
 
 
-def _check_input(x, w):
-    _need(x.is_cuda and x.dtype in _TYPES, "x: a CUDA tensor of float32 or bfloat16 is wanted")
-    _need(w.dim() == 2 and x.dim() >= 2 and x.shape[-1] == w.shape[1],
-          "x is [..., in] and w [out, in]: got %s and %s" % (tuple(x.shape), tuple(w.shape)))
+def _check_input(x, w, activation):
+    if not x.is_cuda or x.dtype not in _TYPES:
+        raise ValueError("x: a CUDA tensor of float32 or bfloat16 is wanted")
+    if w.dim() != 2 or x.dim() < 2 or x.shape[-1] != w.shape[1]:
+        raise ValueError("x is [..., in] and w [out, in]: got %s and %s" % (tuple(x.shape), tuple(w.shape)))
+    if activation not in _ACTS:
+        raise ValueError("activation: one of %s is wanted" % ", ".join(k for k in _ACTS if k))
 
 
-def _flat(t, cols):
-    """[..., cols] as [rows, cols] without a copy."""
+def _flat(t, rows, cols):
+    """[..., cols] as [rows, cols] without a copy (ValueError if its strides need one)."""
     if t is None or t.dim() == 2:
         return t
-    rows = t.numel() // cols if cols else t[..., 0:0].flatten(0, -2).shape[0]
-    return t.view(rows, cols)
-
-
-def _act(name):
-    _need(name in _ACTS, "activation: one of %s is wanted" % ", ".join(k for k in _ACTS if k))
-    return _ACTS[name]
+    try:
+        return t.view(rows, cols)
+    except RuntimeError as e:
+        raise ValueError(str(e)) from None
 
 
 def _work(nbytes, x, stream):
-    """A call's workspace; kept from reuse until `stream`, where it is not the current one, is done."""
+    """A call's workspace (its tensor and its address); kept from reuse until `stream`, where it is not the current
+    one, is done."""
     if not nbytes:
         return None, None
-    ws = _bytes(nbytes, x.device)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
     if stream is not None:
         ws.record_stream(stream)
     return ws, ws.data_ptr()
@@ -81,26 +97,29 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     """(y, pre): y = activation(x w^T + bias) + residual.  x: [..., in], w: [out, in].  `save`: pre =
     x w^T + bias for linear_backward (else None).  `out` and `pre` may be given; `out` may be
     the residual.  Tensors made here belong to the current stream."""
-    _check_input(x, w)
+    _check_input(x, w, activation)
     n, k = w.shape
-    lead = x.shape[:-1]
-    x2 = _flat(x, k)
-    m = x2.shape[0]
-    act = _act(activation)
-    _need(not (pre is not None and not save), "pre is given, but save is not")
-    y = torch.empty(*lead, n, dtype=x.dtype, device=x.device) if out is None else out
+    shape, dtype, device = x.shape, x.dtype, x.device
+    m = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
+    _need(pre is None or save, "pre is given, but save is not")
+    xp, ldx = _rows_of(_flat(x, m, k), "x", m, k, dtype, device)
+    wp, ldw = _rows_of(w, "w", n, k, dtype, device)
+    bp = _vector(bias, "bias", n, dtype, device)
+    rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
+    if out is None:
+        out = x.new_empty((*shape[:-1], n))
+        yp, ldy = out.data_ptr() or None, n
+    else:
+        yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
     if save and pre is None:
-        pre = torch.empty(*lead, n, dtype=x.dtype, device=x.device)
-    a = B.tagc_linear(rows=m, in_=k, out=n, dtype=_TYPES[x.dtype], activation=act)
-    a.x, a.ldx = _rows_of(x2, "x", (m, k), x)
-    a.w, a.ldw = _rows_of(w, "w", (n, k), x)
-    a.bias = _vector(bias, "bias", n, x)
-    a.residual, a.ldr = _rows_of(_flat(residual, n), "residual", (m, n), x)
-    a.y, a.ldy = _rows_of(_flat(y, n), "out", (m, n), x)
-    a.pre, a.ldp = _rows_of(_flat(pre, n), "pre", (m, n), x)
+        pre = x.new_empty((*shape[:-1], n))
+        pp, ldp = pre.data_ptr() or None, n
+    else:
+        pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
+    a = B.tagc_linear(m, k, n, _TYPES[dtype], _ACTS[activation], xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp)
     ws, at = _work(B.tagc_linear_forward_workspace(a), x, stream)
-    B.tagc_linear_forward(a, at, _stream_ptr(stream))
-    return y, pre
+    B.tagc_linear_forward(a, at, _stream_of(stream, device))
+    return out, pre
 
 
 def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=None, accumulate=False,
@@ -108,26 +127,27 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     """dx (None without need_dx).  With `dw` ([out, in], a view into a bucket's gradient) and `db` ([out])
     given, the weight's and the bias's gradient are written there, or added to what is there
     (accumulate).  `pre`: what linear(save=True) gave; None without an activation."""
-    _check_input(x, w)
+    _check_input(x, w, activation)
     n, k = w.shape
-    x2, dy2 = _flat(x, k), _flat(dy, n)
-    m = x2.shape[0]
-    act = _act(activation)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    m = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
+    act = _ACTS[activation]
     _need((act != B.TAGC_ACT_NONE) == (pre is not None), "pre is wanted with an activation, and only then")
     _need(need_dx or dx is None, "dx is given, but need_dx is not")
+    xp, ldx = _rows_of(_flat(x, m, k), "x", m, k, dtype, device)
+    wp, ldw = _rows_of(w, "w", n, k, dtype, device)
+    pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
+    yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
     if need_dx and dx is None:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    a = B.tagc_linear_grad(rows=m, in_=k, out=n, dtype=_TYPES[x.dtype], activation=act,
-                           accumulate=int(bool(accumulate)))
-    a.x, a.ldx = _rows_of(x2, "x", (m, k), x)
-    a.w, a.ldw = _rows_of(w, "w", (n, k), x)
-    a.pre, a.ldp = _rows_of(_flat(pre, n), "pre", (m, n), x)
-    a.dy, a.lddy = _rows_of(dy2, "dy", (m, n), x)
-    a.dx, a.lddx = _rows_of(_flat(dx, k), "dx", (m, k), x)
-    a.dw, a.lddw = _rows_of(dw, "dw", (n, k), x)
-    a.db = _vector(db, "db", n, x)
+        dx = x.new_empty(shape)
+        dp, ldd = dx.data_ptr() or None, k
+    else:
+        dp, ldd = _rows_of(_flat(dx, m, k), "dx", m, k, dtype, device)
+    gp, ldg = _rows_of(dw, "dw", n, k, dtype, device)
+    a = B.tagc_linear_grad(m, k, n, _TYPES[dtype], act, xp, ldx, wp, ldw, pp, ldp, yp, ldy, dp, ldd, gp, ldg,
+                           _vector(db, "db", n, dtype, device), 1 if accumulate else 0, 0)
     ws, at = _work(B.tagc_linear_backward_workspace(a), x, stream)
-    B.tagc_linear_backward(a, at, _stream_ptr(stream))
+    B.tagc_linear_backward(a, at, _stream_of(stream, device))
     return dx
 
 
@@ -138,7 +158,7 @@ class AdamW:
     `params`, `grads`: float32 or bfloat16, tensor by tensor.  `copies`: bfloat16 tensors that get
     the updated parameters, or None (for single ones too).  `bits`: 32, or 8 (m, v: uint8 of the tensor's
     length; bases: int32, one per 256 elements).  `groups`: (lr, weight_decay) pairs, `group_of`: each
-    tensor's.  groups may be changed between steps.  Without params only grad_norm() can be
+    tensor's.  `opt.groups = ...` changes them between steps.  Without params only grad_norm() can be
     called.  The tensors must stay where they are: a gradient is written into, not replaced."""
 
     def __init__(self, params=None, grads=(), m=None, v=None, bases=None, copies=None, groups=((1e-3, 0.01),),
@@ -151,7 +171,7 @@ class AdamW:
         self.device = grads[0].device
         _need(self.device.type == "cuda", "libtagc needs a GPU: no CPU path exists")
         group_of = [0] * n if group_of is None else list(group_of)
-        self.groups = [tuple(g) for g in groups]
+        self.groups = groups
         self.bits, self.grads = bits, grads
         self.params = list(params) if params is not None else None
         lists = {"params": self.params, "copies": copies, "m": m, "v": v, "bases": bases, "group_of": group_of}
@@ -192,7 +212,10 @@ class AdamW:
         start[0] = first_step - 1
         start.view(torch.float32)[5] = 1.0
         self.control = start.to(self.device)
-        B.tagc_optim_upload(self.plan, self.table.data_ptr(), _stream_ptr())
+        f = self.control.view(torch.float32)
+        self.norm, self.factor, self.lr_scale = f[3], f[4], f[5]
+        self._table, self._control = self.table.data_ptr(), self.control.data_ptr()
+        B.tagc_optim_upload(self.plan, self._table, _stream_ptr())
         torch.cuda.current_stream().synchronize()
 
     @staticmethod
@@ -204,27 +227,36 @@ class AdamW:
               "%s[%d]: a contiguous tensor of %d, %s on %s, is wanted" % (name, i, k, " or ".join(map(str, types)), self.device))
         return t.data_ptr() if k else None
 
+    @property
+    def groups(self):
+        return self._groups
+
+    @groups.setter
+    def groups(self, groups):
+        groups = tuple((float(lr), float(decay)) for lr, decay in groups)
+        _need(not hasattr(self, "_groups") or len(groups) == len(self._groups), "groups: as many as there were are wanted")
+        self._groups = groups
+        self._group_array = (B.tagc_group * max(len(groups), 1))(*groups)
+
     def grad_norm(self, stream=None):
-        """Begins a step; (norm, factor) as device scalars, views of the control block."""
-        B.tagc_grad_norm(self.plan, self.table.data_ptr(), self.control.data_ptr(), _stream_ptr(stream))
-        f = self.control.view(torch.float32)
-        return f[3], f[4]
+        """Begins a step; (norm, factor): device scalars, views of the control block."""
+        B.tagc_grad_norm(self.plan, self._table, self._control, _stream_of(stream, self.device))
+        return self.norm, self.factor
 
     def step(self, step=0, stream=None):
-        """One step: the one that grad_norm() began, or, with `step` > 0, that one, unclipped."""
-        B.tagc_adamw_step(self.plan, self.table.data_ptr(), self.groups, step,
-                          self.control.data_ptr(), _stream_ptr(stream))
-
-    @property
-    def lr_scale(self):
-        """Device scalar that the groups' learning rates are multiplied by in step(0)."""
-        return self.control.view(torch.float32)[5]
+        """One step: the one that grad_norm() began, its learning rates times the device scalar
+        `lr_scale`; or, with `step` > 0, that one, unclipped, with the groups' learning rates."""
+        B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control,
+                          _stream_of(stream, self.device))
 
     def unpack(self, stream=None):
         """(m, v): what 8-bit moments stand for, bfloat16, the tensors one behind the other."""
         m, v = (torch.empty(self.sizes.n_elems, dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        B.tagc_adamw_unpack(self.plan, self.table.data_ptr(), m.data_ptr() or None, v.data_ptr() or None,
-                            _stream_ptr(stream))
+        if stream is not None:
+            m.record_stream(stream)
+            v.record_stream(stream)
+        B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None,
+                            _stream_of(stream, self.device))
         return m, v
 
     def close(self):

@@ -108,7 +108,7 @@ def _bwd(**kw):
 @pytest.mark.parametrize("bad,code", [(dict(dtype=2), -1), (dict(activation=5), -1), (dict(x=None), -1), (dict(w=None), -1), (dict(y=None), -1),
                                       (dict(x=AT + 1), -1), (dict(ldx=127), -1), (dict(ldw=1), -1), (dict(ldy=63), -1),
                                       (dict(residual=AT, ldr=63), -1), (dict(pre=AT + 1, ldp=64), -1), (dict(bias=AT + 1), -1),
-                                      (dict(dtype=0, x=AT + 2), -1), (dict(rows=1 << 26), -2), (dict(in_=1 << 26, ldx=1 << 26, ldw=1 << 26), -2),
+                                      (dict(dtype=0, x=AT + 2), -1), (dict(rows=1 << 22), -2), (dict(in_=1 << 22, ldx=1 << 22, ldw=1 << 22), -2),
                                       (dict(rows=1 << 20, out=1 << 18, ldy=1 << 18), -2)])
 def test_forward_refuses(bad, code):
     assert _code(B.tagc_linear_forward_workspace, _fwd(**bad)) == code

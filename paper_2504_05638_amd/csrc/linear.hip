@@ -1,12 +1,14 @@
 // Linear layers at the two ends of the exchange: y = act(x w^T + b) + r, and its gradients.
 //
-// All products are of one form, C[m, n] = sum over k of P[m, k] Q[n, k] with both operands' k contiguous:
-//   forward       P = x,     Q = w      (k: features in)
-//   dx            P = dz,    Q = w^T    (k: features out)
-//   dw            P = dz^T,  Q = x^T    (k: tokens)
-// What does not lie like that -- operands to be turned, rows off a 16-byte boundary, a k that is no multiple
-// of a slab, float32 -- is first laid out anew in the workspace by pack_kernel; its cost is in
-// the order of an operand's bytes, the product's in that of rows times operand.
+// All products are of one form, C[m, n] = sum over k of P[m, k] Q[n, k]:
+//   forward       P = x,               Q = w                   (k: features in)
+//   dx            P = dz,              Q = w, k by k           (k: features out)
+//   dw            P = dz, k by k       Q = x, k by k           (k: tokens)
+// An operand lies in memory row by row, with a row's k's next to each other, or k by k, with a k's rows next
+// to each other (`turned`); local memory holds it as it lies, and the transposing read takes it from there.
+// What cannot be read as it lies -- rows off a 16-byte boundary, float32, dz where there is an
+// activation -- is first laid out anew in the workspace by pack_kernel; its cost is in the order of an
+// operand's bytes, the product's in that of rows times operand.
 #include <math.h>
 #include <string.h>
 
@@ -24,9 +26,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kSlab = 64;        // k's of a stage in local memory: 128 bytes of a row
-constexpr uint32_t kPackTile = 64;
+constexpr uint32_t kPackRows = 64;
 constexpr uint32_t kPlanes = 3;       // bfloat16 numbers that a float32 is taken apart into
-constexpr uint32_t kFewRows = 4;      // rows up to which the weights are streamed past the rows instead
+// rows up to which few_kernel goes: in bfloat16 a thin tile is faster from 17 rows on (weights of 4096 by 11008, 17, 32, 64
+// rows: 32, 35, 48 us, 23, 24, 26 as tiles), in float32 the weights would have to be taken apart first (83, 86, 129 us; 164, 162, 167)
+constexpr uint32_t kFewRows[2] = {64, 16};  // TAGC_F32, TAGC_BF16
 
 constexpr uint64_t kMaxSide = 1u << 22;  // rows, features and direct strides are fewer
 
@@ -112,103 +116,91 @@ struct PackArgs {
     uint64_t ld, ldp;
     uint32_t rows, cols;
     uint32_t act;
-    uint16_t *straight;   // [rows, straight_ld] or NULL, zeros behind cols
-    uint16_t *turned;     // [cols, turned_ld] or NULL, zeros behind rows
-    uint64_t straight_ld, turned_ld, straight_plane, turned_plane;
+    uint16_t *to;         // [rows, to_ld] or NULL, zeros behind cols
+    uint64_t to_ld, to_plane;
     float *sums;          // [tiles of rows, cols] or NULL: sums over a tile's rows
 };
 
-// The bfloat16 numbers that a packed value goes to: itself rounded, or three that add up to it but for
-// 2^-24 of it (an infinity or NaN stays in the first).
+// The bfloat16 numbers that a packed value goes to: itself rounded, or three that add up to it: cut off behind 8 bits (what is
+// finite stays finite), the rest rounded to 8 bits, and what is then left, which has no more than 8.
+// (Of an infinity the second is NaN.)
 template <typename T>
 __device__ inline void split(float x, uint16_t (&out)[sizeof(T) == 2 ? 1 : 3])
 {
-    out[0] = uint16_t(round_to_bf16(x));
-    if constexpr (sizeof(T) == 4) {
-        const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
-        // (cut off, not rounded: what is finite stays finite)
-        if (finite) out[0] = uint16_t(__float_as_uint(x) >> 16);
-        const float y = finite ? x - __uint_as_float(uint32_t(out[0]) << 16) : 0.0f;
-        out[1] = uint16_t(round_to_bf16(y));
-        const float w = y - __uint_as_float(uint32_t(out[1]) << 16);
-        out[2] = uint16_t(round_to_bf16(w));
+    if constexpr (sizeof(T) == 2) {
+        out[0] = uint16_t(round_to_bf16(x));
+    } else {
+        const uint32_t b = __float_as_uint(x);
+        const float y = x - __uint_as_float(b & 0xFFFF0000u);
+        const uint32_t c = __float_as_uint(y) + 0x8000u;
+        const float w = y - __uint_as_float(c & 0xFFFF0000u);
+        out[0] = uint16_t(b >> 16);
+        out[1] = uint16_t(c >> 16);
+        out[2] = uint16_t(__float_as_uint(w) >> 16);
     }
 }
 
-// A workgroup takes a tile of 64 by 64: reads it once, along the source's rows, and writes what is asked for.
+// A workgroup takes a tile of kPackRows by 64, a thread four neighbours of each sixteenth row.
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(PackArgs a)
 {
     constexpr int planes = sizeof(T) == 2 ? 1 : 3;
-    __shared__ float tile[kPackTile][kPackTile + 1];
-    const uint32_t tiles_c = (a.cols + kPackTile - 1) / kPackTile;
-    const uint32_t r0 = blockIdx.x / tiles_c * kPackTile, c0 = blockIdx.x % tiles_c * kPackTile;
+    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+    __shared__ float sums[16][64];
+    const uint32_t tiles_c = (a.cols + 63) / 64;
+    const uint32_t tile = blockIdx.x / tiles_c, r0 = tile * kPackRows, c = blockIdx.x % tiles_c * 64 + threadIdx.x % 16 * 4;
     const T *src = static_cast<const T *>(a.src), *pre = static_cast<const T *>(a.pre);
-    const uint32_t c4 = threadIdx.x % 16 * 4;
+    float x[kPackRows / 16][4] = {}, sum[4] = {};
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-        const uint32_t lr = threadIdx.x / 16 + 16 * i, r = r0 + lr, c = c0 + c4;
-        float x[4] = {0, 0, 0, 0}, z[4] = {0, 0, 0, 0};
+    for (uint32_t i = 0; i < kPackRows / 16; ++i) {
+        const uint32_t r = r0 + threadIdx.x / 16 + 16 * i;
+        float z[4] = {};
         if (r < a.rows) {
             if (c + 4 <= a.cols) {
-                load_n<T, 4>(src + r * a.ld + c, x);
+                load_n<T, 4>(src + r * a.ld + c, x[i]);
                 if (pre) load_n<T, 4>(pre + r * a.ldp + c, z);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (c + j >= a.cols) continue;
-                    x[j] = widen(src[r * a.ld + c + j]);
+                    x[i][j] = widen(src[r * a.ld + c + j]);
                     if (pre) z[j] = widen(pre[r * a.ldp + c + j]);
                 }
             }
         }
+        // (rows and columns that do not exist are 0 whatever the slope at 0 is)
+        if (pre)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            // (rows and columns that do not exist are 0 whatever the slope at 0 is)
-            if (pre) x[j] *= slope(z[j], a.act);
-            tile[lr][c4 + j] = x[j];
-        }
-        if (a.straight && r < a.rows) {
-            typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+            for (int j = 0; j < 4; ++j) x[i][j] *= slope(z[j], a.act);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += x[i][j];
+    }
+    if (a.to)
+#pragma unroll
+        for (uint32_t i = 0; i < kPackRows / 16; ++i) {
+            const uint32_t r = r0 + threadIdx.x / 16 + 16 * i;
+            if (r >= a.rows) break;
             u16x4 out[planes];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint16_t s[planes];
-                split<T>(x[j], s);
+                split<T>(x[i][j], s);
 #pragma unroll
                 for (int q = 0; q < planes; ++q) out[q][j] = s[q];
             }
-            if (c < a.straight_ld)
 #pragma unroll
-                for (int q = 0; q < planes; ++q)
-                    *reinterpret_cast<u16x4 *>(a.straight + q * a.straight_plane + r * a.straight_ld + c) = out[q];
+            for (int q = 0; q < planes; ++q) *reinterpret_cast<u16x4 *>(a.to + q * a.to_plane + r * a.to_ld + c) = out[q];
         }
-    }
+    if (!a.sums) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[threadIdx.x / 16][threadIdx.x % 16 * 4 + j] = sum[j];
     __syncthreads();
-    if (a.turned) {
-        const uint32_t r4 = threadIdx.x % 16 * 4;
+    const uint32_t at = blockIdx.x % tiles_c * 64 + threadIdx.x;
+    if (threadIdx.x < 64 && at < a.cols) {
+        float all = 0;
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            const uint32_t lc = threadIdx.x / 16 + 16 * i;
-            if (c0 + lc >= a.cols || r0 + r4 >= a.turned_ld) continue;
-            typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-            u16x4 out[planes];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint16_t s[planes];
-                split<T>(tile[r4 + j][lc], s);
-#pragma unroll
-                for (int q = 0; q < planes; ++q) out[q][j] = s[q];
-            }
-#pragma unroll
-            for (int q = 0; q < planes; ++q)
-                *reinterpret_cast<u16x4 *>(a.turned + q * a.turned_plane + uint64_t(c0 + lc) * a.turned_ld + r0 + r4) = out[q];
-        }
-    }
-    if (a.sums && threadIdx.x < kPackTile && c0 + threadIdx.x < a.cols) {
-        float sum = 0;
-        for (uint32_t r = 0; r < kPackTile; ++r) sum += tile[r][threadIdx.x];
-        a.sums[uint64_t(r0 / kPackTile) * a.cols + c0 + threadIdx.x] = sum;
+        for (uint32_t r = 0; r < 16; ++r) all += sums[r][threadIdx.x];
+        a.sums[uint64_t(tile) * a.cols + at] = all;
     }
 }
 
@@ -280,8 +272,8 @@ __device__ inline void finish(const Result &r, uint32_t m, uint32_t n, uint32_t 
 // ------------------------------------------------------------------ the product
 
 struct Product {
-    const uint16_t *p, *q;          // [m, k], [n, k] bfloat16, 16-byte aligned, k a multiple of kSlab
-    uint64_t ldp, ldq;              // multiples of 8
+    const uint16_t *p, *q;          // bfloat16, [m, k] and [n, k], or turned [k, m] and [k, n]; 4-byte aligned
+    uint64_t ldp, ldq;              // multiples of 2; k a multiple of 8 where rows lie row by row
     uint64_t plane_p, plane_q;      // from one of the three parts of a float32 to the next
     uint32_t m, n, k;
     uint32_t tiles_m, tiles_n;
@@ -294,6 +286,99 @@ struct Product {
 // The six products of parts whose sum is a float32 product but for 2^-24 of it, smallest first.
 __device__ inline uint32_t term_p(uint32_t t) { return (0x001102u >> (4 * t)) & 3; }
 __device__ inline uint32_t term_q(uint32_t t) { return (0x010120u >> (4 * t)) & 3; }
+
+// One operand of a workgroup's tile: how its slabs get into local memory, 16 bytes a lane, and from there into the matrix
+// instruction's registers (lane l holds row l % 16, k's 8 (l / 16) to 8 (l / 16) + 7).  R rows, kSlab k's.  The
+// loads go through a buffer descriptor that ends where the operand ends: what lies behind comes as zeros.
+template <bool TURNED, uint32_t R, uint32_t THREADS>
+struct Side;
+
+constexpr uint32_t kMostBytes = 1u << 31;  // of a descriptor, and ...
+constexpr uint32_t kNowhere = 3u << 30;    // ... an offset behind every one; what a tile reads has smaller offsets
+
+__device__ inline __amdgpu_buffer_rsrc_t described(const uint16_t *p, uint64_t elems)
+{
+    const uint64_t bytes = elems * 2;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, bytes < kMostBytes ? uint32_t(bytes) : kMostBytes, 0x00020000);
+}
+__device__ inline void load_lds(__amdgpu_buffer_rsrc_t from, uint32_t off, char *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, off, 0, 0, 0);
+}
+
+// Row by row: 128 bytes of k's to a row.  Its eight pieces of 16 bytes lie in an order turned by the row's
+// number, so that lanes that read the same piece of 16 rows meet no bank twice.
+template <uint32_t R, uint32_t THREADS>
+struct Side<false, R, THREADS> {
+    static constexpr uint32_t kLoads = R * 8 / THREADS;
+    uint32_t off[kLoads], k, lane;
+    __device__ inline Side(uint32_t, uint64_t ld)
+    {
+        const uint32_t sub = threadIdx.x >> 3, piece = (threadIdx.x & 7) ^ ((sub >> 1) & 7);
+        lane = threadIdx.x & 63;
+        k = piece * 8;
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) off[i] = (sub + i * (THREADS / 8)) * uint32_t(ld * 2) + piece * 16;
+    }
+    __device__ inline void fetch(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld, char *stage, uint32_t wave) const
+    {
+        // (of a row whose k's are no multiple of eight there are zeros up to one)
+        const __amdgpu_buffer_rsrc_t from = described(p + r0 * ld + k0, (rows - r0 - 1) * ld + ((end + 7) & ~7u) - k0);
+        const bool there = k0 + k < end;  // (the next row lies behind the last k)
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) load_lds(from, there ? off[i] : kNowhere, stage + (i * THREADS + wave * 64) * 16);
+    }
+    // N tiles of 16 rows from `tile` on, 32 k's
+    template <int N>
+    __device__ inline void read(const char *stage, uint32_t tile, uint32_t step, bf16x8 (&to)[N]) const
+    {
+        const uint32_t row = lane & 15, c = step * 4 + (lane >> 4);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            to[i] = *reinterpret_cast<const bf16x8 *>(stage + (tile * 16 + row + 16 * i) * 128 + ((c ^ (row >> 1)) << 4));
+    }
+};
+
+// K by k: 2 R bytes of rows to a k.  The transposing read gives each of 16 lanes one row of four k's, whose 32
+// bytes each lie in four k's places; a wave reads 16 k's so.  Pairs of pieces lie in an order turned by the k's number,
+// so that those 16 places share all banks evenly.
+template <uint32_t R, uint32_t THREADS>
+struct Side<true, R, THREADS> {
+    static constexpr uint32_t kAcross = R / 8, kLoads = R * 8 / THREADS, kDown = THREADS / kAcross;
+    static_assert(kAcross >= 16, "eight pairs of pieces at least");
+    uint32_t off[kLoads], lane;
+    __device__ static inline uint32_t turn(uint32_t k) { return (k & 3) | ((k >> 1) & 4); }
+    __device__ inline Side(uint32_t r0, uint64_t ld)
+    {
+        lane = threadIdx.x & 63;
+        const uint32_t k = threadIdx.x / kAcross;
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i)
+            off[i] = (k + i * kDown) * uint32_t(ld * 2) + (r0 + (threadIdx.x % kAcross ^ (2 * turn(k + i * kDown))) * 8) * 2;
+    }
+    __device__ inline void fetch(const uint16_t *p, uint32_t, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld, char *stage, uint32_t wave) const
+    {
+        // (a descriptor ends with a word: of an odd number of rows there is one more)
+        const __amdgpu_buffer_rsrc_t from = described(p + k0 * ld, (end - k0 - 1) * ld + ((rows + 1) & ~1u));
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) load_lds(from, off[i], stage + (i * THREADS + wave * 64) * 16);
+    }
+    template <int N>
+    __device__ inline void read(const char *stage, uint32_t tile, uint32_t step, bf16x8 (&to)[N]) const
+    {
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        const uint32_t at = step * 32 + 8 * (lane >> 4) + ((lane >> 2) & 3), s = turn(at);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const char *from = stage + at * (R * 2) + (((tile + i) ^ s) << 5) + ((lane & 3) << 3);
+            s4 half[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)  // (four k's further on the turn is the same)
+                half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(from + h * 4 * (R * 2)));
+            to[i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
 
 // A wave computes RM by RN tiles of 16 by 16, WM by WN waves a workgroup's tile.  Q's rows go in as the matrix
 // instruction's first operand, so that a lane ends up with neighbours of a row of C.
@@ -309,13 +394,13 @@ __device__ inline uint32_t term_q(uint32_t t) { return (0x010120u >> (4 * t)) & 
 // found 1113, woven with the reads 1196; 32 x 32 x 16 instructions, which move their sums twice as often, 1196, 16 x 16 x 32 1236;
 // four waves of 128 by 128 1163; eight waves in two groups that take turns at reading and multiplying 1041; slabs
 // of 32 in a ring of four stages, whose loads take half a cache line, 1172.
-template <typename T, int WM, int WN, int RM, int RN>
+template <typename T, int WM, int WN, int RM, int RN, bool PT, bool QT>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
 {
     constexpr uint32_t kThreads = WM * WN * 64, TM = WM * RM * 16, TN = WN * RN * 16;
     constexpr uint32_t terms = sizeof(T) == 2 ? 1 : 6;
     constexpr uint32_t kStage = (TM + TN) * kSlab * 2;
-    constexpr uint32_t kLoadsP = TM * 8 / kThreads, kLoadsQ = TN * 8 / kThreads;
+    constexpr int kLoads = int((TM + TN) * 8 / kThreads);
     constexpr uint32_t kRow = RN * 16 + 4;  // floats of a row of a wave's strip
     static_assert(WM * WN * 32 * kRow * 4 <= 2 * kStage, "the strips fit");
     __shared__ __attribute__((aligned(1024))) char stage0[kStage];
@@ -332,43 +417,21 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     const uint32_t group = b / (8 * a.tiles_n), left = min(a.tiles_m - group * 8, 8u), in = b - group * 8 * a.tiles_n;
     const uint32_t m0 = (group * 8 + in % left) * TM, n0 = in / left * TN;
 
-    // Where this lane's 16 bytes of each load come from.  A row's eight pieces lie in the stage in an order
-    // turned by the row's number, so that lanes that read the same piece of 16 rows meet no
-    // bank twice.
-    uint32_t off_p[kLoadsP], off_q[kLoadsQ];
-    const uint32_t sub = threadIdx.x >> 3, piece = (threadIdx.x & 7) ^ ((sub >> 1) & 7);
-#pragma unroll
-    for (uint32_t i = 0; i < kLoadsP; ++i)
-        off_p[i] = (min(m0 + sub + i * (kThreads / 8), a.m - 1) - m0) * uint32_t(a.ldp * 2) + piece * 16;
-#pragma unroll
-    for (uint32_t i = 0; i < kLoadsQ; ++i)
-        off_q[i] = (min(n0 + sub + i * (kThreads / 8), a.n - 1) - n0) * uint32_t(a.ldq * 2) + piece * 16;
-    const char *p0 = reinterpret_cast<const char *>(a.p + uint64_t(m0) * a.ldp), *q0 = reinterpret_cast<const char *>(a.q + uint64_t(n0) * a.ldq);
+    const Side<PT, TM, kThreads> side_p(m0, a.ldp);
+    const Side<QT, TN, kThreads> side_q(n0, a.ldq);
 
-    const uint32_t first = part * a.slabs, all = a.k / kSlab * terms;
+    const uint32_t first = part * a.slabs, all = (a.k + kSlab - 1) / kSlab * terms;
     const uint32_t count = min(a.slabs, all - first);
 
     auto fetch = [&](uint32_t s, char *stage) {
-        uint32_t ks = s, t = 0;
+        const uint32_t k0 = s / terms * kSlab;
+        const uint16_t *p = a.p, *q = a.q;
         if constexpr (terms > 1) {
-            ks = s / terms;
-            t = s % terms;
+            p += term_p(s % terms) * a.plane_p;
+            q += term_q(s % terms) * a.plane_q;
         }
-        const char *p = p0 + ks * (kSlab * 2), *q = q0 + ks * (kSlab * 2);
-        if constexpr (terms > 1) {
-            p += term_p(t) * a.plane_p * 2;
-            q += term_q(t) * a.plane_q * 2;
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < kLoadsP; ++i)
-            __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void *)(p + off_p[i]),
-                (__attribute__((address_space(3))) void *)(stage + (i * kThreads + wave * 64) * 16), 16, 0, 0);
-#pragma unroll
-        for (uint32_t i = 0; i < kLoadsQ; ++i)
-            __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void *)(q + off_q[i]),
-                (__attribute__((address_space(3))) void *)(stage + TM * 128 + (i * kThreads + wave * 64) * 16), 16, 0, 0);
+        side_p.fetch(p, m0, a.m, k0, a.k, a.ldp, stage, wave);
+        side_q.fetch(q, n0, a.n, k0, a.k, a.ldq, stage + TM * 128, wave);
     };
 
     f32x4 acc[RM][RN];
@@ -381,20 +444,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
 
     constexpr int H = RM / 2;
     bf16x8 fp[2][H], fq[2][RN];
-    const uint32_t row_p = wm * RM * 16 + (lane & 15), row_q = wn * RN * 16 + (lane & 15);
-    // (rows 16 further on are turned the same way)
-    auto read_q = [&](const char *stage, uint32_t step) {
-        const uint32_t c = step * 4 + (lane >> 4);
-#pragma unroll
-        for (int j = 0; j < RN; ++j)
-            fq[step][j] = *reinterpret_cast<const bf16x8 *>(stage + TM * 128 + (row_q + 16 * j) * 128 + ((c ^ ((row_q >> 1) & 7)) << 4));
-    };
-    auto read_p = [&](const char *stage, uint32_t step, int half) {
-        const uint32_t c = step * 4 + (lane >> 4);
-#pragma unroll
-        for (int i = 0; i < H; ++i)
-            fp[half][i] = *reinterpret_cast<const bf16x8 *>(stage + (row_p + 16 * (half * H + i)) * 128 + ((c ^ ((row_p >> 1) & 7)) << 4));
-    };
+    auto read_q = [&](const char *stage, uint32_t step) { side_q.template read<RN>(stage + TM * 128, wn * RN, step, fq[step]); };
+    auto read_p = [&](const char *stage, uint32_t step, int half) { side_p.template read<H>(stage, wm * RM + half * H, step, fp[half]); };
     auto multiply = [&](int step, int half) {
 #pragma unroll
         for (int i = 0; i < H; ++i)
@@ -402,12 +453,15 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
             for (int j = 0; j < RN; ++j)
                 acc[half * H + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fq[step][j], fp[half][i], acc[half * H + i][j], 0, 0, 0);
     };
+    // (a turned operand takes two reads of half the size)
+    constexpr int kEachP = PT ? 2 : 1, kEachQ = QT ? 2 : 1, kReads = H * kEachP + RN * kEachQ;
+    constexpr int kOnce = (kReads + H * RN - 1) / (H * RN), kBoth = (kReads + kOnce - 1) / kOnce;
     // The next pieces are read while the products of the last ones run, one read behind each of the first products.
     auto woven = [&](auto reads) {
 #pragma unroll
         for (int i = 0; i < H * RN; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (i < decltype(reads)::value) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (i < decltype(reads)::value) __builtin_amdgcn_sched_group_barrier(0x100, kOnce, 0);
         }
     };
     // What this wave has asked for has come, then what the others have.
@@ -417,30 +471,31 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     };
     // One slab: its first pieces are in registers, the next slab is on its way to `next`.  (Behind the last slab the
     // last one is fetched again, and never used: a branch here would cost the registers that the loop lacks.)
-    auto slab = [&](uint32_t s, char *now, char *next) {
+    auto slab = [&](uint32_t s, char *__restrict now, const char *__restrict next) {
         read_p(now, 0, 1);
         multiply(0, 0);
-        woven(std::integral_constant<int, H>());
+        woven(std::integral_constant<int, (H * kEachP + kOnce - 1) / kOnce>());
         read_q(now, 1);
         read_p(now, 1, 0);
         multiply(0, 1);
-        woven(std::integral_constant<int, H + RN>());
+        woven(std::integral_constant<int, kBoth>());
         read_p(now, 1, 1);
         multiply(1, 0);
-        woven(std::integral_constant<int, H>());
+        woven(std::integral_constant<int, (H * kEachP + kOnce - 1) / kOnce>());
         // (from here to the next meeting a wave goes before those that have not got here)
         __builtin_amdgcn_s_setprio(0);
         arrived();
         __builtin_amdgcn_s_setprio(1);
-        fetch(first + min(s + 2, count - 1), now);
         read_q(next, 0);
         read_p(next, 0, 0);
+        fetch(first + min(s + 2, count - 1), now);
         multiply(1, 1);
+        // (the reads first: the compiler would have a transposing read wait for the loads before it)
 #pragma unroll
         for (int i = 0; i < H * RN; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (i < H + RN) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            if (i % (H * RN / (kLoadsP + kLoadsQ)) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            if (i < (kReads + 1) / 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            else if (i < (kReads + 1) / 2 + kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
         }
     };
 
@@ -449,10 +504,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     arrived();
     read_q(stage0, 0);
     read_p(stage0, 0, 0);
-    for (uint32_t s = 0; s < count; s += 2) {
-        slab(s, stage0, stage1);
-        if (s + 1 < count) slab(s + 1, stage1, stage0);
-    }
+    // (what is said of the pointers lets a transposing read go before the loads into the other stage)
+    auto two_slabs = [&](uint32_t s, char *__restrict one, char *__restrict other) {
+        slab(s, one, other);
+        if (s + 1 < count) slab(s + 1, other, one);
+    };
+    for (uint32_t s = 0; s < count; s += 2) two_slabs(s, stage0, stage1);
     arrived();
 
     // Results go through the wave's own strip of local memory, 32 rows at a time, so that a row's neighbours
@@ -508,18 +565,20 @@ __global__ __launch_bounds__(256) void join_kernel(const float *partial, uint32_
     for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < uint64_t(rows) * across; i += uint64_t(gridDim.x) * 256) {
         const uint32_t m = uint32_t(i / across), n = uint32_t(i % across) * 8, have = min(8u, cols - n);
         float z[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (uint32_t s = 0; s < splits; ++s) {
-            const float *from = partial + (uint64_t(s) * rows + m) * cols + n;
+        const float *from = partial + uint64_t(m) * cols + n;
+        const uint64_t next = uint64_t(rows) * cols;
+#pragma unroll 4
+        for (uint32_t s = 0; s < splits; ++s, from += next) {
+            float t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             if (have == 8) {
-                float t[8];
                 load_n<float, 8>(from, t);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] += t[j];
             } else {
 #pragma unroll
                 for (uint32_t j = 0; j < 8; ++j)
-                    if (j < have) z[j] += from[j];
+                    if (j < have) t[j] = from[j];
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] += t[j];
         }
         finish<T>(r, m, n, have, z);
     }
@@ -528,46 +587,138 @@ __global__ __launch_bounds__(256) void join_kernel(const float *partial, uint32_
 // ------------------------------------------------------------------ few rows
 
 struct FewArgs {
-    const void *x, *w;
-    uint64_t ldx, ldw;
-    uint32_t in, out;
+    const void *x, *w;      // x: as it lies, or (float32, over 16 rows) taken apart by pack_kernel
+    uint64_t ldx, ldw, plane;
+    uint32_t rows, in, out;
     Result result;
 };
 
-// Up to kFewRows rows: the weights are read once, in the order they lie in, and are all there is to read.  A
-// wave takes a feature out at a time and its lanes the features in, sixteen bytes each.
-template <typename T, int ROWS>
-__global__ __launch_bounds__(256) void few_kernel(FewArgs a)
-{
-    constexpr uint32_t V = 16 / sizeof(T);
-    const uint32_t lane = lane_id(), n = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (n >= a.out) return;
-    const T *w = static_cast<const T *>(a.w) + n * a.ldw, *x = static_cast<const T *>(a.x);
-    float sum[ROWS] = {};
-    uint32_t k = lane * V;
-#pragma unroll 4
-    for (; k + V <= a.in; k += 64 * V) {
-        float wv[V];
-        load_n<T, V>(w + k, wv);
+// Sixteen k's of a row from `k` on as they lie in memory, zeros from `end` on.
+template <typename T>
+struct Piece {
+    T x[16];
+    __device__ inline void load(const T *row, uint32_t k, uint32_t end)
+    {
+        if (k + 16 <= end) {
+            typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            float xv[V];
-            load_n<T, V>(x + r * a.ldx + k, xv);
+            for (uint32_t i = 0; i < sizeof(T); ++i) {
+                const vec v = *reinterpret_cast<const vec *>(row + k + i * (16 / sizeof(T)));
 #pragma unroll
-            for (uint32_t j = 0; j < V; ++j) sum[r] += wv[j] * xv[j];
+                for (uint32_t j = 0; j < 16 / sizeof(T); ++j) x[i * (16 / sizeof(T)) + j] = v[j];
+            }
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) x[j] = k + j < end ? row[k + j] : T(0);
         }
     }
-    for (uint32_t j = 0; j < V; ++j)
-        if (k + j < a.in)
+    // the first or the second eight as the matrix instruction takes them
+    __device__ inline void half(int h, bf16x8 (&to)[sizeof(T) == 2 ? 1 : 3]) const
+    {
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) sum[r] += widen(w[k + j]) * widen(x[r * a.ldx + k + j]);
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (sizeof(T) == 2) {
+                to[0][e] = __builtin_bit_cast(__bf16, x[8 * h + e]);
+            } else {
+                uint16_t s[3];
+                split<T>(x[8 * h + e], s);
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        sum[r] = wave_sum(sum[r]);
-        if (lane == 0) {
-            float z[8] = {sum[r]};
-            finish<T>(a.result, r, n, 1, z);
+                for (int q = 0; q < 3; ++q) to[q][e] = __builtin_bit_cast(__bf16, s[q]);
+            }
         }
+    }
+};
+
+// Few rows: the weights are read once, straight into registers, in pieces of 64 k's of 16 features out; rows of x,
+// which all workgroups read, come from the caches.  kFewWaves waves share the k's of 16 features out and add up their
+// sums in local memory.  The matrix instruction's k's may be in any order that both operands share: a lane takes 16
+// neighbours, so that four lanes read a whole cache line.  float32 weights are taken apart in registers, and so is x
+// up to 16 rows; of more, MT times 16, it was taken apart before.
+//
+// Bound by the weights' bytes (one row of bfloat16 through 4096 by 11008, not in any cache: 18.9 us, 4.8 TB/s; 16 features
+// out to a workgroup, 32 take 27.7; four or sixteen waves 22.1, 20.5; eight pieces on their way instead of
+// four 20.8), from 16 rows on also by x, which is as many bytes to a workgroup then (26.8).
+constexpr int kFewWaves = 8;
+template <typename T, int MT>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void few_kernel(FewArgs a)
+{
+    constexpr bool apart = sizeof(T) == 4 && MT > 1;            // x comes taken apart
+    constexpr int planes = sizeof(T) == 2 ? 1 : 3, read = apart ? 3 : 1;
+    constexpr int D = sizeof(T) == 2 ? 4 : MT == 1 ? 2 : 1;     // pieces on their way
+    typedef typename std::conditional<apart, uint16_t, T>::type X;
+    __shared__ f32x4 sums[kFewWaves][MT][64];
+    const uint32_t lane = lane_id(), wave = threadIdx.x >> 6, at = lane & 15, k0 = (lane >> 4) * 16;
+    const uint32_t n0 = blockIdx.x * 16;
+    const T *w = static_cast<const T *>(a.w) + min(n0 + at, a.out - 1) * a.ldw;
+    const X *x[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) x[i] = static_cast<const X *>(a.x) + min(16 * i + at, a.rows - 1) * a.ldx;
+    f32x4 acc[MT] = {};
+    for (uint32_t k = wave * 64; k < a.in; k += kFewWaves * 64 * D) {
+        Piece<T> pw[D];
+        Piece<X> px[D][MT][read];
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const uint32_t from = k + d * kFewWaves * 64 + k0;
+            pw[d].load(w, from, a.in);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int q = 0; q < read; ++q) px[d][i][q].load(x[i] + q * a.plane, from, a.in);
+        }
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8 fw[planes];
+                pw[d].half(h, fw);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    bf16x8 fx[planes];
+                    if constexpr (apart) {
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) px[d][i][q].half(h, *reinterpret_cast<bf16x8(*)[1]>(&fx[q]));
+                    } else {
+                        px[d][i][0].half(h, fx);
+                    }
+                    if constexpr (planes == 1) {
+                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[0], fx[0], acc[i], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (uint32_t t = 0; t < 6; ++t)
+                            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[term_q(t)], fx[term_p(t)], acc[i], 0, 0, 0);
+                    }
+                }
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    // Eight neighbours of a row, features 8 h to 8 h + 7, are in two lanes' words.
+    for (uint32_t t = threadIdx.x; t < MT * 32; t += kFewWaves * 64) {
+        const uint32_t m = t / 2, h = t % 2, n = n0 + 8 * h;
+        if (m >= a.rows || n >= a.out) continue;
+        float z[8] = {};
+#pragma unroll
+        for (int s = 0; s < kFewWaves; ++s)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const f32x4 v = sums[s][m / 16][(2 * h + q) * 16 + m % 16];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[4 * q + e] += v[e];
+            }
+        finish<T>(a.result, m, n, min(8u, a.out - n), z);
+    }
+}
+
+template <typename T>
+void launch_few(const FewArgs &a, hipStream_t s)
+{
+    const uint32_t grid = (a.out + 15) / 16;
+    if (sizeof(T) == 2 || a.rows <= 16) few_kernel<T, 1><<<grid, kFewWaves * 64, 0, s>>>(a);
+    else if constexpr (sizeof(T) == 4) {
+        if (a.rows <= 32) few_kernel<T, 2><<<grid, kFewWaves * 64, 0, s>>>(a);
+        else few_kernel<T, 4><<<grid, kFewWaves * 64, 0, s>>>(a);
     }
 }
 
@@ -576,18 +727,20 @@ __global__ __launch_bounds__(256) void few_kernel(FewArgs a)
 // How a product is cut: the tile, and the parts of the sum that make up for few tiles.
 struct Shape {
     bool large;
+    uint32_t rows;  // of a tile of Shape::large == false
     uint32_t tiles_m, tiles_n, slabs, splits;
 };
 
-Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t terms)
+Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t terms, bool turned_p)
 {
-    Shape s;
+    Shape s{};
     const uint64_t cus = uint64_t(device_cu_count());
-    const uint64_t slabs = k / kSlab * terms;
-    if (!slabs) return Shape{};
+    const uint64_t slabs = up(k, kSlab) / kSlab * terms;
+    if (!slabs) return s;
     s.large = (m + 255) / 256 * ((n + 255) / 256) >= cus;
     const uint64_t t = s.large ? 256 : 128;
-    s.tiles_m = uint32_t((m + t - 1) / t);
+    s.rows = s.large ? 256 : turned_p || m > 64 ? 128 : m > 32 ? 64 : 32;
+    s.tiles_m = uint32_t((m + s.rows - 1) / s.rows);
     s.tiles_n = uint32_t((n + t - 1) / t);
     const uint64_t tiles = uint64_t(s.tiles_m) * s.tiles_n;
     // two of the smaller workgroups share a compute unit; a part has four slabs at least
@@ -621,30 +774,54 @@ struct Operand {
     uint64_t ld, plane;
 };
 
-// whether rows of k elements can be read as they lie
-bool as_it_lies(uint32_t dtype, const void *p, uint64_t ld, uint64_t k)
+// whether a matrix with `cols` elements to a row can be read as it lies: in words, and, where a row is k's, in pieces of 16 bytes
+// that do not straddle the last of them
+bool as_it_lies(uint32_t dtype, const void *p, uint64_t ld, uint64_t cols, bool turned)
 {
-    return dtype == TAGC_BF16 && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && ld < kMaxSide && k % kSlab == 0;
+    return dtype == TAGC_BF16 && (reinterpret_cast<uintptr_t>(p) & 3) == 0 && ld % 2 == 0 && ld < kMaxSide && cols % (turned ? 2 : 8) == 0;
 }
 
 uint32_t planes_of(uint32_t dtype) { return dtype == TAGC_F32 ? kPlanes : 1; }
 
-Operand room(Places &w, uint32_t dtype, uint64_t rows, uint64_t k)
+Operand room(Places &w, uint32_t dtype, uint64_t rows, uint64_t cols)
 {
-    const uint64_t ld = up(k, kSlab), plane = rows * ld;
+    const uint64_t ld = up(cols, 64), plane = rows * ld;
     return Operand{w.take<uint16_t>(plane * planes_of(dtype)), ld, plane};
+}
+
+PackArgs packed(const void *src, uint64_t ld, uint64_t rows, uint64_t cols, const Operand &to)
+{
+    PackArgs a{};
+    a.src = src;
+    a.ld = ld;
+    a.rows = uint32_t(rows);
+    a.cols = uint32_t(cols);
+    a.to = const_cast<uint16_t *>(to.p);
+    a.to_ld = to.ld;
+    a.to_plane = to.plane;
+    return a;
 }
 
 template <typename T>
 void launch_pack(const PackArgs &a, hipStream_t s)
 {
-    const uint64_t tiles = up(a.rows, kPackTile) / kPackTile * (up(a.cols, kPackTile) / kPackTile);
+    const uint64_t tiles = up(a.rows, kPackRows) / kPackRows * (up(a.cols, 64) / 64);
     if (!tiles) return;
     ProfileScope prof("linear_pack", s);
     pack_kernel<T><<<uint32_t(tiles), 256, 0, s>>>(a);
 }
 
+// a matrix as it lies, or laid out anew
 template <typename T>
+Operand operand(Places &w, uint32_t dtype, const void *src, uint64_t ld, uint64_t rows, uint64_t cols, bool turned, bool enqueue, hipStream_t s)
+{
+    if (as_it_lies(dtype, src, ld, cols, turned)) return Operand{static_cast<const uint16_t *>(src), ld, 0};
+    const Operand to = room(w, dtype, rows, cols);
+    if (enqueue) launch_pack<T>(packed(src, ld, rows, cols, to), s);
+    return to;
+}
+
+template <typename T, bool PT, bool QT>
 void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, uint64_t k, float *partial, const Result &r, hipStream_t s)
 {
     Product a;
@@ -656,8 +833,8 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     a.plane_q = q.plane;
     a.m = uint32_t(m);
     a.n = uint32_t(n);
-    a.k = uint32_t(up(k, kSlab));
-    const Shape f = shape_of(m, n, a.k, sizeof(T) == 4 ? 6 : 1);
+    a.k = uint32_t(k);
+    const Shape f = shape_of(m, n, k, sizeof(T) == 4 ? 6 : 1, PT);
     a.tiles_m = f.tiles_m;
     a.tiles_n = f.tiles_n;
     a.slabs = f.slabs;
@@ -667,8 +844,12 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     const uint32_t grid = f.tiles_m * f.tiles_n * f.splits;
     if (grid) {
         ProfileScope prof("linear_product", s);
-        if (f.large) product_kernel<T, 2, 4, 8, 4><<<grid, 512, 0, s>>>(a);
-        else product_kernel<T, 2, 2, 4, 4><<<grid, 256, 0, s>>>(a);
+        if (f.rows == 256) product_kernel<T, 2, 4, 8, 4, PT, QT><<<grid, 512, 0, s>>>(a);
+        else if (f.rows == 128) product_kernel<T, 2, 2, 4, 4, PT, QT><<<grid, 256, 0, s>>>(a);
+        else if constexpr (!PT) {
+            if (f.rows == 64) product_kernel<T, 1, 4, 4, 2, PT, QT><<<grid, 256, 0, s>>>(a);
+            else product_kernel<T, 1, 4, 2, 2, PT, QT><<<grid, 256, 0, s>>>(a);
+        }
     }
     if (f.splits != 1) {
         ProfileScope prof("linear_join", s);
@@ -678,9 +859,9 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
 }
 
 // elements of the partial sums of a product
-uint64_t partial_elems(uint64_t m, uint64_t n, uint64_t k, uint32_t dtype)
+uint64_t partial_elems(uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, bool turned_p)
 {
-    const Shape f = shape_of(m, n, up(k, kSlab), dtype == TAGC_F32 ? 6 : 1);
+    const Shape f = shape_of(m, n, k, dtype == TAGC_F32 ? 6 : 1, turned_p);
     return f.splits > 1 ? f.splits * m * n : 0;
 }
 
@@ -706,45 +887,25 @@ int forward(const tagc_linear *l, Places &w, bool enqueue, hipStream_t s)
     Result r{l->bias, l->residual, l->y, l->pre, l->ldr, l->ldy, l->ldp, l->activation, 0};
     const uint64_t M = l->rows, K = l->in, N = l->out;
     if (!M || !N) return TAGC_OK;
-    if (M <= kFewRows) {
-        if (!enqueue) return TAGC_OK;
-        const FewArgs a{l->x, l->w, l->ldx, l->ldw, uint32_t(K), uint32_t(N), r};
-        const uint32_t grid = uint32_t((N + 3) / 4);
-        ProfileScope prof("linear_few", s);
-        switch (M) {
-            case 1: few_kernel<T, 1><<<grid, 256, 0, s>>>(a); break;
-            case 2: few_kernel<T, 2><<<grid, 256, 0, s>>>(a); break;
-            case 3: few_kernel<T, 3><<<grid, 256, 0, s>>>(a); break;
-            default: few_kernel<T, 4><<<grid, 256, 0, s>>>(a); break;
+    if (M <= kFewRows[l->dtype]) {
+        FewArgs a{l->x, l->w, l->ldx, l->ldw, 0, uint32_t(M), uint32_t(K), uint32_t(N), r};
+        if (sizeof(T) == 4 && M > 16) {
+            const Operand x = room(w, l->dtype, M, K);
+            if (enqueue) launch_pack<T>(packed(l->x, l->ldx, M, K, x), s);
+            a.x = x.p;
+            a.ldx = x.ld;
+            a.plane = x.plane;
         }
+        if (!enqueue) return TAGC_OK;
+        ProfileScope prof("linear_few", s);
+        launch_few<T>(a, s);
         return hip_ok(hipGetLastError());
     }
-    Operand p{static_cast<const uint16_t *>(l->x), l->ldx, 0}, q{static_cast<const uint16_t *>(l->w), l->ldw, 0};
-    PackArgs a{};
-    a.rows = uint32_t(M);
-    a.cols = uint32_t(K);
-    if (!as_it_lies(l->dtype, l->x, l->ldx, K)) {
-        p = room(w, l->dtype, M, K);
-        a.src = l->x;
-        a.ld = l->ldx;
-        a.straight = const_cast<uint16_t *>(p.p);
-        a.straight_ld = p.ld;
-        a.straight_plane = p.plane;
-        if (enqueue) launch_pack<T>(a, s);
-    }
-    if (!as_it_lies(l->dtype, l->w, l->ldw, K)) {
-        q = room(w, l->dtype, N, K);
-        a.src = l->w;
-        a.ld = l->ldw;
-        a.rows = uint32_t(N);
-        a.straight = const_cast<uint16_t *>(q.p);
-        a.straight_ld = q.ld;
-        a.straight_plane = q.plane;
-        if (enqueue) launch_pack<T>(a, s);
-    }
-    float *partial = w.take<float>(partial_elems(M, N, K, l->dtype));
+    const Operand p = operand<T>(w, l->dtype, l->x, l->ldx, M, K, false, enqueue, s);
+    const Operand q = operand<T>(w, l->dtype, l->w, l->ldw, N, K, false, enqueue, s);
+    float *partial = w.take<float>(partial_elems(M, N, K, l->dtype, false));
     if (!enqueue) return TAGC_OK;
-    launch_product<T>(p, q, M, N, K, partial, r, s);
+    launch_product<T, false, false>(p, q, M, N, K, partial, r, s);
     return hip_ok(hipGetLastError());
 }
 
@@ -752,32 +913,19 @@ template <typename T>
 int backward(const tagc_linear_grad *l, Places &w, bool enqueue, hipStream_t s)
 {
     const uint64_t M = l->rows, K = l->in, N = l->out;
-    // dz as it is needed: by rows for dx, turned for dw
-    Operand dz{static_cast<const uint16_t *>(l->dy), l->lddy, 0}, dzt{};
-    PackArgs a{};
-    a.src = l->dy;
-    a.ld = l->lddy;
+    const bool dx = l->dx && M && K, dw = l->dw && N && K, db = l->db && N;
+    Operand dz{static_cast<const uint16_t *>(l->dy), l->lddy, 0};
+    PackArgs a = packed(l->dy, l->lddy, M, N, Operand{});
+    if ((dx || dw) && (l->pre || !as_it_lies(l->dtype, l->dy, l->lddy, N, !dx))) {
+        dz = room(w, l->dtype, M, N);
+        a = packed(l->dy, l->lddy, M, N, dz);
+    }
     a.pre = l->pre;
     a.ldp = l->ldp;
     a.act = l->activation;
-    a.rows = uint32_t(M);
-    a.cols = uint32_t(N);
-    const bool dx = l->dx && M && K, dw = l->dw && N && K, db = l->db && N;
-    if (dx && (l->pre || !as_it_lies(l->dtype, l->dy, l->lddy, N))) {
-        dz = room(w, l->dtype, M, N);
-        a.straight = const_cast<uint16_t *>(dz.p);
-        a.straight_ld = dz.ld;
-        a.straight_plane = dz.plane;
-    }
-    if (dw) {
-        dzt = room(w, l->dtype, N, M);
-        a.turned = const_cast<uint16_t *>(dzt.p);
-        a.turned_ld = dzt.ld;
-        a.turned_plane = dzt.plane;
-    }
-    const uint32_t tiles = uint32_t(up(M, kPackTile) / kPackTile);
+    const uint32_t tiles = uint32_t(up(M, kPackRows) / kPackRows);
     if (db) a.sums = w.take<float>(uint64_t(tiles) * N);
-    if (enqueue && (a.straight || a.turned || db)) launch_pack<T>(a, s);
+    if (enqueue && (a.to || db)) launch_pack<T>(a, s);
     if (enqueue && db) {
         ProfileScope prof("linear_bias", s);
         bias_kernel<T><<<uint32_t((N + 255) / 256), 256, 0, s>>>(a.sums, tiles, uint32_t(N), static_cast<T *>(l->db), l->accumulate);
@@ -785,40 +933,18 @@ int backward(const tagc_linear_grad *l, Places &w, bool enqueue, hipStream_t s)
     const uint64_t mark = w.at;
     uint64_t most = mark;
     if (dx) {
-        const Operand wt = room(w, l->dtype, K, N);
-        float *partial = w.take<float>(partial_elems(M, K, N, l->dtype));
-        if (enqueue) {
-            PackArgs b{};
-            b.src = l->w;
-            b.ld = l->ldw;
-            b.rows = uint32_t(N);
-            b.cols = uint32_t(K);
-            b.turned = const_cast<uint16_t *>(wt.p);
-            b.turned_ld = wt.ld;
-            b.turned_plane = wt.plane;
-            launch_pack<T>(b, s);
-            const Result r{nullptr, nullptr, l->dx, nullptr, 0, l->lddx, 0, TAGC_ACT_NONE, 0};
-            launch_product<T>(dz, wt, M, K, N, partial, r, s);
-        }
+        const Operand q = operand<T>(w, l->dtype, l->w, l->ldw, N, K, true, enqueue, s);
+        float *partial = w.take<float>(partial_elems(M, K, N, l->dtype, false));
+        const Result r{nullptr, nullptr, l->dx, nullptr, 0, l->lddx, 0, TAGC_ACT_NONE, 0};
+        if (enqueue) launch_product<T, false, true>(dz, q, M, K, N, partial, r, s);
         most = w.at;
     }
     if (dw) {
         w.at = mark;  // what dx needed is done with
-        const Operand xt = room(w, l->dtype, K, M);
-        float *partial = w.take<float>(partial_elems(N, K, M, l->dtype));
-        if (enqueue) {
-            PackArgs b{};
-            b.src = l->x;
-            b.ld = l->ldx;
-            b.rows = uint32_t(M);
-            b.cols = uint32_t(K);
-            b.turned = const_cast<uint16_t *>(xt.p);
-            b.turned_ld = xt.ld;
-            b.turned_plane = xt.plane;
-            launch_pack<T>(b, s);
-            const Result r{nullptr, nullptr, l->dw, nullptr, 0, l->lddw, 0, TAGC_ACT_NONE, l->accumulate};
-            launch_product<T>(dzt, xt, N, K, M, partial, r, s);
-        }
+        const Operand q = operand<T>(w, l->dtype, l->x, l->ldx, M, K, true, enqueue, s);
+        float *partial = w.take<float>(partial_elems(N, K, M, l->dtype, true));
+        const Result r{nullptr, nullptr, l->dw, nullptr, 0, l->lddw, 0, TAGC_ACT_NONE, l->accumulate};
+        if (enqueue) launch_product<T, true, true>(dz, q, N, K, M, partial, r, s);
         if (w.at > most) most = w.at;
     }
     w.at = most;

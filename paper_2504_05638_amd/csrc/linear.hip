@@ -320,10 +320,13 @@ struct Side<false, R, THREADS> {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i) off[i] = (sub + i * (THREADS / 8)) * uint32_t(ld * 2) + piece * 16;
     }
-    __device__ inline void fetch(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld, char *stage, uint32_t wave) const
+    // the operand from row r0 and k0 on (of a row whose k's are no multiple of eight there are zeros up to one)
+    __device__ static inline __amdgpu_buffer_rsrc_t aim(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
     {
-        // (of a row whose k's are no multiple of eight there are zeros up to one)
-        const __amdgpu_buffer_rsrc_t from = described(p + r0 * ld + k0, (rows - r0 - 1) * ld + ((end + 7) & ~7u) - k0);
+        return described(p + r0 * ld + k0, (rows - r0 - 1) * ld + ((end + 7) & ~7u) - k0);
+    }
+    __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, uint32_t k0, uint32_t end, char *stage, uint32_t wave) const
+    {
         const bool there = k0 + k < end;  // (the next row lies behind the last k)
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i) load_lds(from, there ? off[i] : kNowhere, stage + (i * THREADS + wave * 64) * 16);
@@ -356,10 +359,13 @@ struct Side<true, R, THREADS> {
         for (uint32_t i = 0; i < kLoads; ++i)
             off[i] = (k + i * kDown) * uint32_t(ld * 2) + (r0 + (threadIdx.x % kAcross ^ (2 * turn(k + i * kDown))) * 8) * 2;
     }
-    __device__ inline void fetch(const uint16_t *p, uint32_t, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld, char *stage, uint32_t wave) const
+    // the operand from k0 on (a descriptor ends with a word: of an odd number of rows there is one more)
+    __device__ static inline __amdgpu_buffer_rsrc_t aim(const uint16_t *p, uint32_t, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
     {
-        // (a descriptor ends with a word: of an odd number of rows there is one more)
-        const __amdgpu_buffer_rsrc_t from = described(p + k0 * ld, (end - k0 - 1) * ld + ((rows + 1) & ~1u));
+        return described(p + k0 * ld, (end - k0 - 1) * ld + ((rows + 1) & ~1u));
+    }
+    __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, uint32_t, uint32_t, char *stage, uint32_t wave) const
+    {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i) load_lds(from, off[i], stage + (i * THREADS + wave * 64) * 16);
     }
@@ -423,15 +429,22 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     const uint32_t first = part * a.slabs, all = (a.k + kSlab - 1) / kSlab * terms;
     const uint32_t count = min(a.slabs, all - first);
 
-    auto fetch = [&](uint32_t s, char *stage) {
+    struct Aim {
+        __amdgpu_buffer_rsrc_t p, q;
+        uint32_t k0;
+    };
+    auto aim = [&](uint32_t s) {
         const uint32_t k0 = s / terms * kSlab;
         const uint16_t *p = a.p, *q = a.q;
         if constexpr (terms > 1) {
             p += term_p(s % terms) * a.plane_p;
             q += term_q(s % terms) * a.plane_q;
         }
-        side_p.fetch(p, m0, a.m, k0, a.k, a.ldp, stage, wave);
-        side_q.fetch(q, n0, a.n, k0, a.k, a.ldq, stage + TM * 128, wave);
+        return Aim{side_p.aim(p, m0, a.m, k0, a.k, a.ldp), side_q.aim(q, n0, a.n, k0, a.k, a.ldq), k0};
+    };
+    auto fetch = [&](const Aim &at, char *stage) {
+        side_p.fetch(at.p, at.k0, a.k, stage, wave);
+        side_q.fetch(at.q, at.k0, a.k, stage + TM * 128, wave);
     };
 
     f32x4 acc[RM][RN];
@@ -471,7 +484,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     };
     // One slab: its first pieces are in registers, the next slab is on its way to `next`.  (Behind the last slab the
     // last one is fetched again, and never used: a branch here would cost the registers that the loop lacks.)
-    auto slab = [&](uint32_t s, char *__restrict now, const char *__restrict next) {
+    auto slab = [&](uint32_t s, char *now, const char *next) {
         read_p(now, 0, 1);
         multiply(0, 0);
         woven(std::integral_constant<int, (H * kEachP + kOnce - 1) / kOnce>());
@@ -479,6 +492,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
         read_p(now, 1, 0);
         multiply(0, 1);
         woven(std::integral_constant<int, kBoth>());
+        const Aim at = aim(first + min(s + 2, count - 1));
         read_p(now, 1, 1);
         multiply(1, 0);
         woven(std::integral_constant<int, (H * kEachP + kOnce - 1) / kOnce>());
@@ -488,28 +502,38 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
         __builtin_amdgcn_s_setprio(1);
         read_q(next, 0);
         read_p(next, 0, 0);
-        fetch(first + min(s + 2, count - 1), now);
+        fetch(at, now);
         multiply(1, 1);
-        // (the reads first: the compiler would have a transposing read wait for the loads before it)
+        // (A transposing read behind a load would wait for it: there the reads go first.)
 #pragma unroll
         for (int i = 0; i < H * RN; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (i < (kReads + 1) / 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            else if (i < (kReads + 1) / 2 + kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            if constexpr (PT || QT || H * RN < kLoads) {
+                if (i < (kReads + 1) / 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                else if (i < (kReads + 1) / 2 + kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            } else {
+                if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (i % (H * RN / kLoads) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
         }
     };
 
-    fetch(first, stage0);
-    fetch(first + min(1u, count - 1), stage1);
+    fetch(aim(first), stage0);
+    fetch(aim(first + min(1u, count - 1)), stage1);
     arrived();
     read_q(stage0, 0);
     read_p(stage0, 0, 0);
-    // (what is said of the pointers lets a transposing read go before the loads into the other stage)
-    auto two_slabs = [&](uint32_t s, char *__restrict one, char *__restrict other) {
-        slab(s, one, other);
-        if (s + 1 < count) slab(s + 1, other, one);
-    };
-    for (uint32_t s = 0; s < count; s += 2) two_slabs(s, stage0, stage1);
+    // (said of the pointers, this keeps the compiler from having a transposing read wait for loads into the other stage; plain reads
+    // it knows better without)
+    auto slab_apart = [&](uint32_t s, char *__restrict now, const char *__restrict next) { slab(s, now, next); };
+    for (uint32_t s = 0; s < count; s += 2) {
+        if constexpr (PT || QT) slab_apart(s, stage0, stage1);
+        else slab(s, stage0, stage1);
+        if (s + 1 < count) {
+            if constexpr (PT || QT) slab_apart(s + 1, stage1, stage0);
+            else slab(s + 1, stage1, stage0);
+        }
+    }
     arrived();
 
     // Results go through the wave's own strip of local memory, 32 rows at a time, so that a row's neighbours

@@ -748,31 +748,52 @@ void launch_few(const FewArgs &a, hipStream_t s)
 
 // ------------------------------------------------------------------ host
 
-// How a product is cut: the tile, and the parts of the sum that make up for few tiles.
+// How a product is cut: tiles of `rows` by 256 (256 rows) or 128, and the parts of the sum that make up for few tiles.
 struct Shape {
-    bool large;
-    uint32_t rows;  // of a tile of Shape::large == false
-    uint32_t tiles_m, tiles_n, slabs, splits;
+    uint32_t rows, tiles_m, tiles_n, slabs, splits;
 };
 
+// By what the candidates would take, in us, from measurements at sizes from 333 by 1001 by 832 to 8192 by 8192 by 8192 (within 15 %
+// of them): a slab of 256 by 256 takes a compute unit to itself for 1.68; two of 128 by 128 share one for 1.01, one
+// alone takes 0.70; parts of a sum cost a launch, and their bytes written and read.  (us, 256 by 256 / 128 by 128
+// in one, two, four parts: 4096 cubed 107 / 124; 8192 by 2560 by 1024 64 / 53; 2048 by 2048 by 4096 81 / 45, 49; 1024 by 4096 by
+// 1024 31 / 16, 27; 1024 by 1024 by 4096 - / 47, 32, 25; 333 by 1001 by 832 - / 11, 14, 15.)
 Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t terms, bool turned_p)
 {
     Shape s{};
-    const uint64_t cus = uint64_t(device_cu_count());
-    const uint64_t slabs = up(k, kSlab) / kSlab * terms;
+    const uint64_t cus = uint64_t(device_cu_count()), slabs = up(k, kSlab) / kSlab * terms;
     if (!slabs) return s;
-    s.large = (m + 255) / 256 * ((n + 255) / 256) >= cus;
-    const uint64_t t = s.large ? 256 : 128;
-    s.rows = s.large ? 256 : turned_p || m > 64 ? 128 : m > 32 ? 64 : 32;
-    s.tiles_m = uint32_t((m + s.rows - 1) / s.rows);
-    s.tiles_n = uint32_t((n + t - 1) / t);
-    const uint64_t tiles = uint64_t(s.tiles_m) * s.tiles_n;
-    // two of the smaller workgroups share a compute unit; a part has four slabs at least
     uint64_t splits = 1;
-    if (!s.large && tiles < 2 * cus) {
-        splits = 2 * cus / tiles;
+    if (!turned_p && m <= 64) {
+        // thin tiles: the weights' bytes count, and many workgroups to ask for them
+        s.rows = m <= 32 ? 32 : 64;
+        s.tiles_m = 1;
+        s.tiles_n = uint32_t((n + 127) / 128);
+        splits = 2 * cus / s.tiles_n;
         if (splits > slabs / 4) splits = slabs / 4;
         if (splits < 1) splits = 1;
+    } else {
+        double best = 0;
+        for (const uint32_t t : {256u, 128u}) {
+            const uint64_t tm = (m + t - 1) / t, tn = (n + t - 1) / t, tiles = tm * tn;
+            for (uint64_t parts = 1; parts <= 16 && parts <= slabs; ++parts) {
+                const uint64_t each = (slabs + parts - 1) / parts, groups = tiles * parts;
+                double rounds;
+                if (t == 256) {
+                    rounds = 1.68 * double((groups + cus - 1) / cus);
+                } else {
+                    const uint64_t rest = groups % (2 * cus);
+                    rounds = 1.01 * double(groups / (2 * cus)) + (!rest ? 0.0 : rest <= cus ? 0.70 : 1.01);
+                }
+                const double us = rounds * double(each) + (parts > 1 ? 4.5 + double(parts * m * n * 8) / 4e6 : 0.0);
+                if (s.rows && us >= best) continue;
+                best = us;
+                s.rows = t;
+                s.tiles_m = uint32_t(tm);
+                s.tiles_n = uint32_t(tn);
+                splits = parts;
+            }
+        }
     }
     s.slabs = uint32_t((slabs + splits - 1) / splits);
     s.splits = uint32_t((slabs + s.slabs - 1) / s.slabs);
@@ -869,7 +890,7 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     if (grid) {
         ProfileScope prof("linear_product", s);
         if (f.rows == 256) product_kernel<T, 2, 4, 8, 4, PT, QT><<<grid, 512, 0, s>>>(a);
-        else if (f.rows == 128) product_kernel<T, 2, 2, 4, 4, PT, QT><<<grid, 256, 0, s>>>(a);
+        else if (f.rows == 128) product_kernel<T, 2, 4, 4, 2, PT, QT><<<grid, 512, 0, s>>>(a);
         else if constexpr (!PT) {
             if (f.rows == 64) product_kernel<T, 1, 4, 4, 2, PT, QT><<<grid, 256, 0, s>>>(a);
             else product_kernel<T, 1, 4, 2, 2, PT, QT><<<grid, 256, 0, s>>>(a);

@@ -121,6 +121,12 @@ struct PackArgs {
     float *sums;          // [tiles of rows, cols] or NULL: sums over a tile's rows
 };
 
+// What a call lays out, in one launch.
+struct PackJobs {
+    PackArgs job[3];
+    uint32_t first[3];    // workgroup of each (one that there is not begins behind the last)
+};
+
 // The bfloat16 numbers that a packed value goes to: itself rounded, or three that add up to it: cut off behind 8 bits (what is
 // finite stays finite), the rest rounded to 8 bits, and what is then left, which has no more than 8.
 // (Of an infinity the second is NaN.)
@@ -142,13 +148,16 @@ __device__ inline void split(float x, uint16_t (&out)[sizeof(T) == 2 ? 1 : 3])
 
 // A workgroup takes a tile of kPackRows by 64, a thread four neighbours of each sixteenth row.
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(PackArgs a)
+__global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
 {
+    const uint32_t which = blockIdx.x >= jobs.first[2] ? 2 : blockIdx.x >= jobs.first[1] ? 1 : 0;
+    const PackArgs a = which == 0 ? jobs.job[0] : which == 1 ? jobs.job[1] : jobs.job[2];
+    const uint32_t block = blockIdx.x - jobs.first[which];
     constexpr int planes = sizeof(T) == 2 ? 1 : 3;
     typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
     __shared__ float sums[16][64];
     const uint32_t tiles_c = (a.cols + 63) / 64;
-    const uint32_t tile = blockIdx.x / tiles_c, r0 = tile * kPackRows, c = blockIdx.x % tiles_c * 64 + threadIdx.x % 16 * 4;
+    const uint32_t tile = block / tiles_c, r0 = tile * kPackRows, c = block % tiles_c * 64 + threadIdx.x % 16 * 4;
     const T *src = static_cast<const T *>(a.src), *pre = static_cast<const T *>(a.pre);
     float x[kPackRows / 16][4] = {}, sum[4] = {};
 #pragma unroll
@@ -195,7 +204,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a)
 #pragma unroll
     for (int j = 0; j < 4; ++j) sums[threadIdx.x / 16][threadIdx.x % 16 * 4 + j] = sum[j];
     __syncthreads();
-    const uint32_t at = blockIdx.x % tiles_c * 64 + threadIdx.x;
+    const uint32_t at = block % tiles_c * 64 + threadIdx.x;
     if (threadIdx.x < 64 && at < a.cols) {
         float all = 0;
 #pragma unroll
@@ -211,6 +220,7 @@ __global__ __launch_bounds__(256) void bias_kernel(const float *sums, uint32_t t
     const uint32_t c = blockIdx.x * 256 + threadIdx.x;
     if (c >= cols) return;
     float s = 0;
+#pragma unroll 8
     for (uint32_t t = 0; t < tiles; ++t) s += sums[uint64_t(t) * cols + c];
     db[c] = narrow<T>(accumulate ? s + widen(db[c]) : s);
 }
@@ -847,24 +857,34 @@ PackArgs packed(const void *src, uint64_t ld, uint64_t rows, uint64_t cols, cons
     return a;
 }
 
-template <typename T>
-void launch_pack(const PackArgs &a, hipStream_t s)
-{
-    const uint64_t tiles = up(a.rows, kPackRows) / kPackRows * (up(a.cols, 64) / 64);
-    if (!tiles) return;
-    ProfileScope prof("linear_pack", s);
-    pack_kernel<T><<<uint32_t(tiles), 256, 0, s>>>(a);
-}
-
-// a matrix as it lies, or laid out anew
-template <typename T>
-Operand operand(Places &w, uint32_t dtype, const void *src, uint64_t ld, uint64_t rows, uint64_t cols, bool turned, bool enqueue, hipStream_t s)
-{
-    if (as_it_lies(dtype, src, ld, cols, turned)) return Operand{static_cast<const uint16_t *>(src), ld, 0};
-    const Operand to = room(w, dtype, rows, cols);
-    if (enqueue) launch_pack<T>(packed(src, ld, rows, cols, to), s);
-    return to;
-}
+// What a call has to lay out, gathered while its workspace is handed out.
+struct Packs {
+    PackJobs jobs{};
+    uint64_t groups = 0;
+    int n = 0;
+    void add(const PackArgs &a)
+    {
+        jobs.job[n] = a;
+        jobs.first[n++] = uint32_t(groups);
+        groups += up(a.rows, kPackRows) / kPackRows * (up(a.cols, 64) / 64);
+    }
+    // a matrix as it lies, or laid out anew
+    Operand operand(Places &w, uint32_t dtype, const void *src, uint64_t ld, uint64_t rows, uint64_t cols, bool turned)
+    {
+        if (as_it_lies(dtype, src, ld, cols, turned)) return Operand{static_cast<const uint16_t *>(src), ld, 0};
+        const Operand to = room(w, dtype, rows, cols);
+        add(packed(src, ld, rows, cols, to));
+        return to;
+    }
+    template <typename T>
+    void launch(hipStream_t s)
+    {
+        if (!groups) return;
+        for (int i = n; i < 3; ++i) jobs.first[i] = uint32_t(groups);
+        ProfileScope prof("linear_pack", s);
+        pack_kernel<T><<<uint32_t(groups), 256, 0, s>>>(jobs);
+    }
+};
 
 template <typename T, bool PT, bool QT>
 void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, uint64_t k, float *partial, const Result &r, hipStream_t s)
@@ -920,9 +940,9 @@ int check_sizes(uint64_t rows, uint64_t in, uint64_t out, uint32_t dtype, uint32
     if (dtype > TAGC_BF16 || act > TAGC_ACT_SILU) return TAGC_EINVAL;
     // a tile's 256 rows span fewer than 2^32 bytes
     if (rows >= kMaxSide || in >= kMaxSide || out >= kMaxSide) return TAGC_ESIZE;
-    // a launch has fewer than 2^32 threads: at most a workgroup of 256 for a tile of 64 by 64
+    // a launch has fewer than 2^32 threads: at most a workgroup of 256 for each tile of 64 by 64 of all three matrices
     const uint64_t r = up(rows, 64) / 64, i = up(in, 64) / 64, o = up(out, 64) / 64;
-    if (r * i >= (1ull << 24) || r * o >= (1ull << 24) || i * o >= (1ull << 24)) return TAGC_ESIZE;
+    if (r * i + r * o + i * o >= (1ull << 24)) return TAGC_ESIZE;
     return TAGC_OK;
 }
 
@@ -935,8 +955,9 @@ int forward(const tagc_linear *l, Places &w, bool enqueue, hipStream_t s)
     if (M <= kFewRows[l->dtype]) {
         FewArgs a{l->x, l->w, l->ldx, l->ldw, 0, uint32_t(M), uint32_t(K), uint32_t(N), r};
         if (sizeof(T) == 4 && M > 16) {
-            const Operand x = room(w, l->dtype, M, K);
-            if (enqueue) launch_pack<T>(packed(l->x, l->ldx, M, K, x), s);
+            Packs packs;
+            const Operand x = packs.operand(w, l->dtype, l->x, l->ldx, M, K, false);
+            if (enqueue) packs.launch<T>(s);
             a.x = x.p;
             a.ldx = x.ld;
             a.plane = x.plane;
@@ -946,10 +967,12 @@ int forward(const tagc_linear *l, Places &w, bool enqueue, hipStream_t s)
         launch_few<T>(a, s);
         return hip_ok(hipGetLastError());
     }
-    const Operand p = operand<T>(w, l->dtype, l->x, l->ldx, M, K, false, enqueue, s);
-    const Operand q = operand<T>(w, l->dtype, l->w, l->ldw, N, K, false, enqueue, s);
+    Packs packs;
+    const Operand p = packs.operand(w, l->dtype, l->x, l->ldx, M, K, false);
+    const Operand q = packs.operand(w, l->dtype, l->w, l->ldw, N, K, false);
     float *partial = w.take<float>(partial_elems(M, N, K, l->dtype, false));
     if (!enqueue) return TAGC_OK;
+    packs.launch<T>(s);
     launch_product<T, false, false>(p, q, M, N, K, partial, r, s);
     return hip_ok(hipGetLastError());
 }
@@ -970,30 +993,25 @@ int backward(const tagc_linear_grad *l, Places &w, bool enqueue, hipStream_t s)
     a.act = l->activation;
     const uint32_t tiles = uint32_t(up(M, kPackRows) / kPackRows);
     if (db) a.sums = w.take<float>(uint64_t(tiles) * N);
-    if (enqueue && (a.to || db)) launch_pack<T>(a, s);
-    if (enqueue && db) {
+    Packs packs;
+    if (a.to || db) packs.add(a);
+    Operand wq{}, xq{};
+    if (dx) wq = packs.operand(w, l->dtype, l->w, l->ldw, N, K, true);
+    if (dw) xq = packs.operand(w, l->dtype, l->x, l->ldx, M, K, true);
+    // (dx is done with its partial sums when dw begins)
+    const uint64_t for_dx = dx ? partial_elems(M, K, N, l->dtype, false) : 0, for_dw = dw ? partial_elems(N, K, M, l->dtype, true) : 0;
+    float *partial = w.take<float>(for_dx > for_dw ? for_dx : for_dw);
+    if (!enqueue) return TAGC_OK;
+    packs.launch<T>(s);
+    if (db) {
         ProfileScope prof("linear_bias", s);
         bias_kernel<T><<<uint32_t((N + 255) / 256), 256, 0, s>>>(a.sums, tiles, uint32_t(N), static_cast<T *>(l->db), l->accumulate);
     }
-    const uint64_t mark = w.at;
-    uint64_t most = mark;
-    if (dx) {
-        const Operand q = operand<T>(w, l->dtype, l->w, l->ldw, N, K, true, enqueue, s);
-        float *partial = w.take<float>(partial_elems(M, K, N, l->dtype, false));
-        const Result r{nullptr, nullptr, l->dx, nullptr, 0, l->lddx, 0, TAGC_ACT_NONE, 0};
-        if (enqueue) launch_product<T, false, true>(dz, q, M, K, N, partial, r, s);
-        most = w.at;
-    }
-    if (dw) {
-        w.at = mark;  // what dx needed is done with
-        const Operand q = operand<T>(w, l->dtype, l->x, l->ldx, M, K, true, enqueue, s);
-        float *partial = w.take<float>(partial_elems(N, K, M, l->dtype, true));
-        const Result r{nullptr, nullptr, l->dw, nullptr, 0, l->lddw, 0, TAGC_ACT_NONE, l->accumulate};
-        if (enqueue) launch_product<T, true, true>(dz, q, N, K, M, partial, r, s);
-        if (w.at > most) most = w.at;
-    }
-    w.at = most;
-    return enqueue ? hip_ok(hipGetLastError()) : TAGC_OK;
+    if (dx) launch_product<T, false, true>(dz, wq, M, K, N, partial, Result{nullptr, nullptr, l->dx, nullptr, 0, l->lddx, 0, TAGC_ACT_NONE, 0}, s);
+    if (dw)
+        launch_product<T, true, true>(dz, xq, N, K, M, partial,
+                                      Result{nullptr, nullptr, l->dw, nullptr, 0, l->lddw, 0, TAGC_ACT_NONE, l->accumulate}, s);
+    return hip_ok(hipGetLastError());
 }
 
 int check_forward(const tagc_linear *l, bool pointers)

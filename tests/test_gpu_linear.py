@@ -128,6 +128,27 @@ def test_backward(shape, dtype):
         assert torch.equal(bucket[:7], was[:7]) and torch.equal(bucket[-5:], was[-5:])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(4001, 4006, 4003), (3904, 4096, 4160)], ids=str)
+def test_large_tiles(shape, dtype):
+    """Sizes at which every product, forward and backward, takes the large tiles, with and without laying operands out."""
+    from paper_2504_05638_amd.train import linear, linear_backward
+    M, K, N = shape
+    t = T[dtype]
+    x, w, b, dy = _randn((M, K), 1, t), _randn((N, K), 2, t, K ** -0.5), _randn((1, N), 3, t)[0], _randn((M, N), 4, t)
+    y, pre = linear(x, w, b, activation="silu", save=True)
+    z, z_err, ref, err = _forward_ref(x, w, b, None, "silu")
+    _near(y, ref, err, t, "y")
+    _near(pre, z, z_err, t, "pre")
+    del y, z, z_err, ref, err
+    dw, db = torch.empty_like(w), torch.empty_like(b)
+    dx = linear_backward(dy, x, w, dw=dw, db=db)
+    dz, xd, wd = dy.double(), x.double(), w.double()
+    _near(dx, dz @ wd, (N + 8) * 2 * E * (dz.abs() @ wd.abs()), t, "dx")
+    _near(dw, dz.t() @ xd, (M + 8) * 2 * E * (dz.abs().t() @ xd.abs()), t, "dw")
+    _near(db, dz.sum(0), (M + 8) * 2 * E * dz.abs().sum(0), t, "db")
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_gradient_against_differences(act):
     """d(sum(c * y)) / dw, dx, db by central differences of the library's own forward in float32."""

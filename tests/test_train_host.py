@@ -129,9 +129,12 @@ def test_workspaces():
     # rows off a 16-byte boundary are laid out anew: 100 rows of 128
     assert (B.tagc_linear_forward_workspace(_fwd(x=AT + 2)) - B.tagc_linear_forward_workspace(_fwd())) == 100 * 128 * 2
     assert B.tagc_linear_forward_workspace(_fwd(dtype=B.TAGC_F32)) >= (100 + 64) * 128 * 6
-    need = B.tagc_linear_backward_workspace(_bwd())
-    assert need > 0
-    assert _code(B.tagc_linear_backward, _bwd(), None) == -1
-    assert _code(B.tagc_linear_backward, _bwd(), AT + 16) == -1
-    assert B.tagc_linear_backward_workspace(_bwd(dx=None, w=None)) <= need
+    # behind an activation dz is laid out, and a bias's gradient has partial sums
+    behind = dict(pre=AT, ldp=64, activation=B.TAGC_ACT_SILU)
+    need = B.tagc_linear_backward_workspace(_bwd(**behind))
+    assert need >= 100 * 64 * 2
+    assert B.tagc_linear_backward_workspace(_bwd(db=AT, **behind)) > need
+    assert _code(B.tagc_linear_backward, _bwd(**behind), None) == -1
+    assert _code(B.tagc_linear_backward, _bwd(**behind), AT + 16) == -1
+    assert B.tagc_linear_backward_workspace(_bwd(dx=None, w=None, **behind)) <= need
     assert B.tagc_linear_backward_workspace(_bwd(dx=None, dw=None)) == 0

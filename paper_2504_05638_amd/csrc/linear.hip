@@ -38,39 +38,83 @@ inline uint64_t up(uint64_t a, uint64_t b) { return (a + b - 1) / b * b; }
 
 // ------------------------------------------------------------------ activations
 
-__device__ inline float sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+// (the hardware's exp2 and reciprocal: within 2 ulp each)
+__device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
 // (tanh form: 0.5 (1 + tanh a) = sigmoid(2 a))
 constexpr float kTanhIn = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kCubic = 0.044715f;
 
-__device__ inline float activate(float z, uint32_t act)
+// 0.5 (1 + erf(z / sqrt(2))) and exp(-z^2 / 2).  For bfloat16 by Abramowitz and Stegun, 7.1.26, which is
+// off by 1.5e-7 at most, a fiftieth of what rounding the result leaves of it even where it is smallest against it.
+template <typename T>
+__device__ inline float normal_below(float z, float &bell)
 {
+    bell = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
+    if constexpr (sizeof(T) == 4) return 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678118654752f * fabsf(z));
+    const float tail = 0.5f * bell * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    return z < 0 ? tail : 1.0f - tail;
+}
+
+template <typename T, int N>
+__device__ inline void activate(float (&z)[N], uint32_t act)
+{
+    float bell;
     switch (act) {
-        case TAGC_ACT_RELU: return z > 0 ? z : (z != z ? z : 0.0f);
-        case TAGC_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-        case TAGC_ACT_GELU_TANH: return z * sigmoid(kTanhIn * (z + kCubic * z * z * z));
-        case TAGC_ACT_SILU: return z * sigmoid(z);
-        default: return z;
+        case TAGC_ACT_RELU:
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] = z[j] > 0 ? z[j] : (z[j] != z[j] ? z[j] : 0.0f);
+            break;
+        case TAGC_ACT_GELU:
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] *= normal_below<T>(z[j], bell);
+            break;
+        case TAGC_ACT_GELU_TANH:
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] *= sigmoid(kTanhIn * (z[j] + kCubic * z[j] * z[j] * z[j]));
+            break;
+        case TAGC_ACT_SILU:
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] *= sigmoid(z[j]);
+            break;
+        default: break;
     }
 }
 
-__device__ inline float slope(float z, uint32_t act)
+// x times the activation's slope at z
+template <typename T, int N>
+__device__ inline void times_slope(float (&x)[N], const float (&z)[N], uint32_t act)
 {
+    float bell;
     switch (act) {
-        case TAGC_ACT_RELU: return z > 0 ? 1.0f : 0.0f;
+        case TAGC_ACT_RELU:
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] *= z[j] > 0 ? 1.0f : (z[j] != z[j] ? z[j] : 0.0f);
+            break;
         case TAGC_ACT_GELU:
-            return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
-        case TAGC_ACT_GELU_TANH: {
-            // (beyond 16 the sigmoid is 0 or 1, and z^2 would meet its 0 as an infinity)
-            const float s = sigmoid(kTanhIn * (z + kCubic * z * z * z)), c = fminf(fmaxf(z, -16.0f), 16.0f);
-            return s + c * s * (1.0f - s) * kTanhIn * (1.0f + 3.0f * kCubic * c * c);
-        }
-        case TAGC_ACT_SILU: {
-            const float s = sigmoid(z);
-            return s * (1.0f + z * (1.0f - s));
-        }
-        default: return 1.0f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float below = normal_below<T>(z[j], bell);
+                x[j] *= below + z[j] * 0.39894228040143268f * bell;
+            }
+            break;
+        case TAGC_ACT_GELU_TANH:
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                // (beyond 16 the sigmoid is 0 or 1, and z^2 would meet its 0 as an infinity)
+                const float s = sigmoid(kTanhIn * (z[j] + kCubic * z[j] * z[j] * z[j])), c = fminf(fmaxf(z[j], -16.0f), 16.0f);
+                x[j] *= s + c * s * (1.0f - s) * kTanhIn * (1.0f + 3.0f * kCubic * c * c);
+            }
+            break;
+        case TAGC_ACT_SILU:
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float s = sigmoid(z[j]);
+                x[j] *= s * (1.0f + z[j] * (1.0f - s));
+            }
+            break;
+        default: break;
     }
 }
 
@@ -85,27 +129,33 @@ __device__ inline float widen(T x)
 template <typename T>
 __device__ inline T narrow(float x)
 {
-    if constexpr (sizeof(T) == 2) return T(round_to_bf16(x));
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(T, static_cast<__bf16>(x));  // to nearest, ties to even
     else return x;
 }
 
 // N neighbours at an element's address
 template <typename T, int N>
+struct Lane {
+    typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    vec v;
+    __device__ inline void load(const T *p) { v = *reinterpret_cast<const vec *>(p); }
+    __device__ inline float operator[](int j) const { return widen(T(v[j])); }
+};
+template <typename T, int N>
 __device__ inline void load_n(const T *p, float (&out)[N])
 {
-    typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    const vec v = *reinterpret_cast<const vec *>(p);
+    Lane<T, N> in;
+    in.load(p);
 #pragma unroll
-    for (int j = 0; j < N; ++j) out[j] = widen(T(v[j]));
+    for (int j = 0; j < N; ++j) out[j] = in[j];
 }
 template <typename T, int N>
 __device__ inline void store_n(T *p, const float (&in)[N])
 {
-    typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    vec v;
+    typename Lane<T, N>::vec v;
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = narrow<T>(in[j]);
-    *reinterpret_cast<vec *>(p) = v;
+    *reinterpret_cast<typename Lane<T, N>::vec *>(p) = v;
 }
 
 // ------------------------------------------------------------------ laying operands out
@@ -178,9 +228,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
             }
         }
         // (rows and columns that do not exist are 0 whatever the slope at 0 is)
-        if (pre)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[i][j] *= slope(z[j], a.act);
+        if (pre) times_slope<T>(x[i], z, a.act);
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] += x[i][j];
     }
@@ -228,54 +276,51 @@ __global__ __launch_bounds__(256) void bias_kernel(const float *sums, uint32_t t
 // ------------------------------------------------------------------ results
 
 struct Result {
-    const void *bias;      // [n] or NULL
-    const void *residual;  // [m, n] or NULL
+    const void *bias;   // [n] or NULL
+    const void *added;  // [m, n] or NULL: the residual, or the result itself where it is added to
     void *out;
-    void *pre;             // or NULL
-    uint64_t ldr, ldo, ldp;
-    uint32_t act, accumulate;
+    void *pre;          // or NULL
+    uint64_t lda, ldo, ldp;
+    uint32_t act;
 };
 
-// Eight neighbours of a row of the result, of which `count` exist.
+// Eight neighbours of a row of the result, all there; what is added has been read.
+template <typename T>
+__device__ inline void finish(const Result &r, uint32_t m, uint32_t n, const float (&bias)[8], const Lane<T, 8> &added, float (&z)[8])
+{
+    if (r.bias)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] += bias[j];
+    if (r.pre) store_n<T, 8>(static_cast<T *>(r.pre) + m * r.ldp + n, z);
+    activate<T>(z, r.act);
+    if (r.added)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] += added[j];
+    store_n<T, 8>(static_cast<T *>(r.out) + m * r.ldo + n, z);
+}
+
+// The same of which `count` are there.
 template <typename T>
 __device__ inline void finish(const Result &r, uint32_t m, uint32_t n, uint32_t count, float (&z)[8])
 {
-    const T *bias = static_cast<const T *>(r.bias), *res = static_cast<const T *>(r.residual);
-    T *out = static_cast<T *>(r.out) + m * r.ldo + n, *pre = static_cast<T *>(r.pre);
-    float t[8];
+    const T *bias = static_cast<const T *>(r.bias) + n, *add = static_cast<const T *>(r.added) + m * r.lda + n;
     if (count == 8) {
-        if (bias) {
-            load_n<T, 8>(bias + n, t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] += t[j];
-        }
-        if (pre) store_n<T, 8>(pre + m * r.ldp + n, z);
-        if (r.act)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = activate(z[j], r.act);
-        if (res) {
-            load_n<T, 8>(res + m * r.ldr + n, t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] += t[j];
-        }
-        if (r.accumulate) {
-            load_n<T, 8>(out, t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] += t[j];
-        }
-        store_n<T, 8>(out, z);
-        return;
+        float b[8];
+        Lane<T, 8> added;
+        if (r.bias) load_n<T, 8>(bias, b);
+        if (r.added) added.load(add);
+        return finish<T>(r, m, n, b, added, z);
     }
+    T *out = static_cast<T *>(r.out) + m * r.ldo + n, *pre = static_cast<T *>(r.pre) + m * r.ldp + n;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (uint32_t(j) >= count) continue;
-        float x = z[j];
-        if (bias) x += widen(bias[n + j]);
-        if (pre) pre[m * r.ldp + n + j] = narrow<T>(x);
-        x = activate(x, r.act);
-        if (res) x += widen(res[m * r.ldr + n + j]);
-        if (r.accumulate) x += widen(out[j]);
-        out[j] = narrow<T>(x);
+    for (uint32_t j = 0; j < 8; ++j) {
+        if (j >= count) break;
+        float x[1] = {z[j]};
+        if (r.bias) x[0] += widen(bias[j]);
+        if (r.pre) pre[j] = narrow<T>(x[0]);
+        activate<T>(x, r.act);
+        if (r.added) x[0] += widen(add[j]);
+        out[j] = narrow<T>(x[0]);
     }
 }
 
@@ -550,34 +595,43 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     // are written together.
     float *strip = reinterpret_cast<float *>(wave * 32 * kRow * 4 + 32 * kRow * 4 <= kStage ? stage0 + wave * 32 * kRow * 4
                                                                                             : stage1 + (wave - kStage / (32 * kRow * 4)) * 32 * kRow * 4);
-#pragma unroll
-    for (int i = 0; i < RM; i += 2) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < RN; ++j)
-                *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[i + h][j];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        constexpr uint32_t across = RN * 2, rows = 64 / across;
+    constexpr uint32_t across = RN * 2, rows = 64 / across, kLines = 32 / rows;
+    const uint32_t ln = lane % across * 8, n = n0 + wn * RN * 16 + ln, have = n < a.n ? min(8u, a.n - n) : 0;
+    const Result &res = a.result;
+    float bias[8] = {};
+    if (res.bias && have == 8) load_n<T, 8>(static_cast<const T *>(res.bias) + n, bias);
 #pragma unroll 1
-        for (uint32_t r = 0; r < 32; r += rows) {
-            const uint32_t lr = r + lane / across, ln = lane % across * 8;
-            const uint32_t m = m0 + (wm * RM + i) * 16 + lr, n = n0 + wn * RN * 16 + ln;
+    for (int i = 0; i < RM; i += 2) {
+        // (one copy of what follows for all strips; registers are not found by a number at run time)
+#pragma unroll
+        for (int at = 0; at < RM; at += 2)
+            if (at == i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < RN; ++j)
+                        *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[at + h][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const uint32_t m = m0 + (wm * RM + i) * 16 + lane / across;
+        Lane<T, 8> added[kLines];
+        if (res.added && a.splits == 1 && have == 8)
+#pragma unroll
+            for (uint32_t l = 0; l < kLines; ++l)
+                if (m + l * rows < a.m) added[l].load(static_cast<const T *>(res.added) + (m + l * rows) * res.lda + n);
+#pragma unroll
+        for (uint32_t l = 0; l < kLines; ++l) {
+            if (m + l * rows >= a.m || !have) continue;
             float z[8];
 #pragma unroll
             for (int h = 0; h < 8; h += 4) {
-                const float4 v = *reinterpret_cast<const float4 *>(strip + lr * kRow + ln + h);
+                const float4 v = *reinterpret_cast<const float4 *>(strip + (l * rows + lane / across) * kRow + ln + h);
                 z[h] = v.x;
                 z[h + 1] = v.y;
                 z[h + 2] = v.z;
                 z[h + 3] = v.w;
             }
-            if (m >= a.m || n >= a.n) continue;
-            const uint32_t have = min(8u, a.n - n);
-            if (a.splits == 1) {
-                finish<T>(a.result, m, n, have, z);
-            } else {
-                float *to = a.partial + (uint64_t(part) * a.m + m) * a.n + n;
+            if (a.splits != 1) {
+                float *to = a.partial + (uint64_t(part) * a.m + m + l * rows) * a.n + n;
                 if (have == 8) {
                     store_n<float, 8>(to, z);
                 } else {
@@ -585,6 +639,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
                     for (uint32_t h = 0; h < 8; ++h)
                         if (h < have) to[h] = z[h];
                 }
+            } else if (have == 8) {
+                finish<T>(res, m + l * rows, n, bias, added[l], z);
+            } else {
+                finish<T>(res, m + l * rows, n, have, z);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -949,7 +1007,7 @@ int check_sizes(uint64_t rows, uint64_t in, uint64_t out, uint32_t dtype, uint32
 template <typename T>
 int forward(const tagc_linear *l, Places &w, bool enqueue, hipStream_t s)
 {
-    Result r{l->bias, l->residual, l->y, l->pre, l->ldr, l->ldy, l->ldp, l->activation, 0};
+    const Result r{l->bias, l->residual, l->y, l->pre, l->ldr, l->ldy, l->ldp, l->activation};
     const uint64_t M = l->rows, K = l->in, N = l->out;
     if (!M || !N) return TAGC_OK;
     if (M <= kFewRows[l->dtype]) {
@@ -1007,10 +1065,10 @@ int backward(const tagc_linear_grad *l, Places &w, bool enqueue, hipStream_t s)
         ProfileScope prof("linear_bias", s);
         bias_kernel<T><<<uint32_t((N + 255) / 256), 256, 0, s>>>(a.sums, tiles, uint32_t(N), static_cast<T *>(l->db), l->accumulate);
     }
-    if (dx) launch_product<T, false, true>(dz, wq, M, K, N, partial, Result{nullptr, nullptr, l->dx, nullptr, 0, l->lddx, 0, TAGC_ACT_NONE, 0}, s);
+    if (dx) launch_product<T, false, true>(dz, wq, M, K, N, partial, Result{nullptr, nullptr, l->dx, nullptr, 0, l->lddx, 0, TAGC_ACT_NONE}, s);
     if (dw)
         launch_product<T, true, true>(dz, xq, N, K, M, partial,
-                                      Result{nullptr, nullptr, l->dw, nullptr, 0, l->lddw, 0, TAGC_ACT_NONE, l->accumulate}, s);
+                                      Result{nullptr, l->accumulate ? l->dw : nullptr, l->dw, nullptr, l->lddw, l->lddw, 0, TAGC_ACT_NONE}, s);
     return hip_ok(hipGetLastError());
 }
 

@@ -158,8 +158,8 @@ enum { TAGC_ACT_NONE = 0, TAGC_ACT_RELU = 1, TAGC_ACT_GELU = 2 /* with erf */,
  * element; speed is best where they and the strides are multiples of 16 bytes.
  */
 typedef struct tagc_linear {
-    uint64_t rows, in, out;         /* tokens, features in and out; each < 2^22, the
-                                       three matrices together < 2^36 elements           */
+    uint64_t rows, in, out;         /* tokens, features in and out; each < 2^22 (float32:
+                                       2^20), the three matrices together < 2^36 elements */
     uint32_t dtype, activation;     /* TAGC_F32 | TAGC_BF16; TAGC_ACT_*                   */
     const void *x; uint64_t ldx;    /* [rows, in]                                         */
     const void *w; uint64_t ldw;    /* [out, in]                                          */

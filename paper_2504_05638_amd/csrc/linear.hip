@@ -27,12 +27,12 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kSlab = 64;        // k's of a stage in local memory: 128 bytes of a row
 constexpr uint32_t kPackRows = 64;
-constexpr uint32_t kPlanes = 3;       // bfloat16 numbers that a float32 is taken apart into
+constexpr uint32_t kParts = 3;        // bfloat16 numbers that a float32 is taken apart into
 // rows up to which few_kernel goes: in bfloat16 a thin tile is faster from 17 rows on (weights of 4096 by 11008, 17, 32, 64
 // rows: 32, 35, 48 us, 23, 24, 26 as tiles), in float32 the weights would have to be taken apart first (83, 86, 129 us; 164, 162, 167)
 constexpr uint32_t kFewRows[2] = {64, 16};  // TAGC_F32, TAGC_BF16
 
-constexpr uint64_t kMaxSide = 1u << 22;  // rows, features and direct strides are fewer
+constexpr uint64_t kMaxSide = 1u << 22;  // rows, features (in float32 a quarter) and strides as they lie are fewer
 
 inline uint64_t up(uint64_t a, uint64_t b) { return (a + b - 1) / b * b; }
 
@@ -167,7 +167,8 @@ struct PackArgs {
     uint32_t rows, cols;
     uint32_t act;
     uint16_t *to;         // [rows, to_ld] or NULL, zeros behind cols
-    uint64_t to_ld, to_plane;
+    uint64_t to_ld;
+    uint32_t to_part;     // float32: elements from one of the three parts of a row to the next
     float *sums;          // [tiles of rows, cols] or NULL: sums over a tile's rows
 };
 
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
                 for (int q = 0; q < planes; ++q) out[q][j] = s[q];
             }
 #pragma unroll
-            for (int q = 0; q < planes; ++q) *reinterpret_cast<u16x4 *>(a.to + q * a.to_plane + r * a.to_ld + c) = out[q];
+            for (int q = 0; q < planes; ++q) *reinterpret_cast<u16x4 *>(a.to + r * a.to_ld + q * a.to_part + c) = out[q];
         }
     if (!a.sums) return;
 #pragma unroll
@@ -329,7 +330,7 @@ __device__ inline void finish(const Result &r, uint32_t m, uint32_t n, uint32_t 
 struct Product {
     const uint16_t *p, *q;          // bfloat16, [m, k] and [n, k], or turned [k, m] and [k, n]; 4-byte aligned
     uint64_t ldp, ldq;              // multiples of 2; k a multiple of 8 where rows lie row by row
-    uint64_t plane_p, plane_q;      // from one of the three parts of a float32 to the next
+    uint32_t part_p, part_q;        // float32: elements from one of the three parts of a row to the next
     uint32_t m, n, k;
     uint32_t tiles_m, tiles_n;
     uint32_t slabs;                 // slabs of one part of the sum, in all terms
@@ -351,11 +352,24 @@ struct Side;
 constexpr uint32_t kMostBytes = 1u << 31;  // of a descriptor, and ...
 constexpr uint32_t kNowhere = 3u << 30;    // ... an offset behind every one; what a tile reads has smaller offsets
 
-__device__ inline __amdgpu_buffer_rsrc_t described(const uint16_t *p, uint64_t elems)
-{
-    const uint64_t bytes = elems * 2;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, bytes < kMostBytes ? uint32_t(bytes) : kMostBytes, 0x00020000);
-}
+
+// Where an operand's next slab begins, and how many elements there are from there to the operand's end.
+struct Walk {
+    const uint16_t *p;
+    uint64_t left;
+    uint32_t step;  // elements from one slab to the next
+    __device__ inline void advance(bool on)
+    {
+        p += on ? step : 0;
+        left -= on ? step : 0;
+    }
+    // the slab of one of a float32's three parts, `part` elements further on
+    __device__ inline __amdgpu_buffer_rsrc_t described(uint32_t part) const
+    {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p) + part, 0, left < kMostBytes / 2 ? uint32_t(left) * 2 : kMostBytes, 0x00020000);
+    }
+};
+
 __device__ inline void load_lds(__amdgpu_buffer_rsrc_t from, uint32_t off, char *to)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, off, 0, 0, 0);
@@ -376,9 +390,9 @@ struct Side<false, R, THREADS> {
         for (uint32_t i = 0; i < kLoads; ++i) off[i] = (sub + i * (THREADS / 8)) * uint32_t(ld * 2) + piece * 16;
     }
     // the operand from row r0 and k0 on (of a row whose k's are no multiple of eight there are zeros up to one)
-    __device__ static inline __amdgpu_buffer_rsrc_t aim(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
+    __device__ static inline Walk walk(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
     {
-        return described(p + r0 * ld + k0, (rows - r0 - 1) * ld + ((end + 7) & ~7u) - k0);
+        return Walk{p + r0 * ld + k0, (rows - r0 - 1) * ld + ((end + 7) & ~7u) - k0, kSlab};
     }
     __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, uint32_t k0, uint32_t end, char *stage, uint32_t wave) const
     {
@@ -415,9 +429,9 @@ struct Side<true, R, THREADS> {
             off[i] = (k + i * kDown) * uint32_t(ld * 2) + (r0 + (threadIdx.x % kAcross ^ (2 * turn(k + i * kDown))) * 8) * 2;
     }
     // the operand from k0 on (a descriptor ends with a word: of an odd number of rows there is one more)
-    __device__ static inline __amdgpu_buffer_rsrc_t aim(const uint16_t *p, uint32_t, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
+    __device__ static inline Walk walk(const uint16_t *p, uint32_t, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
     {
-        return described(p + k0 * ld, (end - k0 - 1) * ld + ((rows + 1) & ~1u));
+        return Walk{p + k0 * ld, (end - k0 - 1) * ld + ((rows + 1) & ~1u), uint32_t(ld) * kSlab};
     }
     __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, uint32_t, uint32_t, char *stage, uint32_t wave) const
     {
@@ -484,20 +498,24 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     const uint32_t first = part * a.slabs, all = (a.k + kSlab - 1) / kSlab * terms;
     const uint32_t count = min(a.slabs, all - first);
 
+    // The next slab to fetch, found before the waves meet.  Behind the last one it is the last one again.
     struct Aim {
         __amdgpu_buffer_rsrc_t p, q;
         uint32_t k0;
     };
-    auto aim = [&](uint32_t s) {
-        const uint32_t k0 = s / terms * kSlab;
-        const uint16_t *p = a.p, *q = a.q;
-        if constexpr (terms > 1) {
-            p += term_p(s % terms) * a.plane_p;
-            q += term_q(s % terms) * a.plane_q;
-        }
-        return Aim{side_p.aim(p, m0, a.m, k0, a.k, a.ldp), side_q.aim(q, n0, a.n, k0, a.k, a.ldq), k0};
+    uint32_t k0 = first / terms * kSlab, term = first % terms, to_come = count;
+    Walk walk_p = side_p.walk(a.p, m0, a.m, k0, a.k, a.ldp), walk_q = side_q.walk(a.q, n0, a.n, k0, a.k, a.ldq);
+    auto aim = [&]() __attribute__((always_inline)) {
+        const Aim at{walk_p.described(terms > 1 ? term_p(term) * a.part_p : 0), walk_q.described(terms > 1 ? term_q(term) * a.part_q : 0), k0};
+        const bool more = to_come > 1, on = more && term + 1 == terms;
+        to_come -= more;
+        term = on ? 0 : term + more;
+        k0 += on ? kSlab : 0;
+        walk_p.advance(on);
+        walk_q.advance(on);
+        return at;
     };
-    auto fetch = [&](const Aim &at, char *stage) {
+    auto fetch = [&](const Aim &at, char *stage) __attribute__((always_inline)) {
         side_p.fetch(at.p, at.k0, a.k, stage, wave);
         side_q.fetch(at.q, at.k0, a.k, stage + TM * 128, wave);
     };
@@ -512,9 +530,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
 
     constexpr int H = RM / 2;
     bf16x8 fp[2][H], fq[2][RN];
-    auto read_q = [&](const char *stage, uint32_t step) { side_q.template read<RN>(stage + TM * 128, wn * RN, step, fq[step]); };
-    auto read_p = [&](const char *stage, uint32_t step, int half) { side_p.template read<H>(stage, wm * RM + half * H, step, fp[half]); };
-    auto multiply = [&](int step, int half) {
+    auto read_q = [&](const char *stage, uint32_t step) __attribute__((always_inline)) { side_q.template read<RN>(stage + TM * 128, wn * RN, step, fq[step]); };
+    auto read_p = [&](const char *stage, uint32_t step, int half) __attribute__((always_inline)) { side_p.template read<H>(stage, wm * RM + half * H, step, fp[half]); };
+    auto multiply = [&](int step, int half) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < H; ++i)
 #pragma unroll
@@ -525,7 +543,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     constexpr int kEachP = PT ? 2 : 1, kEachQ = QT ? 2 : 1, kReads = H * kEachP + RN * kEachQ;
     constexpr int kOnce = (kReads + H * RN - 1) / (H * RN), kBoth = (kReads + kOnce - 1) / kOnce;
     // The next pieces are read while the products of the last ones run, one read behind each of the first products.
-    auto woven = [&](auto reads) {
+    auto woven = [&](auto reads) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < H * RN; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -533,13 +551,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
         }
     };
     // What this wave has asked for has come, then what the others have.
-    auto arrived = [&]() {
+    auto arrived = [&]() __attribute__((always_inline)) {
         wait_own_memory_ops();
         __syncthreads();
     };
     // One slab: its first pieces are in registers, the next slab is on its way to `next`.  (Behind the last slab the
     // last one is fetched again, and never used: a branch here would cost the registers that the loop lacks.)
-    auto slab = [&](uint32_t s, char *now, const char *next) {
+    auto slab = [&](char *now, const char *next) __attribute__((always_inline)) {
         read_p(now, 0, 1);
         multiply(0, 0);
         woven(std::integral_constant<int, (H * kEachP + kOnce - 1) / kOnce>());
@@ -547,7 +565,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
         read_p(now, 1, 0);
         multiply(0, 1);
         woven(std::integral_constant<int, kBoth>());
-        const Aim at = aim(first + min(s + 2, count - 1));
+        const Aim at = aim();
         read_p(now, 1, 1);
         multiply(1, 0);
         woven(std::integral_constant<int, (H * kEachP + kOnce - 1) / kOnce>());
@@ -573,20 +591,20 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
         }
     };
 
-    fetch(aim(first), stage0);
-    fetch(aim(first + min(1u, count - 1)), stage1);
+    fetch(aim(), stage0);
+    fetch(aim(), stage1);
     arrived();
     read_q(stage0, 0);
     read_p(stage0, 0, 0);
     // (said of the pointers, this keeps the compiler from having a transposing read wait for loads into the other stage; plain reads
     // it knows better without)
-    auto slab_apart = [&](uint32_t s, char *__restrict now, const char *__restrict next) { slab(s, now, next); };
+    auto slab_apart = [&](char *__restrict now, const char *__restrict next) __attribute__((always_inline)) { slab(now, next); };
     for (uint32_t s = 0; s < count; s += 2) {
-        if constexpr (PT || QT) slab_apart(s, stage0, stage1);
-        else slab(s, stage0, stage1);
+        if constexpr (PT || QT) slab_apart(stage0, stage1);
+        else slab(stage0, stage1);
         if (s + 1 < count) {
-            if constexpr (PT || QT) slab_apart(s + 1, stage1, stage0);
-            else slab(s + 1, stage1, stage0);
+            if constexpr (PT || QT) slab_apart(stage1, stage0);
+            else slab(stage1, stage0);
         }
     }
     arrived();
@@ -680,7 +698,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float *partial, uint32_
 
 struct FewArgs {
     const void *x, *w;      // x: as it lies, or (float32, over 16 rows) taken apart by pack_kernel
-    uint64_t ldx, ldw, plane;
+    uint64_t ldx, ldw;
+    uint32_t part;          // elements from one of the three parts of a row of x to the next
     uint32_t rows, in, out;
     Result result;
 };
@@ -756,7 +775,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void few_kernel(FewArgs a)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int q = 0; q < read; ++q) px[d][i][q].load(x[i] + q * a.plane, from, a.in);
+                for (int q = 0; q < read; ++q) px[d][i][q].load(x[i] + q * a.part, from, a.in);
         }
 #pragma unroll
         for (int d = 0; d < D; ++d)
@@ -884,7 +903,8 @@ struct Places {
 
 struct Operand {
     const uint16_t *p;
-    uint64_t ld, plane;
+    uint64_t ld;
+    uint32_t part;  // of float32 the three parts of a row, one behind the other, are so far apart
 };
 
 // whether a matrix with `cols` elements to a row can be read as it lies: in words, and, where a row is k's, in pieces of 16 bytes
@@ -894,12 +914,10 @@ bool as_it_lies(uint32_t dtype, const void *p, uint64_t ld, uint64_t cols, bool 
     return dtype == TAGC_BF16 && (reinterpret_cast<uintptr_t>(p) & 3) == 0 && ld % 2 == 0 && ld < kMaxSide && cols % (turned ? 2 : 8) == 0;
 }
 
-uint32_t planes_of(uint32_t dtype) { return dtype == TAGC_F32 ? kPlanes : 1; }
-
 Operand room(Places &w, uint32_t dtype, uint64_t rows, uint64_t cols)
 {
-    const uint64_t ld = up(cols, 64), plane = rows * ld;
-    return Operand{w.take<uint16_t>(plane * planes_of(dtype)), ld, plane};
+    const uint64_t part = up(cols, 64), ld = part * (dtype == TAGC_F32 ? kParts : 1);
+    return Operand{w.take<uint16_t>(rows * ld), ld, uint32_t(part)};
 }
 
 PackArgs packed(const void *src, uint64_t ld, uint64_t rows, uint64_t cols, const Operand &to)
@@ -911,7 +929,7 @@ PackArgs packed(const void *src, uint64_t ld, uint64_t rows, uint64_t cols, cons
     a.cols = uint32_t(cols);
     a.to = const_cast<uint16_t *>(to.p);
     a.to_ld = to.ld;
-    a.to_plane = to.plane;
+    a.to_part = to.part;
     return a;
 }
 
@@ -952,8 +970,8 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     a.q = q.p;
     a.ldp = p.ld;
     a.ldq = q.ld;
-    a.plane_p = p.plane;
-    a.plane_q = q.plane;
+    a.part_p = p.part;
+    a.part_q = q.part;
     a.m = uint32_t(m);
     a.n = uint32_t(n);
     a.k = uint32_t(k);
@@ -997,7 +1015,8 @@ int check_sizes(uint64_t rows, uint64_t in, uint64_t out, uint32_t dtype, uint32
 {
     if (dtype > TAGC_BF16 || act > TAGC_ACT_SILU) return TAGC_EINVAL;
     // a tile's 256 rows span fewer than 2^32 bytes
-    if (rows >= kMaxSide || in >= kMaxSide || out >= kMaxSide) return TAGC_ESIZE;
+    const uint64_t most = dtype == TAGC_F32 ? kMaxSide / 4 : kMaxSide;
+    if (rows >= most || in >= most || out >= most) return TAGC_ESIZE;
     // a launch has fewer than 2^32 threads: at most a workgroup of 256 for each tile of 64 by 64 of all three matrices
     const uint64_t r = up(rows, 64) / 64, i = up(in, 64) / 64, o = up(out, 64) / 64;
     if (r * i + r * o + i * o >= (1ull << 24)) return TAGC_ESIZE;
@@ -1018,7 +1037,7 @@ int forward(const tagc_linear *l, Places &w, bool enqueue, hipStream_t s)
             if (enqueue) packs.launch<T>(s);
             a.x = x.p;
             a.ldx = x.ld;
-            a.plane = x.plane;
+            a.part = x.part;
         }
         if (!enqueue) return TAGC_OK;
         ProfileScope prof("linear_few", s);

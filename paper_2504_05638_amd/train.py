@@ -5,7 +5,7 @@ marshalling only; all arithmetic is the library's (include/tagc_train.h).
     y, pre = linear(x, w, b, activation="gelu", save=True)
     dx = linear_backward(dy, x, w, pre, activation="gelu", dw=bucket_grad_view, db=...)
     ...                                # the exchange: bucket.TagcBucket
-    opt = AdamW(params=..., grads=..., max_norm=1.0, bits=8)
+    opt = AdamW(params=..., grads=dense_views(bucket), max_norm=1.0, bits=8)
     opt.grad_norm()                    # norm, clip factor and step count, on the device
     opt.step()
 """
@@ -149,6 +149,20 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     ws, at = _work(B.tagc_linear_backward_workspace(a), x, stream)
     B.tagc_linear_backward(a, at, _stream_of(stream, device))
     return dx
+
+
+def dense_views(bucket):
+    """Per segment of a TagcBucket with a dense output: its summed gradient, float32, a view that the next decode
+    fills anew; None for a segment that is not compressed."""
+    _need(bucket.out_dense is not None, "a bucket made with dense=True is wanted")
+    dense, views, at = bucket.out_dense.view(torch.float32), [], 0
+    for _, length, _, flags in bucket.segments:
+        if not flags & B.TAGC_SEG_COMPRESS:
+            views.append(None)
+            continue
+        views.append(dense[at:at + length])
+        at += -(-length // 32) * 32  # segments begin at multiples of 32 there
+    return views
 
 
 class AdamW:

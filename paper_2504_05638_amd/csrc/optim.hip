@@ -22,7 +22,13 @@ constexpr uint32_t kOptimThreads = 256;
 constexpr uint32_t kSteps = 4;                                   // times that a thread takes four neighbours
 constexpr uint32_t kChunk = kOptimThreads * 4 * kSteps;          // elements of a workgroup
 constexpr uint32_t kNormGroups = 2048;                           // most workgroups of the norm
+constexpr uint32_t kArriveTogether = 32, kArriveWords = 16;      // workgroups that a count is for; words from count to count
+constexpr uint32_t kArriveBytes = 4 * kArriveWords * (1 + kNormGroups / kArriveTogether);
 constexpr uint64_t kMaxLength = 1ull << 34;                      // an element's number / 4 fits 32 bits
+// (8-bit moments: half the steps; 202 M with bf16 gradients 549 -> 539 us, 9 M at odd places 30.1 -> 27.4; with 32 bits two steps
+// are the slower ones, 151 M 717 -> 733 us)
+constexpr uint32_t kCodeThreads = 512, kCodeSteps = 2;
+static_assert(kCodeThreads * 4 * kCodeSteps == kChunk, "the same chunks");
 static_assert(kChunk % TAGC_MOMENT_BLOCK == 0 && TAGC_MOMENT_BLOCK == 4 * 64, "a wave's step is a block");
 
 struct TensorDev {
@@ -56,7 +62,7 @@ struct tagc_optim_s {
     uint32_t n_groups;  // groups that the tensors name
     tagc_optim_sizes sizes;
 
-    // the table: rows, chunks, then the device state: arrivals (16 bytes), the norm's partial sums
+    // the table: rows, chunks, then the device state: arrivals, the norm's partial sums
     uint64_t chunks_at() const { return rows.size() * sizeof(tagc::TensorDev); }
     uint64_t state_at() const { return (chunks_at() + chunks.size() * sizeof(tagc::ChunkDev) + 15) & ~uint64_t(15); }
 };
@@ -109,7 +115,7 @@ __device__ inline void store_f32(T *p, uint64_t i, uint64_t n, const float (&x)[
     T raw[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        if constexpr (sizeof(T) == 2) raw[j] = uint16_t(round_to_bf16(x[j]));
+        if constexpr (sizeof(T) == 2) raw[j] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x[j]));  // to nearest, ties to even
         else raw[j] = x[j];
     }
     if (i + 4 <= n) {
@@ -157,7 +163,11 @@ struct NormArgs {
     uint32_t n_chunks;
 };
 
-// Each workgroup leaves its part of the sum; the last to arrive adds the parts up, in their order.
+// Each workgroup leaves its part of the sum; the last to arrive adds the parts up, in their order.  Arrivals are counted
+// by 32 and then by those: 2048 adds to one word took some 12 ns each (9 M gradients 33 us, and 12 so).
+//
+// Bound by the gradients' bytes: 809 M in bfloat16 take 255 us, 151 M in float32 95, 6.3 TB/s both; a
+// call takes 5 us at least.
 __global__ __launch_bounds__(kOptimThreads) void norm_kernel(NormArgs a)
 {
     __shared__ double smem[kOptimThreads / 64];
@@ -174,7 +184,15 @@ __global__ __launch_bounds__(kOptimThreads) void norm_kernel(NormArgs a)
     if (threadIdx.x == 0) {
         __hip_atomic_store(&a.partial[blockIdx.x], uint64_t(__double_as_longlong(sum)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         wait_own_memory_ops();
-        last = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        const uint32_t group = blockIdx.x / kArriveTogether, groups = (gridDim.x + kArriveTogether - 1) / kArriveTogether;
+        const uint32_t of = min(kArriveTogether, gridDim.x - group * kArriveTogether);
+        uint32_t *mine = a.arrived + kArriveWords * (1 + group);
+        last = 0;
+        if (__hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1) {
+            // (counts are left as the next call expects them)
+            __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
+        }
     }
     __syncthreads();
     if (!last) return;
@@ -183,7 +201,7 @@ __global__ __launch_bounds__(kOptimThreads) void norm_kernel(NormArgs a)
         all += __longlong_as_double(int64_t(__hip_atomic_load(&a.partial[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
     all = block_sum<double, kOptimThreads / 64>(all, smem);
     if (threadIdx.x) return;
-    *a.arrived = 0;  // as the next call expects it
+    __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     tagc_optim_control *c = a.control;
     const double norm = a.grad_scale * sqrt(all);
     // (a norm that float32 cannot hold is not finite either)
@@ -229,9 +247,13 @@ __device__ inline void adamw(const Hyper &h, float grad, float &m, float &v, flo
     const float g = grad * h.factor;
     m = m * h.beta1 + g * h.rest1;
     v = v * h.beta2 + (g * g) * h.rest2;
-    p = p * h.decay - m / (sqrtf(v) * h.bias2 + h.eps) * h.size;
+    // (root and reciprocal as the hardware has them, within an ulp each: they go nowhere but into the update)
+    p = p * h.decay - m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * h.bias2 + h.eps) * h.size;
 }
 
+// Bound by bytes: 151 M elements in float32 (28 bytes each) take 713 us, 5.9 TB/s.  All loads of a thread, four times four
+// neighbours of four arrays, go out before the first is used, and none is kept by the caches (with
+// ordinary loads and stores 779 us).
 template <typename P, typename G>
 __device__ inline void adamw32_chunk(const TensorDev &t, uint64_t at, const Hyper &h)
 {
@@ -295,14 +317,37 @@ __device__ inline uint32_t rounded(uint32_t bits, uint32_t u)
     return min(q, most > 0x7F7u ? most : 0x7F7u);
 }
 
-__device__ inline uint32_t wave_max(uint32_t x)
+// Two 16-bit numbers' largest over a wave, each for itself, by the VALU alone.
+__device__ inline uint32_t max2(uint32_t a, uint32_t b)
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x = max(x, uint32_t(__shfl_xor(int(x), d, 64)));
-    return x;
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+template <int CTRL>
+__device__ inline uint32_t max2_from(uint32_t x)
+{
+    return max2(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, true)));
+}
+__device__ inline uint32_t wave_max2(uint32_t x)
+{
+    x = max2_from<0x111>(x);  // row_shr:1, 2, 4, 8: a row's last lane has the row's
+    x = max2_from<0x112>(x);
+    x = max2_from<0x114>(x);
+    x = max2_from<0x118>(x);
+    x = max2_from<0x142>(x);  // row_bcast:15, 31: the last lane has the wave's
+    x = max2_from<0x143>(x);
+    return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
 }
 
-// A wave's step is a block: its 64 lanes hold four neighbours each.
+// whether one of a word's bytes is 0
+__device__ inline bool zero_byte(uint32_t x) { return ((x - 0x01010101u) & ~x & 0x80808080u) != 0; }
+
+// A wave's step is a block: its 64 lanes hold four neighbours each, and the base takes one maximum over the wave.
+//
+// Bound by bytes where weights are float32 (202 M with bfloat16 gradients and copies, 16 bytes each, 540 us, 6.0 TB/s), by
+// the VALU where they are not (10 bytes each, 393 us, 5.1 TB/s): some 50 instructions an element, after root and
+// reciprocal by the hardware (659 -> 587 us, 535 -> 464), the maximum of both moments at once without local memory, and
+// what is seldom behind branches (587 -> 549, 464 -> 401).
 template <typename P, typename G>
 __device__ inline void adamw8_chunk(const TensorDev &t, uint64_t at, const Hyper &h, uint32_t key)
 {
@@ -312,11 +357,11 @@ __device__ inline void adamw8_chunk(const TensorDev &t, uint64_t at, const Hyper
     uint32_t *bases = as_global(t.bases);
     uint16_t *copy = as_global(t.copy);
     const uint64_t n = t.length;
-    float g[kSteps][4], p[kSteps][4];
-    uint32_t mc[kSteps], vc[kSteps], base[kSteps];
+    float g[kCodeSteps][4], p[kCodeSteps][4];
+    uint32_t mc[kCodeSteps], vc[kCodeSteps], base[kCodeSteps];
 #pragma unroll
-    for (uint32_t k = 0; k < kSteps; ++k) {
-        const uint64_t i = at + 4 * (k * kOptimThreads + threadIdx.x);
+    for (uint32_t k = 0; k < kCodeSteps; ++k) {
+        const uint64_t i = at + 4 * (k * kCodeThreads + threadIdx.x);
         const uint64_t block = i / TAGC_MOMENT_BLOCK;
         base[k] = block * TAGC_MOMENT_BLOCK < n ? bases[block] : 0;
         mc[k] = load_codes(mp, i, n);
@@ -325,38 +370,70 @@ __device__ inline void adamw8_chunk(const TensorDev &t, uint64_t at, const Hyper
         load_f32(param, i, n, p[k]);
     }
 #pragma unroll
-    for (uint32_t k = 0; k < kSteps; ++k) {
-        const uint64_t i = at + 4 * (k * kOptimThreads + threadIdx.x);
+    for (uint32_t k = 0; k < kCodeSteps; ++k) {
+        const uint64_t i = at + 4 * (k * kCodeThreads + threadIdx.x);
         const uint64_t block = i / TAGC_MOMENT_BLOCK;
         if (block * TAGC_MOMENT_BLOCK >= n) break;  // (the same for a whole wave)
-        const uint32_t word = mix32(uint32_t(i / 4) ^ key);
+        const uint32_t word = mix32(uint32_t(i / 4) ^ key), base_m = base[k] & 0xFFFF, base_v = base[k] >> 16;
         float m[4], v[4];
-        uint32_t u[4], qm[4], qv[4], most_m = 0, most_v = 0;
+        uint32_t u[4], bits_m[4], bits_v[4], q[4], most = 0;
+        // Codes of 0, numbers that are not finite and numbers far under the block's largest are seldom: what they
+        // take is a branch that whole waves go past.
+        const bool zeros = zero_byte(mc[k] & 0x7F7F7F7Fu) | zero_byte(vc[k]);
+        if (__builtin_expect(__any(zeros), 0)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t c = (mc[k] >> (8 * j)) & 0xFF, d = (vc[k] >> (8 * j)) & 0xFF;
+                m[j] = __uint_as_float(code_bits(c & 127, base_m) | (c & 128) << 24);
+                v[j] = __uint_as_float(code_bits(d, base_v));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t c = (mc[k] >> (8 * j)) & 0xFF, d = (vc[k] >> (8 * j)) & 0xFF;
+                m[j] = __uint_as_float(((c & 127) + base_m) << 20 | (c & 128) << 24);
+                v[j] = __uint_as_float((d + base_v) << 20);
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t c = (mc[k] >> (8 * j)) & 0xFF, d = (vc[k] >> (8 * j)) & 0xFF;
-            m[j] = __uint_as_float(code_bits(c & 127, base[k] & 0xFFFF) | (c & 128) << 24);
-            v[j] = __uint_as_float(code_bits(d, base[k] >> 16));
             adamw(h, g[k][j], m[j], v[j], p[k][j]);
             u[j] = j ? (word >> (8 * j)) | (word << (32 - 8 * j)) : word;
-            qm[j] = rounded(__float_as_uint(m[j]) & 0x7FFFFFFFu, u[j] & 0xFFFF);
-            qv[j] = rounded(__float_as_uint(v[j]) & 0x7FFFFFFFu, u[j] >> 16);
-            most_m = max(most_m, qm[j]);
-            most_v = max(most_v, qv[j]);
+            bits_m[j] = __float_as_uint(m[j]);
+            bits_v[j] = __float_as_uint(v[j]);
+            q[j] = ((bits_m[j] & 0x7FFFFFFFu) + (u[j] & 0xFFFF) * 16) >> 20 | ((bits_v[j] & 0x7FFFFFFFu) + (u[j] >> 16) * 16) >> 20 << 16;
+            most = max2(most, q[j]);
         }
-        most_m = wave_max(most_m);
-        most_v = wave_max(most_v);
-        const uint32_t bm = most_m > 127 ? most_m - 127 : 0, bv = most_v > 255 ? most_v - 255 : 0;
-        const float least = __uint_as_float((bm + 1) << 20);
-        uint32_t new_m = 0, new_v = 0;
+        most = wave_max2(most);
+        uint32_t new_m = 0, new_v = 0, bm = max(most & 0xFFFF, 127u) - 127, bv = max(most >> 16, 255u) - 255;
+        bool low = false;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t low_m = float(u[j] & 0xFFFF) * 0x1p-16f * least < fabsf(m[j]);
-            const uint32_t low_v = v[j] > 0;
-            const uint32_t c = (qm[j] > bm ? qm[j] - bm : low_m) | (m[j] < 0 ? 128u : 0u);
-            const uint32_t d = qv[j] > bv ? qv[j] - bv : low_v;
-            new_m |= c << (8 * j);
-            new_v |= d << (8 * j);
+        for (int j = 0; j < 4; ++j) low |= (q[j] & 0xFFFF) <= bm || q[j] >> 16 <= bv;
+        if (__builtin_expect((most & 0xFFFF) < 0x7F8 && most >> 16 < 0x7F8 && !__any(low), 1)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                new_m |= ((q[j] & 0xFFFF) - bm | (bits_m[j] >> 24 & 128)) << (8 * j);
+                new_v |= ((q[j] >> 16) - bv) << (8 * j);
+            }
+        } else {
+            uint32_t qm[4], qv[4];
+            most = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                qm[j] = rounded(bits_m[j] & 0x7FFFFFFFu, u[j] & 0xFFFF);
+                qv[j] = rounded(bits_v[j] & 0x7FFFFFFFu, u[j] >> 16);
+                most = max2(most, qm[j] | qv[j] << 16);
+            }
+            most = wave_max2(most);
+            bm = max(most & 0xFFFF, 127u) - 127;
+            bv = max(most >> 16, 255u) - 255;
+            const float least = __uint_as_float((bm + 1) << 20);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t low_m = float(u[j] & 0xFFFF) * 0x1p-16f * least < fabsf(m[j]), low_v = v[j] > 0;
+                new_m |= ((qm[j] > bm ? qm[j] - bm : low_m) | (m[j] < 0 ? 128u : 0u)) << (8 * j);
+                new_v |= (qv[j] > bv ? qv[j] - bv : low_v) << (8 * j);
+            }
         }
         if (i < n) {
             store_codes(mp, i, n, new_m);
@@ -369,7 +446,7 @@ __device__ inline void adamw8_chunk(const TensorDev &t, uint64_t at, const Hyper
 }
 
 template <int BITS>
-__global__ __launch_bounds__(kOptimThreads) void adamw_kernel(StepArgs a)
+__global__ __launch_bounds__(BITS == 32 ? kOptimThreads : kCodeThreads) void adamw_kernel(StepArgs a)
 {
     const ChunkDev ch = a.chunks[blockIdx.x];
     const TensorDev &t = a.rows[ch.tensor];
@@ -407,7 +484,7 @@ __global__ __launch_bounds__(kOptimThreads) void adamw_kernel(StepArgs a)
 }
 
 // A code's bfloat16: the upper half of (base + c) << 20, and the sign.
-__global__ __launch_bounds__(kOptimThreads) void unpack_kernel(const TensorDev *rows, const ChunkDev *chunks,
+__global__ __launch_bounds__(kCodeThreads) void unpack_kernel(const TensorDev *rows, const ChunkDev *chunks,
                                                                uint16_t *m_out, uint16_t *v_out)
 {
     const ChunkDev ch = chunks[blockIdx.x];
@@ -416,17 +493,17 @@ __global__ __launch_bounds__(kOptimThreads) void unpack_kernel(const TensorDev *
     const uint32_t *bases = as_global(t.bases);
     const uint64_t n = t.length;
     uint16_t *mo = m_out + t.first, *vo = v_out + t.first;
-    uint32_t mc[kSteps], vc[kSteps], base[kSteps];
+    uint32_t mc[kCodeSteps], vc[kCodeSteps], base[kCodeSteps];
 #pragma unroll
-    for (uint32_t k = 0; k < kSteps; ++k) {
-        const uint64_t i = uint64_t(ch.chunk) * kChunk + 4 * (k * kOptimThreads + threadIdx.x);
+    for (uint32_t k = 0; k < kCodeSteps; ++k) {
+        const uint64_t i = uint64_t(ch.chunk) * kChunk + 4 * (k * kCodeThreads + threadIdx.x);
         base[k] = i < n ? bases[i / TAGC_MOMENT_BLOCK] : 0;
         mc[k] = load_codes(mp, i, n);
         vc[k] = load_codes(vp, i, n);
     }
 #pragma unroll
-    for (uint32_t k = 0; k < kSteps; ++k) {
-        const uint64_t i = uint64_t(ch.chunk) * kChunk + 4 * (k * kOptimThreads + threadIdx.x);
+    for (uint32_t k = 0; k < kCodeSteps; ++k) {
+        const uint64_t i = uint64_t(ch.chunk) * kChunk + 4 * (k * kCodeThreads + threadIdx.x);
         uint16_t m[4], v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -524,7 +601,7 @@ extern "C" int tagc_optim_plan(const tagc_optim_config *cfg, const tagc_tensor *
         return TAGC_ENOMEM;
     }
     p->sizes.n_chunks = p->chunks.size();
-    p->sizes.table_bytes = p->state_at() + 16 + 8 * kNormGroups;
+    p->sizes.table_bytes = p->state_at() + kArriveBytes + 8 * kNormGroups;
     *out = p;
     return TAGC_OK;
 }
@@ -549,7 +626,7 @@ extern "C" int tagc_optim_upload(const tagc_optim_t *p, void *table, void *strea
     if (!p->chunks.empty() && hipMemcpyAsync(t + p->chunks_at(), p->chunks.data(), p->chunks.size() * sizeof(ChunkDev),
                                              hipMemcpyHostToDevice, s) != hipSuccess)
         return TAGC_EHIP;
-    return hip_ok(hipMemsetAsync(t + p->state_at(), 0, 16, s));
+    return hip_ok(hipMemsetAsync(t + p->state_at(), 0, kArriveBytes, s));
 }
 
 extern "C" int tagc_grad_norm(const tagc_optim_t *p, void *table, tagc_optim_control *control, void *stream)
@@ -561,7 +638,7 @@ extern "C" int tagc_grad_norm(const tagc_optim_t *p, void *table, tagc_optim_con
     a.rows = reinterpret_cast<const TensorDev *>(t);
     a.chunks = reinterpret_cast<const ChunkDev *>(t + p->chunks_at());
     a.arrived = reinterpret_cast<uint32_t *>(t + p->state_at());
-    a.partial = reinterpret_cast<uint64_t *>(t + p->state_at() + 16);
+    a.partial = reinterpret_cast<uint64_t *>(t + p->state_at() + kArriveBytes);
     a.control = control;
     a.grad_scale = p->cfg.grad_scale;
     a.max_norm = p->cfg.max_norm;
@@ -613,7 +690,7 @@ extern "C" int tagc_adamw_step(const tagc_optim_t *p, const void *table, const t
         adamw_kernel<32><<<grid, kOptimThreads, 0, s>>>(a);
     } else {
         ProfileScope prof("adamw8", s);
-        adamw_kernel<8><<<grid, kOptimThreads, 0, s>>>(a);
+        adamw_kernel<8><<<grid, kCodeThreads, 0, s>>>(a);
     }
     return hip_ok(hipGetLastError());
 }
@@ -627,7 +704,7 @@ extern "C" int tagc_adamw_unpack(const tagc_optim_t *p, const void *table, void 
     hipStream_t s = static_cast<hipStream_t>(stream);
     const char *t = static_cast<const char *>(table);
     ProfileScope prof("adamw_unpack", s);
-    unpack_kernel<<<uint32_t(p->chunks.size()), kOptimThreads, 0, s>>>(
+    unpack_kernel<<<uint32_t(p->chunks.size()), kCodeThreads, 0, s>>>(
         reinterpret_cast<const TensorDev *>(t), reinterpret_cast<const ChunkDev *>(t + p->chunks_at()),
         static_cast<uint16_t *>(m_out), static_cast<uint16_t *>(v_out));
     return hip_ok(hipGetLastError());

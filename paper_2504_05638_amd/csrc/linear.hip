@@ -343,6 +343,80 @@ struct Product {
 __device__ inline uint32_t term_p(uint32_t t) { return (0x001102u >> (4 * t)) & 3; }
 __device__ inline uint32_t term_q(uint32_t t) { return (0x010120u >> (4 * t)) & 3; }
 
+// Which tile and which part of its sum a workgroup takes.  Workgroups go to the eight XCDs in turn.  Each XCD gets
+// neighbouring tiles, and goes through them in groups of eight rows of tiles, so that what its L2 holds is used again.
+struct Place {
+    uint32_t m0, n0, part;
+};
+template <uint32_t TM, uint32_t TN>
+__device__ inline Place place(const Product &a)
+{
+    const uint32_t tiles = a.tiles_m * a.tiles_n, part = blockIdx.x / tiles, b = blockIdx.x % tiles;
+    const uint32_t xcd = b % 8, extra = tiles % 8, at = xcd * (tiles / 8) + min(xcd, extra) + b / 8;
+    const uint32_t group = at / (8 * a.tiles_n), left = min(a.tiles_m - group * 8, 8u), in = at - group * 8 * a.tiles_n;
+    return Place{(group * 8 + in % left) * TM, in / left * TN, part};
+}
+
+// A wave's sums, rows from m0 and columns from n0 on, go through its own strip of local memory, 32 rows at a time, so that a
+// row's neighbours are written together.
+template <typename T, int RM, int RN>
+__device__ inline __attribute__((always_inline)) void write_out(const Product &a, const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0,
+                                                                uint32_t part)
+{
+    constexpr uint32_t kRow = RN * 16 + 4, across = RN * 2, rows = 64 / across, kLines = 32 / rows;
+    const uint32_t ln = lane % across * 8, n = n0 + ln, have = n < a.n ? min(8u, a.n - n) : 0;
+    const Result &res = a.result;
+    float bias[8] = {};
+    if (res.bias && have == 8) load_n<T, 8>(static_cast<const T *>(res.bias) + n, bias);
+#pragma unroll 1
+    for (int i = 0; i < RM; i += 2) {
+        // (one copy of what follows for all strips; registers are not found by a number at run time)
+#pragma unroll
+        for (int at = 0; at < RM; at += 2)
+            if (at == i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < RN; ++j)
+                        *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[at + h][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const uint32_t m = m0 + i * 16 + lane / across;
+        Lane<T, 8> added[kLines];
+        if (res.added && a.splits == 1 && have == 8)
+#pragma unroll
+            for (uint32_t l = 0; l < kLines; ++l)
+                if (m + l * rows < a.m) added[l].load(static_cast<const T *>(res.added) + (m + l * rows) * res.lda + n);
+#pragma unroll
+        for (uint32_t l = 0; l < kLines; ++l) {
+            if (m + l * rows >= a.m || !have) continue;
+            float z[8];
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(strip + (l * rows + lane / across) * kRow + ln + h);
+                z[h] = v.x;
+                z[h + 1] = v.y;
+                z[h + 2] = v.z;
+                z[h + 3] = v.w;
+            }
+            if (a.splits != 1) {
+                float *to = a.partial + (uint64_t(part) * a.m + m + l * rows) * a.n + n;
+                if (have == 8) {
+                    store_n<float, 8>(to, z);
+                } else {
+#pragma unroll
+                    for (uint32_t h = 0; h < 8; ++h)
+                        if (h < have) to[h] = z[h];
+                }
+            } else if (have == 8) {
+                finish<T>(res, m + l * rows, n, bias, added[l], z);
+            } else {
+                finish<T>(res, m + l * rows, n, have, z);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
 // One operand of a workgroup's tile: how its slabs get into local memory, 16 bytes a lane, and from there into the matrix
 // instruction's registers (lane l holds row l % 16, k's 8 (l / 16) to 8 (l / 16) + 7).  R rows, kSlab k's.  The
 // loads go through a buffer descriptor that ends where the operand ends: what lies behind comes as zeros.
@@ -363,10 +437,9 @@ struct Walk {
         p += on ? step : 0;
         left -= on ? step : 0;
     }
-    // the slab of one of a float32's three parts, `part` elements further on
-    __device__ inline __amdgpu_buffer_rsrc_t described(uint32_t part) const
+    __device__ inline __amdgpu_buffer_rsrc_t described() const
     {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p) + part, 0, left < kMostBytes / 2 ? uint32_t(left) * 2 : kMostBytes, 0x00020000);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, left < kMostBytes / 2 ? uint32_t(left) * 2 : kMostBytes, 0x00020000);
     }
 };
 
@@ -445,11 +518,12 @@ struct Side<true, R, THREADS> {
         const uint32_t at = step * 32 + 8 * (lane >> 4) + ((lane >> 2) & 3), s = turn(at);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const char *from = stage + at * (R * 2) + (((tile + i) ^ s) << 5) + ((lane & 3) << 3);
+            // (one sum: the compiler loses sight of which stage is read behind a few steps of a pointer, and would wait for loads)
+            const uint32_t from = at * (R * 2) + (((tile + i) ^ s) << 5) + ((lane & 3) << 3);
             s4 half[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h)  // (four k's further on the turn is the same)
-                half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(from + h * 4 * (R * 2)));
+                half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(stage + (from + h * 4 * (R * 2))));
             to[i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
@@ -469,11 +543,10 @@ struct Side<true, R, THREADS> {
 // found 1113, woven with the reads 1196; 32 x 32 x 16 instructions, which move their sums twice as often, 1196, 16 x 16 x 32 1236;
 // four waves of 128 by 128 1163; eight waves in two groups that take turns at reading and multiplying 1041; slabs
 // of 32 in a ring of four stages, whose loads take half a cache line, 1172.
-template <typename T, int WM, int WN, int RM, int RN, bool PT, bool QT>
+template <int WM, int WN, int RM, int RN, bool PT, bool QT>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
 {
     constexpr uint32_t kThreads = WM * WN * 64, TM = WM * RM * 16, TN = WN * RN * 16;
-    constexpr uint32_t terms = sizeof(T) == 2 ? 1 : 6;
     constexpr uint32_t kStage = (TM + TN) * kSlab * 2;
     constexpr int kLoads = int((TM + TN) * 8 / kThreads);
     constexpr uint32_t kRow = RN * 16 + 4;  // floats of a row of a wave's strip
@@ -482,34 +555,25 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     __shared__ __attribute__((aligned(1024))) char stage1[kStage];
     const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave % WM, wn = wave / WM;
-    uint32_t b = blockIdx.x;
-    const uint32_t tiles = a.tiles_m * a.tiles_n, part = b / tiles;
-    b %= tiles;
-    // Workgroups go to the eight XCDs in turn.  Each XCD gets neighbouring tiles, and goes through them in groups of
-    // eight rows of tiles, so that what its L2 holds is used again.
-    const uint32_t xcd = b % 8, extra = tiles % 8;
-    b = xcd * (tiles / 8) + min(xcd, extra) + b / 8;
-    const uint32_t group = b / (8 * a.tiles_n), left = min(a.tiles_m - group * 8, 8u), in = b - group * 8 * a.tiles_n;
-    const uint32_t m0 = (group * 8 + in % left) * TM, n0 = in / left * TN;
+    const Place at = place<TM, TN>(a);
+    const uint32_t m0 = at.m0, n0 = at.n0;
 
     const Side<PT, TM, kThreads> side_p(m0, a.ldp);
     const Side<QT, TN, kThreads> side_q(n0, a.ldq);
 
-    const uint32_t first = part * a.slabs, all = (a.k + kSlab - 1) / kSlab * terms;
-    const uint32_t count = min(a.slabs, all - first);
+    const uint32_t first = at.part * a.slabs, count = min(a.slabs, (a.k + kSlab - 1) / kSlab - first);
 
     // The next slab to fetch, found before the waves meet.  Behind the last one it is the last one again.
     struct Aim {
         __amdgpu_buffer_rsrc_t p, q;
         uint32_t k0;
     };
-    uint32_t k0 = first / terms * kSlab, term = first % terms, to_come = count;
+    uint32_t k0 = first * kSlab, to_come = count;
     Walk walk_p = side_p.walk(a.p, m0, a.m, k0, a.k, a.ldp), walk_q = side_q.walk(a.q, n0, a.n, k0, a.k, a.ldq);
     auto aim = [&]() __attribute__((always_inline)) {
-        const Aim at{walk_p.described(terms > 1 ? term_p(term) * a.part_p : 0), walk_q.described(terms > 1 ? term_q(term) * a.part_q : 0), k0};
-        const bool more = to_come > 1, on = more && term + 1 == terms;
-        to_come -= more;
-        term = on ? 0 : term + more;
+        const Aim at{walk_p.described(), walk_q.described(), k0};
+        const bool on = to_come > 1;
+        to_come -= on;
         k0 += on ? kSlab : 0;
         walk_p.advance(on);
         walk_q.advance(on);
@@ -577,7 +641,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
         read_p(next, 0, 0);
         fetch(at, now);
         multiply(1, 1);
-        // (A transposing read behind a load would wait for it: there the reads go first.)
+        // (of turned operands, whose reads are more, the reads go first; woven with the loads they take the same time)
 #pragma unroll
         for (int i = 0; i < H * RN; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -596,75 +660,170 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     arrived();
     read_q(stage0, 0);
     read_p(stage0, 0, 0);
-    // (said of the pointers, this keeps the compiler from having a transposing read wait for loads into the other stage; plain reads
-    // it knows better without)
-    auto slab_apart = [&](char *__restrict now, const char *__restrict next) __attribute__((always_inline)) { slab(now, next); };
     for (uint32_t s = 0; s < count; s += 2) {
-        if constexpr (PT || QT) slab_apart(stage0, stage1);
-        else slab(stage0, stage1);
-        if (s + 1 < count) {
-            if constexpr (PT || QT) slab_apart(stage1, stage0);
-            else slab(stage1, stage0);
-        }
+        slab(stage0, stage1);
+        if (s + 1 < count) slab(stage1, stage0);
     }
     arrived();
 
-    // Results go through the wave's own strip of local memory, 32 rows at a time, so that a row's neighbours
-    // are written together.
     float *strip = reinterpret_cast<float *>(wave * 32 * kRow * 4 + 32 * kRow * 4 <= kStage ? stage0 + wave * 32 * kRow * 4
                                                                                             : stage1 + (wave - kStage / (32 * kRow * 4)) * 32 * kRow * 4);
-    constexpr uint32_t across = RN * 2, rows = 64 / across, kLines = 32 / rows;
-    const uint32_t ln = lane % across * 8, n = n0 + wn * RN * 16 + ln, have = n < a.n ? min(8u, a.n - n) : 0;
-    const Result &res = a.result;
-    float bias[8] = {};
-    if (res.bias && have == 8) load_n<T, 8>(static_cast<const T *>(res.bias) + n, bias);
-#pragma unroll 1
-    for (int i = 0; i < RM; i += 2) {
-        // (one copy of what follows for all strips; registers are not found by a number at run time)
-#pragma unroll
-        for (int at = 0; at < RM; at += 2)
-            if (at == i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < RN; ++j)
-                        *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[at + h][j];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const uint32_t m = m0 + (wm * RM + i) * 16 + lane / across;
-        Lane<T, 8> added[kLines];
-        if (res.added && a.splits == 1 && have == 8)
-#pragma unroll
-            for (uint32_t l = 0; l < kLines; ++l)
-                if (m + l * rows < a.m) added[l].load(static_cast<const T *>(res.added) + (m + l * rows) * res.lda + n);
-#pragma unroll
-        for (uint32_t l = 0; l < kLines; ++l) {
-            if (m + l * rows >= a.m || !have) continue;
-            float z[8];
-#pragma unroll
-            for (int h = 0; h < 8; h += 4) {
-                const float4 v = *reinterpret_cast<const float4 *>(strip + (l * rows + lane / across) * kRow + ln + h);
-                z[h] = v.x;
-                z[h + 1] = v.y;
-                z[h + 2] = v.z;
-                z[h + 3] = v.w;
-            }
-            if (a.splits != 1) {
-                float *to = a.partial + (uint64_t(part) * a.m + m + l * rows) * a.n + n;
-                if (have == 8) {
-                    store_n<float, 8>(to, z);
-                } else {
-#pragma unroll
-                    for (uint32_t h = 0; h < 8; ++h)
-                        if (h < have) to[h] = z[h];
-                }
-            } else if (have == 8) {
-                finish<T>(res, m + l * rows, n, bias, added[l], z);
-            } else {
-                finish<T>(res, m + l * rows, n, have, z);
-            }
+    write_out<uint16_t, RM, RN>(a, acc, strip, lane, m0 + wm * RM * 16, n0 + wn * RN * 16, at.part);
+}
+
+// One operand of the float32 product's tile, taken apart: slabs of 32 k's of all three parts, R rows, a load of 16
+// bytes to a thread for each part.  As Side otherwise, but that rows are 64 bytes of k's and that every k that a slab
+// has is there, if only as a zero.
+constexpr uint32_t kSlab3 = 32;
+template <bool TURNED, uint32_t R>
+struct Side3 {
+    static constexpr uint32_t kThreads = R * 4;  // (32 k's of R rows, in pieces of 8)
+    uint32_t off[kParts], lane;
+    __device__ static inline uint32_t turn(uint32_t k) { return Side<true, R, kThreads>::turn(k); }
+    __device__ inline Side3(uint32_t r0, uint64_t ld, uint32_t part)
+    {
+        lane = threadIdx.x & 63;
+        uint32_t at;
+        if constexpr (TURNED) {
+            const uint32_t k = threadIdx.x / (R / 8);
+            at = k * uint32_t(ld * 2) + (r0 + (threadIdx.x % (R / 8) ^ (2 * turn(k))) * 8) * 2;
+        } else {
+            const uint32_t row = threadIdx.x >> 2;
+            at = row * uint32_t(ld * 2) + ((threadIdx.x & 3) ^ ((row >> 2) & 3)) * 16;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (uint32_t q = 0; q < kParts; ++q) off[q] = at + q * part * 2;
     }
+    __device__ static inline Walk walk(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
+    {
+        if constexpr (TURNED) return Walk{p + k0 * ld, (end - k0) * ld, uint32_t(ld) * kSlab3};
+        else return Walk{p + r0 * ld + k0, (rows - r0) * ld - k0, kSlab3};
+    }
+    __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, char *stage, uint32_t wave) const
+    {
+#pragma unroll
+        for (uint32_t q = 0; q < kParts; ++q) load_lds(from, off[q], stage + q * R * 64 + wave * 1024);
+    }
+    template <int N>
+    __device__ inline void read(const char *stage, uint32_t tile, bf16x8 (&to)[kParts][N]) const
+    {
+        if constexpr (TURNED) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            const uint32_t at = 8 * (lane >> 4) + ((lane >> 2) & 3), s = turn(at);
+#pragma unroll
+            for (uint32_t q = 0; q < kParts; ++q)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const uint32_t from = q * R * 64 + at * (R * 2) + (((tile + i) ^ s) << 5) + ((lane & 3) << 3);
+                    s4 half[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(stage + (from + h * 4 * (R * 2))));
+                    to[q][i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+        } else {
+            const uint32_t row = lane & 15;
+#pragma unroll
+            for (uint32_t q = 0; q < kParts; ++q)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    to[q][i] = *reinterpret_cast<const bf16x8 *>(stage + q * R * 64 + ((tile + i) * 16 + row) * 64 + (((lane >> 4) ^ (row >> 2)) << 4));
+        }
+    }
+};
+
+// The product of operands taken apart: 128 by 128 to a workgroup of two by four waves, 64 by 32 to a wave.  All six products
+// of parts are taken from one fetch and one read of the three: the next slab's pieces are read while this one's 48
+// products run, from three stages, two of which are on their way while the third is multiplied.
+//
+// Bound by the matrix units and their power at large sizes (4096 by 4096 by 4096: 677 us, 203
+// TFLOP/s, 1220 of bfloat16 products).  A bfloat16
+// product of six times as many k's, tile of 256 by 256, fetches and reads each part two or three times: 616 us there, but 70
+// instead of 56 at 1024 by 4096 by 1024, 146 instead of 114 for both gradients at 1024 by 1024 by 4096, and 755 instead of 665 for
+// those at 8192 by 1024 by 4096.
+template <bool PT, bool QT>
+__global__ __launch_bounds__(512, 2) void product3_kernel(Product a)
+{
+    constexpr int RM = 4, RN = 2;
+    constexpr uint32_t T = 128, kStage = 2 * T * kParts * 64, kRow = RN * 16 + 4;
+    constexpr int kLoads = 2 * kParts, kReads = kParts * (RM * (PT ? 2 : 1) + RN * (QT ? 2 : 1));
+    static_assert(8 * 32 * kRow * 4 <= kStage, "the strips fit");
+    __shared__ __attribute__((aligned(1024))) char stage0[kStage];
+    __shared__ __attribute__((aligned(1024))) char stage1[kStage];
+    __shared__ __attribute__((aligned(1024))) char stage2[kStage];
+    const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wm = wave & 1, wn = wave >> 1;
+    const Place at = place<T, T>(a);
+    const Side3<PT, T> side_p(at.m0, a.ldp, a.part_p);
+    const Side3<QT, T> side_q(at.n0, a.ldq, a.part_q);
+    const uint32_t first = at.part * a.slabs, count = min(a.slabs, (a.k + kSlab3 - 1) / kSlab3 - first);
+    uint32_t to_come = count;
+    Walk walk_p = side_p.walk(a.p, at.m0, a.m, first * kSlab3, a.k, a.ldp), walk_q = side_q.walk(a.q, at.n0, a.n, first * kSlab3, a.k, a.ldq);
+    // (behind the last slab the last one again, which nobody uses)
+    auto fetch = [&](char *stage) __attribute__((always_inline)) {
+        side_p.fetch(walk_p.described(), stage, wave);
+        side_q.fetch(walk_q.described(), stage + T * kParts * 64, wave);
+        const bool on = to_come > 1;
+        to_come -= on;
+        walk_p.advance(on);
+        walk_q.advance(on);
+    };
+    f32x4 acc[RM][RN] = {};
+    bf16x8 fp[2][kParts][RM], fq[2][kParts][RN];
+    auto read = [&](const char *stage, int to) __attribute__((always_inline)) {
+        side_q.template read<RN>(stage + T * kParts * 64, wn * RN, fq[to]);
+        side_p.template read<RM>(stage, wm * RM, fp[to]);
+    };
+    // All that this wave has read, and what it has asked for but for `slabs` slabs; then the same for the others.
+    auto meet = [&](auto slabs) __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070 | decltype(slabs)::value * kLoads);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // A slab, whose pieces are in registers: its stage, `now`, is free.
+    auto slab = [&](int from, char *now, const char *next) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(0);
+        meet(std::integral_constant<int, 1>());
+        __builtin_amdgcn_s_setprio(1);
+        read(next, from ^ 1);
+        fetch(now);
+#pragma unroll
+        for (uint32_t t = 0; t < 6; ++t)
+#pragma unroll
+            for (int i = 0; i < RM; ++i)
+#pragma unroll
+                for (int j = 0; j < RN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fq[from][term_q(t)][j], fp[from][term_p(t)][i], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 48; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            else if (i < kReads + kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+    };
+    fetch(stage0);
+    fetch(stage1);
+    fetch(stage2);
+    meet(std::integral_constant<int, 2>());
+    read(stage0, 0);
+    // (a way round a slab inside the loop would have the compiler expect any stage to be the newest one, and wait)
+    uint32_t left = count;
+    for (; left >= 6; left -= 6) {
+        slab(0, stage0, stage1);
+        slab(1, stage1, stage2);
+        slab(0, stage2, stage0);
+        slab(1, stage0, stage1);
+        slab(0, stage1, stage2);
+        slab(1, stage2, stage0);
+    }
+    if (left > 0) slab(0, stage0, stage1);
+    if (left > 1) slab(1, stage1, stage2);
+    if (left > 2) slab(0, stage2, stage0);
+    if (left > 3) slab(1, stage0, stage1);
+    if (left > 4) slab(0, stage1, stage2);
+    meet(std::integral_constant<int, 0>());
+    write_out<float, RM, RN>(a, acc, reinterpret_cast<float *>(stage0) + wave * 32 * kRow, lane, at.m0 + wm * RM * 16, at.n0 + wn * RN * 16, at.part);
 }
 
 // The parts of a split sum, added up in their order; a sum without terms is no parts.
@@ -842,16 +1001,16 @@ struct Shape {
 
 // By what the candidates would take, in us, from measurements at sizes from 333 by 1001 by 832 to 8192 by 8192 by 8192 (within 15 %
 // of them): a slab of 256 by 256 takes a compute unit to itself for 1.68; two of 128 by 128 share one for 1.01, one
-// alone takes 0.70; parts of a sum cost a launch, and their bytes written and read.  (us, 256 by 256 / 128 by 128
+// alone takes 0.70, a slab of 32 float32 1.1; parts of a sum cost a launch, and their bytes written and read.  (us, 256 by 256 / 128 by 128
 // in one, two, four parts: 4096 cubed 107 / 124; 8192 by 2560 by 1024 64 / 53; 2048 by 2048 by 4096 81 / 45, 49; 1024 by 4096 by
 // 1024 31 / 16, 27; 1024 by 1024 by 4096 - / 47, 32, 25; 333 by 1001 by 832 - / 11, 14, 15.)
-Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t terms, bool turned_p)
+Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, bool turned_p)
 {
     Shape s{};
-    const uint64_t cus = uint64_t(device_cu_count()), slabs = up(k, kSlab) / kSlab * terms;
+    const uint64_t cus = uint64_t(device_cu_count()), slab = dtype == TAGC_F32 ? kSlab3 : kSlab, slabs = up(k, slab) / slab;
     if (!slabs) return s;
     uint64_t splits = 1;
-    if (!turned_p && m <= 64) {
+    if (dtype == TAGC_BF16 && !turned_p && m <= 64) {
         // thin tiles: the weights' bytes count, and many workgroups to ask for them
         s.rows = m <= 32 ? 32 : 64;
         s.tiles_m = 1;
@@ -862,11 +1021,14 @@ Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t terms, bool turned_p
     } else {
         double best = 0;
         for (const uint32_t t : {256u, 128u}) {
+            if (t == 256 && dtype == TAGC_F32) continue;
             const uint64_t tm = (m + t - 1) / t, tn = (n + t - 1) / t, tiles = tm * tn;
             for (uint64_t parts = 1; parts <= 16 && parts <= slabs; ++parts) {
                 const uint64_t each = (slabs + parts - 1) / parts, groups = tiles * parts;
                 double rounds;
-                if (t == 256) {
+                if (dtype == TAGC_F32) {
+                    rounds = 1.1 * double((groups + cus - 1) / cus);
+                } else if (t == 256) {
                     rounds = 1.68 * double((groups + cus - 1) / cus);
                 } else {
                     const uint64_t rest = groups % (2 * cus);
@@ -975,7 +1137,7 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     a.m = uint32_t(m);
     a.n = uint32_t(n);
     a.k = uint32_t(k);
-    const Shape f = shape_of(m, n, k, sizeof(T) == 4 ? 6 : 1, PT);
+    const Shape f = shape_of(m, n, k, sizeof(T) == 4 ? TAGC_F32 : TAGC_BF16, PT);
     a.tiles_m = f.tiles_m;
     a.tiles_n = f.tiles_n;
     a.slabs = f.slabs;
@@ -985,11 +1147,15 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     const uint32_t grid = f.tiles_m * f.tiles_n * f.splits;
     if (grid) {
         ProfileScope prof("linear_product", s);
-        if (f.rows == 256) product_kernel<T, 2, 4, 8, 4, PT, QT><<<grid, 512, 0, s>>>(a);
-        else if (f.rows == 128) product_kernel<T, 2, 4, 4, 2, PT, QT><<<grid, 512, 0, s>>>(a);
-        else if constexpr (!PT) {
-            if (f.rows == 64) product_kernel<T, 1, 4, 4, 2, PT, QT><<<grid, 256, 0, s>>>(a);
-            else product_kernel<T, 1, 4, 2, 2, PT, QT><<<grid, 256, 0, s>>>(a);
+        if constexpr (sizeof(T) == 4) {
+            product3_kernel<PT, QT><<<grid, 512, 0, s>>>(a);
+        } else {
+            if (f.rows == 256) product_kernel<2, 4, 8, 4, PT, QT><<<grid, 512, 0, s>>>(a);
+            else if (f.rows == 128) product_kernel<2, 4, 4, 2, PT, QT><<<grid, 512, 0, s>>>(a);
+            else if constexpr (!PT) {
+                if (f.rows == 64) product_kernel<1, 4, 4, 2, PT, QT><<<grid, 256, 0, s>>>(a);
+                else product_kernel<1, 4, 2, 2, PT, QT><<<grid, 256, 0, s>>>(a);
+            }
         }
     }
     if (f.splits != 1) {
@@ -1002,7 +1168,7 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
 // elements of the partial sums of a product
 uint64_t partial_elems(uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, bool turned_p)
 {
-    const Shape f = shape_of(m, n, k, dtype == TAGC_F32 ? 6 : 1, turned_p);
+    const Shape f = shape_of(m, n, k, dtype, turned_p);
     return f.splits > 1 ? f.splits * m * n : 0;
 }
 

@@ -24,13 +24,14 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kSlab = 64;        // k's of a stage in local memory: 128 bytes of a row
 constexpr uint32_t kPackRows = 64;
 constexpr uint32_t kParts = 3;        // bfloat16 numbers that a float32 is taken apart into
-// rows up to which few_kernel goes: in bfloat16 a thin tile is faster from 17 rows on (weights of 4096 by 11008, 17, 32, 64
-// rows: 32, 35, 48 us, 23, 24, 26 as tiles), in float32 the weights would have to be taken apart first (83, 86, 129 us; 164, 162, 167)
-constexpr uint32_t kFewRows[2] = {64, 16};  // TAGC_F32, TAGC_BF16
+// rows up to which few_kernel goes; from there on tiles are faster (weights of 4096 by 11008, 17, 32, 64 rows, us: bfloat16
+// 32, 35, 48, as tiles 23, 24, 26; float32 76, 95, 164, as tiles 80, 80, 84)
+constexpr uint32_t kFewRows = 16;
 
 constexpr uint64_t kMaxSide = 1u << 22;  // rows, features (in float32 a quarter) and strides as they lie are fewer
 
@@ -178,23 +179,14 @@ struct PackJobs {
     uint32_t first[3];    // workgroup of each (one that there is not begins behind the last)
 };
 
-// The bfloat16 numbers that a packed value goes to: itself rounded, or three that add up to it: cut off behind 8 bits (what is
-// finite stays finite), the rest rounded to 8 bits, and what is then left, which has no more than 8.
-// (Of an infinity the second is NaN.)
-template <typename T>
-__device__ inline void split(float x, uint16_t (&out)[sizeof(T) == 2 ? 1 : 3])
+// The three bfloat16 numbers, in the upper halves, that add up to a float32: it cut off behind 8 bits (what is finite stays finite),
+// the rest rounded to 8 bits, and what is then left, which has no more than 8.  (Of an infinity the second is NaN.)
+__device__ inline void split(float x, uint32_t (&out)[kParts])
 {
-    if constexpr (sizeof(T) == 2) {
-        out[0] = uint16_t(round_to_bf16(x));
-    } else {
-        const uint32_t b = __float_as_uint(x);
-        const float y = x - __uint_as_float(b & 0xFFFF0000u);
-        const uint32_t c = __float_as_uint(y) + 0x8000u;
-        const float w = y - __uint_as_float(c & 0xFFFF0000u);
-        out[0] = uint16_t(b >> 16);
-        out[1] = uint16_t(c >> 16);
-        out[2] = uint16_t(__float_as_uint(w) >> 16);
-    }
+    out[0] = __float_as_uint(x);
+    const float y = x - __uint_as_float(out[0] & 0xFFFF0000u);
+    out[1] = __float_as_uint(y) + 0x8000u;
+    out[2] = __float_as_uint(y - __uint_as_float(out[1] & 0xFFFF0000u));
 }
 
 // A workgroup takes a tile of kPackRows by 64, a thread four neighbours of each sixteenth row.
@@ -241,10 +233,14 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJobs jobs)
             u16x4 out[planes];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                uint16_t s[planes];
-                split<T>(x[i][j], s);
+                if constexpr (planes == 1) {
+                    out[0][j] = narrow<T>(x[i][j]);
+                } else {
+                    uint32_t s[kParts];
+                    split(x[i][j], s);
 #pragma unroll
-                for (int q = 0; q < planes; ++q) out[q][j] = s[q];
+                    for (int q = 0; q < planes; ++q) out[q][j] = uint16_t(s[q] >> 16);
+                }
             }
 #pragma unroll
             for (int q = 0; q < planes; ++q) *reinterpret_cast<u16x4 *>(a.to + r * a.to_ld + q * a.to_part + c) = out[q];
@@ -328,12 +324,12 @@ __device__ inline void finish(const Result &r, uint32_t m, uint32_t n, uint32_t 
 // ------------------------------------------------------------------ the product
 
 struct Product {
-    const uint16_t *p, *q;          // bfloat16, [m, k] and [n, k], or turned [k, m] and [k, n]; 4-byte aligned
-    uint64_t ldp, ldq;              // multiples of 2; k a multiple of 8 where rows lie row by row
-    uint32_t part_p, part_q;        // float32: elements from one of the three parts of a row to the next
+    const void *p, *q;              // [m, k] and [n, k], or turned [k, m] and [k, n]: bfloat16, float32 taken apart, or float32 as it lies
+    uint64_t ldp, ldq;              // bfloat16: multiples of 2; k a multiple of 8 where rows lie row by row
+    uint32_t part_p, part_q;        // taken apart: elements from one of the three parts of a row to the next
     uint32_t m, n, k;
     uint32_t tiles_m, tiles_n;
-    uint32_t slabs;                 // slabs of one part of the sum, in all terms
+    uint32_t slabs;                 // slabs of one part of the sum
     uint32_t splits;                // parts of the sum; 1: finished here
     float *partial;                 // [splits][m][n]
     Result result;
@@ -426,10 +422,10 @@ struct Side;
 constexpr uint32_t kMostBytes = 1u << 31;  // of a descriptor, and ...
 constexpr uint32_t kNowhere = 3u << 30;    // ... an offset behind every one; what a tile reads has smaller offsets
 
-
 // Where an operand's next slab begins, and how many elements there are from there to the operand's end.
+template <typename T>
 struct Walk {
-    const uint16_t *p;
+    const T *p;
     uint64_t left;
     uint32_t step;  // elements from one slab to the next
     __device__ inline void advance(bool on)
@@ -439,7 +435,7 @@ struct Walk {
     }
     __device__ inline __amdgpu_buffer_rsrc_t described() const
     {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0, left < kMostBytes / 2 ? uint32_t(left) * 2 : kMostBytes, 0x00020000);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(p), 0, left < kMostBytes / sizeof(T) ? uint32_t(left) * uint32_t(sizeof(T)) : kMostBytes, 0x00020000);
     }
 };
 
@@ -463,9 +459,10 @@ struct Side<false, R, THREADS> {
         for (uint32_t i = 0; i < kLoads; ++i) off[i] = (sub + i * (THREADS / 8)) * uint32_t(ld * 2) + piece * 16;
     }
     // the operand from row r0 and k0 on (of a row whose k's are no multiple of eight there are zeros up to one)
-    __device__ static inline Walk walk(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
+    __device__ static inline Walk<uint16_t> walk(const void *base, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
     {
-        return Walk{p + r0 * ld + k0, (rows - r0 - 1) * ld + ((end + 7) & ~7u) - k0, kSlab};
+        const uint16_t *p = static_cast<const uint16_t *>(base);
+        return Walk<uint16_t>{p + r0 * ld + k0, (rows - r0 - 1) * ld + ((end + 7) & ~7u) - k0, kSlab};
     }
     __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, uint32_t k0, uint32_t end, char *stage, uint32_t wave) const
     {
@@ -502,9 +499,10 @@ struct Side<true, R, THREADS> {
             off[i] = (k + i * kDown) * uint32_t(ld * 2) + (r0 + (threadIdx.x % kAcross ^ (2 * turn(k + i * kDown))) * 8) * 2;
     }
     // the operand from k0 on (a descriptor ends with a word: of an odd number of rows there is one more)
-    __device__ static inline Walk walk(const uint16_t *p, uint32_t, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
+    __device__ static inline Walk<uint16_t> walk(const void *base, uint32_t, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
     {
-        return Walk{p + k0 * ld, (end - k0 - 1) * ld + ((rows + 1) & ~1u), uint32_t(ld) * kSlab};
+        const uint16_t *p = static_cast<const uint16_t *>(base);
+        return Walk<uint16_t>{p + k0 * ld, (end - k0 - 1) * ld + ((rows + 1) & ~1u), uint32_t(ld) * kSlab};
     }
     __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, uint32_t, uint32_t, char *stage, uint32_t wave) const
     {
@@ -569,7 +567,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
         uint32_t k0;
     };
     uint32_t k0 = first * kSlab, to_come = count;
-    Walk walk_p = side_p.walk(a.p, m0, a.m, k0, a.k, a.ldp), walk_q = side_q.walk(a.q, n0, a.n, k0, a.k, a.ldq);
+    Walk<uint16_t> walk_p = side_p.walk(a.p, m0, a.m, k0, a.k, a.ldp), walk_q = side_q.walk(a.q, n0, a.n, k0, a.k, a.ldq);
     auto aim = [&]() __attribute__((always_inline)) {
         const Aim at{walk_p.described(), walk_q.described(), k0};
         const bool on = to_come > 1;
@@ -694,10 +692,11 @@ struct Side3 {
 #pragma unroll
         for (uint32_t q = 0; q < kParts; ++q) off[q] = at + q * part * 2;
     }
-    __device__ static inline Walk walk(const uint16_t *p, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
+    __device__ static inline Walk<uint16_t> walk(const void *base, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
     {
-        if constexpr (TURNED) return Walk{p + k0 * ld, (end - k0) * ld, uint32_t(ld) * kSlab3};
-        else return Walk{p + r0 * ld + k0, (rows - r0) * ld - k0, kSlab3};
+        const uint16_t *p = static_cast<const uint16_t *>(base);
+        if constexpr (TURNED) return Walk<uint16_t>{p + k0 * ld, (end - k0) * ld, uint32_t(ld) * kSlab3};
+        else return Walk<uint16_t>{p + r0 * ld + k0, (rows - r0) * ld - k0, kSlab3};
     }
     __device__ inline void fetch(__amdgpu_buffer_rsrc_t from, char *stage, uint32_t wave) const
     {
@@ -732,6 +731,17 @@ struct Side3 {
     }
 };
 
+template <int RM, int RN>
+__device__ inline __attribute__((always_inline)) void six_products(f32x4 (&acc)[RM][RN], const bf16x8 (&p)[kParts][RM], const bf16x8 (&q)[kParts][RN])
+{
+#pragma unroll
+    for (uint32_t t = 0; t < 6; ++t)
+#pragma unroll
+        for (int i = 0; i < RM; ++i)
+#pragma unroll
+            for (int j = 0; j < RN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[term_q(t)][j], p[term_p(t)][i], acc[i][j], 0, 0, 0);
+}
+
 // The product of operands taken apart: 128 by 128 to a workgroup of two by four waves, 64 by 32 to a wave.  All six products
 // of parts are taken from one fetch and one read of the three: the next slab's pieces are read while this one's 48
 // products run, from three stages, two of which are on their way while the third is multiplied.
@@ -758,7 +768,7 @@ __global__ __launch_bounds__(512, 2) void product3_kernel(Product a)
     const Side3<QT, T> side_q(at.n0, a.ldq, a.part_q);
     const uint32_t first = at.part * a.slabs, count = min(a.slabs, (a.k + kSlab3 - 1) / kSlab3 - first);
     uint32_t to_come = count;
-    Walk walk_p = side_p.walk(a.p, at.m0, a.m, first * kSlab3, a.k, a.ldp), walk_q = side_q.walk(a.q, at.n0, a.n, first * kSlab3, a.k, a.ldq);
+    Walk<uint16_t> walk_p = side_p.walk(a.p, at.m0, a.m, first * kSlab3, a.k, a.ldp), walk_q = side_q.walk(a.q, at.n0, a.n, first * kSlab3, a.k, a.ldq);
     // (behind the last slab the last one again, which nobody uses)
     auto fetch = [&](char *stage) __attribute__((always_inline)) {
         side_p.fetch(walk_p.described(), stage, wave);
@@ -788,13 +798,7 @@ __global__ __launch_bounds__(512, 2) void product3_kernel(Product a)
         __builtin_amdgcn_s_setprio(1);
         read(next, from ^ 1);
         fetch(now);
-#pragma unroll
-        for (uint32_t t = 0; t < 6; ++t)
-#pragma unroll
-            for (int i = 0; i < RM; ++i)
-#pragma unroll
-                for (int j = 0; j < RN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fq[from][term_q(t)][j], fp[from][term_p(t)][i], acc[i][j], 0, 0, 0);
+        six_products(acc, fp[from], fq[from]);
 #pragma unroll
         for (int i = 0; i < 48; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -823,6 +827,143 @@ __global__ __launch_bounds__(512, 2) void product3_kernel(Product a)
     if (left > 3) slab(1, stage0, stage1);
     if (left > 4) slab(0, stage1, stage2);
     meet(std::integral_constant<int, 0>());
+    write_out<float, RM, RN>(a, acc, reinterpret_cast<float *>(stage0) + wave * 32 * kRow, lane, at.m0 + wm * RM * 16, at.n0 + wn * RN * 16, at.part);
+}
+
+// A float32 operand as it lies, row by row: a thread's eight k's of a row are taken apart on the way into local memory, to where
+// Side3 has them.
+template <uint32_t R>
+struct Raw3 {
+    uint32_t off, k;
+    __device__ inline explicit Raw3(uint64_t ld)
+    {
+        const uint32_t row = threadIdx.x >> 2;
+        k = ((threadIdx.x & 3) ^ ((row >> 2) & 3)) * 8;
+        off = row * uint32_t(ld * 4) + k * 4;
+    }
+    __device__ static inline Walk<float> walk(const void *base, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t end, uint64_t ld)
+    {
+        return Walk<float>{static_cast<const float *>(base) + r0 * ld + k0, (rows - r0 - 1) * ld + end - k0, kSlab3};
+    }
+    struct Piece {
+        u32x4 x[2];
+    };
+    __device__ inline Piece load(__amdgpu_buffer_rsrc_t from) const
+    {
+        Piece r;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) r.x[h] = __builtin_amdgcn_raw_buffer_load_b128(from, off + h * 16, 0, 0);
+        return r;
+    }
+    // of a slab with `have` k's (behind a row's last one lies the next row)
+    __device__ inline void cut(Piece &r, uint32_t have) const
+    {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (k + j >= have) r.x[j / 4][j % 4] = 0;
+    }
+    __device__ inline void put(const Piece &r, char *stage) const
+    {
+        u32x4 to[kParts];
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            uint32_t s[2][kParts];
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) split(__uint_as_float(r.x[j / 2][j % 2 * 2 + h]), s[h]);
+#pragma unroll
+            for (uint32_t q = 0; q < kParts; ++q) to[q][j] = __builtin_amdgcn_perm(s[1][q], s[0][q], 0x07060302);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kParts; ++q) *reinterpret_cast<u32x4 *>(stage + (q * R * 64 + threadIdx.x * 16)) = to[q];
+    }
+};
+
+// The same product of operands as they lie: while a slab's 48 products run, the next one's pieces are read from one stage, the one
+// after that is taken apart into the other, and two more are on their way to registers.
+//
+// It saves the launch and the bytes of laying out, but takes an operand apart once for each tile that reads it, and
+// the vector unit's instructions cost the matrix units a sixth of their rate: taken where operands are many bytes for their
+// products (raw_pays).  (us, as they lie / laid out: 333 by 1001 by 777 19 / 26, 1024 by 1024 by 1024 25 / 32, 512 by 4096 by 4096
+// 100 / 124, 8192 by 1024 by 4096 356 / 382, 2048 by 2048 by 4096 178 / 185; 8192 by 4096 by 1024 388 / 371, 4096 cubed 717 / 677.  Of
+// turned operands, whose laying out dx and dw share, both gradients at 8192 by 1024 by 4096 took 722 / 666.)
+__global__ __launch_bounds__(512, 2) void raw3_kernel(Product a)
+{
+    constexpr int RM = 4, RN = 2;
+    constexpr uint32_t T = 128, kStage = 2 * T * kParts * 64, kRow = RN * 16 + 4;
+    constexpr int kReads = kParts * (RM + RN);
+    static_assert(8 * 32 * kRow * 4 <= kStage, "the strips fit");
+    __shared__ __attribute__((aligned(1024))) char stage0[kStage];
+    __shared__ __attribute__((aligned(1024))) char stage1[kStage];
+    const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wm = wave & 1, wn = wave >> 1;
+    const Place at = place<T, T>(a);
+    const Raw3<T> side_p(a.ldp), side_q(a.ldq);
+    const Side3<false, T> parts(0, 0, 0);
+    const uint32_t first = at.part * a.slabs, count = min(a.slabs, (a.k + kSlab3 - 1) / kSlab3 - first), last = first + count - 1;
+    // The last slab, which alone may have fewer k's, goes first; `load` asks for the others (behind the last of them for that one
+    // again, which nobody uses).
+    uint32_t to_come = count;
+    Walk<float> walk_p = side_p.walk(a.p, at.m0, a.m, first * kSlab3, a.k, a.ldp), walk_q = side_q.walk(a.q, at.n0, a.n, first * kSlab3, a.k, a.ldq);
+    Raw3<T>::Piece raw_p[2], raw_q[2];
+    auto load = [&](int to) __attribute__((always_inline)) {
+        raw_p[to] = side_p.load(walk_p.described());
+        raw_q[to] = side_q.load(walk_q.described());
+        const bool on = to_come > 2;
+        to_come -= on;
+        walk_p.advance(on);
+        walk_q.advance(on);
+    };
+    auto put = [&](int from, char *stage) __attribute__((always_inline)) {
+        side_p.put(raw_p[from], stage);
+        side_q.put(raw_q[from], stage + T * kParts * 64);
+    };
+    f32x4 acc[RM][RN] = {};
+    bf16x8 fp[2][kParts][RM], fq[2][kParts][RN];
+    auto read = [&](const char *stage, int to) __attribute__((always_inline)) {
+        parts.template read<RN>(stage + T * kParts * 64, wn * RN, fq[to]);
+        parts.template read<RM>(stage, wm * RM, fp[to]);
+    };
+    // What this wave has read has come, and what it has written is there; then the same for the others.
+    auto meet = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
+    // A slab, whose pieces are in registers: its stage, `now`, is free.
+    auto slab = [&](int from, char *now, const char *next) __attribute__((always_inline)) {
+        meet();
+        read(next, from ^ 1);
+        put(from, now);
+        load(from);
+        six_products(acc, fp[from], fq[from]);
+#pragma unroll
+        for (int i = 0; i < 48; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (i < 42) __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            if ((i >= 20 && i < 23) || (i >= 42 && i < 45)) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            if (i >= 44) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+    };
+    const Walk<float> end_p = side_p.walk(a.p, at.m0, a.m, last * kSlab3, a.k, a.ldp), end_q = side_q.walk(a.q, at.n0, a.n, last * kSlab3, a.k, a.ldq);
+    raw_p[0] = side_p.load(end_p.described());
+    raw_q[0] = side_q.load(end_q.described());
+    load(1);
+    side_p.cut(raw_p[0], a.k - last * kSlab3);
+    side_q.cut(raw_q[0], a.k - last * kSlab3);
+    put(0, stage0);
+    load(0);
+    put(1, stage1);
+    load(1);
+    meet();
+    read(stage0, 0);
+    uint32_t left = count;
+    for (; left >= 2; left -= 2) {
+        slab(0, stage0, stage1);
+        slab(1, stage1, stage0);
+    }
+    if (left) slab(0, stage0, stage1);
+    meet();
     write_out<float, RM, RN>(a, acc, reinterpret_cast<float *>(stage0) + wave * 32 * kRow, lane, at.m0 + wm * RM * 16, at.n0 + wn * RN * 16, at.part);
 }
 
@@ -856,9 +997,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float *partial, uint32_
 // ------------------------------------------------------------------ few rows
 
 struct FewArgs {
-    const void *x, *w;      // x: as it lies, or (float32, over 16 rows) taken apart by pack_kernel
+    const void *x, *w;
     uint64_t ldx, ldw;
-    uint32_t part;          // elements from one of the three parts of a row of x to the next
     uint32_t rows, in, out;
     Result result;
 };
@@ -890,106 +1030,72 @@ struct Piece {
             if constexpr (sizeof(T) == 2) {
                 to[0][e] = __builtin_bit_cast(__bf16, x[8 * h + e]);
             } else {
-                uint16_t s[3];
-                split<T>(x[8 * h + e], s);
+                uint32_t s[kParts];
+                split(x[8 * h + e], s);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) to[q][e] = __builtin_bit_cast(__bf16, s[q]);
+                for (uint32_t q = 0; q < kParts; ++q) to[q][e] = __builtin_bit_cast(__bf16, uint16_t(s[q] >> 16));
             }
         }
     }
 };
 
-// Few rows: the weights are read once, straight into registers, in pieces of 64 k's of 16 features out; rows of x,
+// Up to kFewRows rows: the weights are read once, straight into registers, in pieces of 64 k's of 16 features out; rows of x,
 // which all workgroups read, come from the caches.  kFewWaves waves share the k's of 16 features out and add up their
 // sums in local memory.  The matrix instruction's k's may be in any order that both operands share: a lane takes 16
-// neighbours, so that four lanes read a whole cache line.  float32 weights are taken apart in registers, and so is x
-// up to 16 rows; of more, MT times 16, it was taken apart before.
+// neighbours, so that four lanes read a whole cache line.  float32 is taken apart in registers.
 //
-// Bound by the weights' bytes (one row of bfloat16 through 4096 by 11008, not in any cache: 18.9 us, 4.8 TB/s; 16 features
-// out to a workgroup, 32 take 27.7; four or sixteen waves 22.1, 20.5; eight pieces on their way instead of
-// four 20.8), from 16 rows on also by x, which is as many bytes to a workgroup then (26.8).
+// Bound by the weights' bytes (one row of bfloat16 through 4096 by 11008, not in any cache: 17.5 us, 5.2 TB/s; 16 features
+// out to a workgroup, 32 take half as long again; four or sixteen waves a sixth and a twelfth more; eight pieces on their way instead
+// of four a tenth), at 16 rows also by x, which is as many bytes to a workgroup then (26.0).
 constexpr int kFewWaves = 8;
-template <typename T, int MT>
+template <typename T>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void few_kernel(FewArgs a)
 {
-    constexpr bool apart = sizeof(T) == 4 && MT > 1;            // x comes taken apart
-    constexpr int planes = sizeof(T) == 2 ? 1 : 3, read = apart ? 3 : 1;
-    constexpr int D = sizeof(T) == 2 ? 4 : MT == 1 ? 2 : 1;     // pieces on their way
-    typedef typename std::conditional<apart, uint16_t, T>::type X;
-    __shared__ f32x4 sums[kFewWaves][MT][64];
+    constexpr int planes = sizeof(T) == 2 ? 1 : 3, D = sizeof(T) == 2 ? 4 : 2;  // pieces on their way
+    __shared__ f32x4 sums[kFewWaves][64];
     const uint32_t lane = lane_id(), wave = threadIdx.x >> 6, at = lane & 15, k0 = (lane >> 4) * 16;
     const uint32_t n0 = blockIdx.x * 16;
     const T *w = static_cast<const T *>(a.w) + min(n0 + at, a.out - 1) * a.ldw;
-    const X *x[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) x[i] = static_cast<const X *>(a.x) + min(16 * i + at, a.rows - 1) * a.ldx;
-    f32x4 acc[MT] = {};
+    const T *x = static_cast<const T *>(a.x) + min(at, a.rows - 1) * a.ldx;
+    f32x4 acc = {};
     for (uint32_t k = wave * 64; k < a.in; k += kFewWaves * 64 * D) {
-        Piece<T> pw[D];
-        Piece<X> px[D][MT][read];
+        Piece<T> pw[D], px[D];
 #pragma unroll
         for (int d = 0; d < D; ++d) {
             const uint32_t from = k + d * kFewWaves * 64 + k0;
             pw[d].load(w, from, a.in);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int q = 0; q < read; ++q) px[d][i][q].load(x[i] + q * a.part, from, a.in);
+            px[d].load(x, from, a.in);
         }
 #pragma unroll
         for (int d = 0; d < D; ++d)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                bf16x8 fw[planes];
+                bf16x8 fw[planes], fx[planes];
                 pw[d].half(h, fw);
+                px[d].half(h, fx);
+                if constexpr (planes == 1) {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[0], fx[0], acc, 0, 0, 0);
+                } else {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    bf16x8 fx[planes];
-                    if constexpr (apart) {
-#pragma unroll
-                        for (int q = 0; q < 3; ++q) px[d][i][q].half(h, *reinterpret_cast<bf16x8(*)[1]>(&fx[q]));
-                    } else {
-                        px[d][i][0].half(h, fx);
-                    }
-                    if constexpr (planes == 1) {
-                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[0], fx[0], acc[i], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (uint32_t t = 0; t < 6; ++t)
-                            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[term_q(t)], fx[term_p(t)], acc[i], 0, 0, 0);
-                    }
+                    for (uint32_t t = 0; t < 6; ++t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[term_q(t)], fx[term_p(t)], acc, 0, 0, 0);
                 }
             }
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    sums[wave][lane] = acc;
     __syncthreads();
     // Eight neighbours of a row, features 8 h to 8 h + 7, are in two lanes' words.
-    for (uint32_t t = threadIdx.x; t < MT * 32; t += kFewWaves * 64) {
-        const uint32_t m = t / 2, h = t % 2, n = n0 + 8 * h;
-        if (m >= a.rows || n >= a.out) continue;
-        float z[8] = {};
+    const uint32_t m = threadIdx.x / 2, h = threadIdx.x % 2, n = n0 + 8 * h;
+    if (m >= a.rows || n >= a.out) return;
+    float z[8] = {};
 #pragma unroll
-        for (int s = 0; s < kFewWaves; ++s)
+    for (int s = 0; s < kFewWaves; ++s)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const f32x4 v = sums[s][m / 16][(2 * h + q) * 16 + m % 16];
+        for (int q = 0; q < 2; ++q) {
+            const f32x4 v = sums[s][(2 * h + q) * 16 + m];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z[4 * q + e] += v[e];
-            }
-        finish<T>(a.result, m, n, min(8u, a.out - n), z);
-    }
-}
-
-template <typename T>
-void launch_few(const FewArgs &a, hipStream_t s)
-{
-    const uint32_t grid = (a.out + 15) / 16;
-    if (sizeof(T) == 2 || a.rows <= 16) few_kernel<T, 1><<<grid, kFewWaves * 64, 0, s>>>(a);
-    else if constexpr (sizeof(T) == 4) {
-        if (a.rows <= 32) few_kernel<T, 2><<<grid, kFewWaves * 64, 0, s>>>(a);
-        else few_kernel<T, 4><<<grid, kFewWaves * 64, 0, s>>>(a);
-    }
+            for (int e = 0; e < 4; ++e) z[4 * q + e] += v[e];
+        }
+    finish<T>(a.result, m, n, min(8u, a.out - n), z);
 }
 
 // ------------------------------------------------------------------ host
@@ -1064,7 +1170,7 @@ struct Places {
 };
 
 struct Operand {
-    const uint16_t *p;
+    const void *p;
     uint64_t ld;
     uint32_t part;  // of float32 the three parts of a row, one behind the other, are so far apart
 };
@@ -1075,6 +1181,10 @@ bool as_it_lies(uint32_t dtype, const void *p, uint64_t ld, uint64_t cols, bool 
 {
     return dtype == TAGC_BF16 && (reinterpret_cast<uintptr_t>(p) & 3) == 0 && ld % 2 == 0 && ld < kMaxSide && cols % (turned ? 2 : 8) == 0;
 }
+
+// Whether float32 rows of k's are read as they lie (raw3_kernel): laying out (m + n) k elements takes 2.1 us a million, and m n k products
+// of what lies as it did 1.6 us a thousand million more.
+bool raw_pays(uint64_t m, uint64_t n) { return m * n < 1300 * (m + n); }
 
 Operand room(Places &w, uint32_t dtype, uint64_t rows, uint64_t cols)
 {
@@ -1089,7 +1199,7 @@ PackArgs packed(const void *src, uint64_t ld, uint64_t rows, uint64_t cols, cons
     a.ld = ld;
     a.rows = uint32_t(rows);
     a.cols = uint32_t(cols);
-    a.to = const_cast<uint16_t *>(to.p);
+    a.to = static_cast<uint16_t *>(const_cast<void *>(to.p));
     a.to_ld = to.ld;
     a.to_part = to.part;
     return a;
@@ -1109,7 +1219,7 @@ struct Packs {
     // a matrix as it lies, or laid out anew
     Operand operand(Places &w, uint32_t dtype, const void *src, uint64_t ld, uint64_t rows, uint64_t cols, bool turned)
     {
-        if (as_it_lies(dtype, src, ld, cols, turned)) return Operand{static_cast<const uint16_t *>(src), ld, 0};
+        if (as_it_lies(dtype, src, ld, cols, turned)) return Operand{src, ld, 0};
         const Operand to = room(w, dtype, rows, cols);
         add(packed(src, ld, rows, cols, to));
         return to;
@@ -1148,7 +1258,12 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
     if (grid) {
         ProfileScope prof("linear_product", s);
         if constexpr (sizeof(T) == 4) {
-            product3_kernel<PT, QT><<<grid, 512, 0, s>>>(a);
+            if constexpr (!PT && !QT) {
+                if (!p.part) raw3_kernel<<<grid, 512, 0, s>>>(a);
+                else product3_kernel<PT, QT><<<grid, 512, 0, s>>>(a);
+            } else {
+                product3_kernel<PT, QT><<<grid, 512, 0, s>>>(a);
+            }
         } else {
             if (f.rows == 256) product_kernel<2, 4, 8, 4, PT, QT><<<grid, 512, 0, s>>>(a);
             else if (f.rows == 128) product_kernel<2, 4, 4, 2, PT, QT><<<grid, 512, 0, s>>>(a);
@@ -1195,24 +1310,18 @@ int forward(const tagc_linear *l, Places &w, bool enqueue, hipStream_t s)
     const Result r{l->bias, l->residual, l->y, l->pre, l->ldr, l->ldy, l->ldp, l->activation};
     const uint64_t M = l->rows, K = l->in, N = l->out;
     if (!M || !N) return TAGC_OK;
-    if (M <= kFewRows[l->dtype]) {
-        FewArgs a{l->x, l->w, l->ldx, l->ldw, 0, uint32_t(M), uint32_t(K), uint32_t(N), r};
-        if (sizeof(T) == 4 && M > 16) {
-            Packs packs;
-            const Operand x = packs.operand(w, l->dtype, l->x, l->ldx, M, K, false);
-            if (enqueue) packs.launch<T>(s);
-            a.x = x.p;
-            a.ldx = x.ld;
-            a.part = x.part;
-        }
+    if (M <= kFewRows) {
         if (!enqueue) return TAGC_OK;
         ProfileScope prof("linear_few", s);
-        launch_few<T>(a, s);
+        few_kernel<T><<<uint32_t((N + 15) / 16), kFewWaves * 64, 0, s>>>(FewArgs{l->x, l->w, l->ldx, l->ldw, uint32_t(M), uint32_t(K), uint32_t(N), r});
         return hip_ok(hipGetLastError());
     }
     Packs packs;
-    const Operand p = packs.operand(w, l->dtype, l->x, l->ldx, M, K, false);
-    const Operand q = packs.operand(w, l->dtype, l->w, l->ldw, N, K, false);
+    Operand p{l->x, l->ldx, 0}, q{l->w, l->ldw, 0};
+    if (sizeof(T) == 2 || !raw_pays(M, N) || l->ldx >= kMaxSide || l->ldw >= kMaxSide) {
+        p = packs.operand(w, l->dtype, l->x, l->ldx, M, K, false);
+        q = packs.operand(w, l->dtype, l->w, l->ldw, N, K, false);
+    }
     float *partial = w.take<float>(partial_elems(M, N, K, l->dtype, false));
     if (!enqueue) return TAGC_OK;
     packs.launch<T>(s);
@@ -1225,7 +1334,7 @@ int backward(const tagc_linear_grad *l, Places &w, bool enqueue, hipStream_t s)
 {
     const uint64_t M = l->rows, K = l->in, N = l->out;
     const bool dx = l->dx && M && K, dw = l->dw && N && K, db = l->db && N;
-    Operand dz{static_cast<const uint16_t *>(l->dy), l->lddy, 0};
+    Operand dz{l->dy, l->lddy, 0};
     PackArgs a = packed(l->dy, l->lddy, M, N, Operand{});
     if ((dx || dw) && (l->pre || !as_it_lies(l->dtype, l->dy, l->lddy, N, !dx))) {
         dz = room(w, l->dtype, M, N);

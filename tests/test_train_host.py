@@ -128,7 +128,8 @@ def test_workspaces():
     assert B.tagc_linear_forward_workspace(_fwd(rows=1)) == 0          # the weights as they lie
     # rows off a 16-byte boundary are laid out anew: 100 rows of 128
     assert (B.tagc_linear_forward_workspace(_fwd(x=AT + 2)) - B.tagc_linear_forward_workspace(_fwd())) == 100 * 128 * 2
-    assert B.tagc_linear_forward_workspace(_fwd(dtype=B.TAGC_F32)) >= (100 + 64) * 128 * 6
+    # float32 is taken apart in the product where tiles are few, in the workspace where they are many
+    assert B.tagc_linear_forward_workspace(_fwd(dtype=B.TAGC_F32, rows=4096, out=4096, ldy=4096)) >= 2 * 4096 * 128 * 6
     # behind an activation dz is laid out, and a bias's gradient has partial sums
     behind = dict(pre=AT, ldp=64, activation=B.TAGC_ACT_SILU)
     need = B.tagc_linear_backward_workspace(_bwd(**behind))

@@ -149,6 +149,18 @@ def test_large_tiles(shape, dtype):
     _near(db, dz.sum(0), (M + 8) * 2 * E * dz.abs().sum(0), t, "db")
 
 
+# float32 rows end inside, at and behind a slab of the product, one or many slabs to a tile; the last shape has tiles enough to be
+# laid out beforehand
+@pytest.mark.parametrize("shape", [(m, k, n) for k in (1, 31, 32, 33, 63, 65, 97, 161, 1537) for m, n in ((17, 130), (130, 200))] + [(2700, 100, 2650)], ids=str)
+def test_float32_rows_ending_anywhere(shape):
+    from paper_2504_05638_amd.train import linear
+    M, K, N = shape
+    print("[case] float32 rows", shape, flush=True)
+    x, w = _randn((M, K), 5, torch.float32, ld_more=5, shift=3), _randn((N, K), 6, torch.float32, ld_more=1)
+    _, _, ref, err = _forward_ref(x, w, None, None, "none")
+    _near(linear(x, w)[0], ref, err, torch.float32, shape)
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_gradient_against_differences(act):
     """d(sum(c * y)) / dw, dx, db by central differences of the library's own forward in float32."""

@@ -669,6 +669,100 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(Product a)
     write_out<uint16_t, RM, RN>(a, acc, strip, lane, m0 + wm * RM * 16, n0 + wn * RN * 16, at.part);
 }
 
+// The product where there is no more than a tile of 128 by 128 for each compute unit, which its eight waves have to themselves: what
+// they wait for is memory, so four stages keep three slabs on their way, and a slab's pieces are all read
+// while the one before is multiplied.  (us, here / by two workgroups of product_kernel to a compute unit: 2048 by 2048 by 4096 35 / 47,
+// 700 by 4096 by 4096 31 / 43, 1024 by 4096 by 1024 14 / 18, 4096 by 1024 by 2048 20 / 27; with two tiles for each
+// compute unit, one behind the other here, 8192 by 1024 by 4096 74 / 65.)
+template <bool PT, bool QT>
+__global__ __launch_bounds__(512, 2) void lone_kernel(Product a)
+{
+    constexpr int RM = 4, RN = 2, kSteps = kSlab / 32;
+    constexpr uint32_t T = 128, kStage = 2 * T * kSlab * 2, kRow = RN * 16 + 4;
+    constexpr int kLoads = 2 * T * 8 / 512, kReads = kSteps * (RM * (PT ? 2 : 1) + RN * (QT ? 2 : 1)), kProducts = kSteps * RM * RN;
+    __shared__ __attribute__((aligned(1024))) char stage0[kStage];
+    __shared__ __attribute__((aligned(1024))) char stage1[kStage];
+    __shared__ __attribute__((aligned(1024))) char stage2[kStage];
+    __shared__ __attribute__((aligned(1024))) char stage3[kStage];
+    static_assert(4 * 32 * kRow * 4 <= kStage, "half the strips fit");
+    const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wm = wave & 1, wn = wave >> 1;
+    const Place at = place<T, T>(a);
+    const Side<PT, T, 512> side_p(at.m0, a.ldp);
+    const Side<QT, T, 512> side_q(at.n0, a.ldq);
+    const uint32_t first = at.part * a.slabs, count = min(a.slabs, (a.k + kSlab - 1) / kSlab - first);
+    uint32_t k0 = first * kSlab, to_come = count;
+    Walk<uint16_t> walk_p = side_p.walk(a.p, at.m0, a.m, k0, a.k, a.ldp), walk_q = side_q.walk(a.q, at.n0, a.n, k0, a.k, a.ldq);
+    // (behind the last slab the last one again, which nobody uses)
+    auto fetch = [&](char *stage) __attribute__((always_inline)) {
+        side_p.fetch(walk_p.described(), k0, a.k, stage, wave);
+        side_q.fetch(walk_q.described(), k0, a.k, stage + T * 128, wave);
+        const bool on = to_come > 1;
+        to_come -= on;
+        k0 += on ? kSlab : 0;
+        walk_p.advance(on);
+        walk_q.advance(on);
+    };
+    f32x4 acc[RM][RN] = {};
+    bf16x8 fp[2][kSteps][RM], fq[2][kSteps][RN];
+    auto read = [&](const char *stage, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < kSteps; ++h) {
+            side_q.template read<RN>(stage + T * 128, wn * RN, h, fq[to][h]);
+            side_p.template read<RM>(stage, wm * RM, h, fp[to][h]);
+        }
+    };
+    // All that this wave has read, and what it has asked for but for `slabs` slabs; then the same for the others.
+    auto meet = [&](auto slabs) __attribute__((always_inline)) {
+        static_assert(decltype(slabs)::value * kLoads < 16, "fits the count");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070 | decltype(slabs)::value * kLoads);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // A slab, whose pieces are in registers: its stage, `now`, is free.
+    auto slab = [&](int from, char *now, const char *next) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(0);
+        meet(std::integral_constant<int, 2>());
+        __builtin_amdgcn_s_setprio(1);
+        read(next, from ^ 1);
+        fetch(now);
+#pragma unroll
+        for (int h = 0; h < kSteps; ++h)
+#pragma unroll
+            for (int i = 0; i < RM; ++i)
+#pragma unroll
+                for (int j = 0; j < RN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fq[from][h][j], fp[from][h][i], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kProducts; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (2 * i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            if (i >= kProducts - kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+    };
+    fetch(stage0);
+    fetch(stage1);
+    fetch(stage2);
+    fetch(stage3);
+    meet(std::integral_constant<int, 3>());
+    read(stage0, 0);
+    // (a way round a slab inside the loop would have the compiler expect any stage to be the newest one, and wait)
+    uint32_t left = count;
+    for (; left >= 4; left -= 4) {
+        slab(0, stage0, stage1);
+        slab(1, stage1, stage2);
+        slab(0, stage2, stage3);
+        slab(1, stage3, stage0);
+    }
+    if (left > 0) slab(0, stage0, stage1);
+    if (left > 1) slab(1, stage1, stage2);
+    if (left > 2) slab(0, stage2, stage3);
+    meet(std::integral_constant<int, 0>());
+    float *strip = reinterpret_cast<float *>(wave < 4 ? stage0 : stage1) + (wave & 3) * 32 * kRow;
+    write_out<uint16_t, RM, RN>(a, acc, strip, lane, at.m0 + wm * RM * 16, at.n0 + wn * RN * 16, at.part);
+}
+
 // One operand of the float32 product's tile, taken apart: slabs of 32 k's of all three parts, R rows, a load of 16
 // bytes to a thread for each part.  As Side otherwise, but that rows are 64 bytes of k's and that every k that a slab
 // has is there, if only as a zero.
@@ -1107,9 +1201,9 @@ struct Shape {
 
 // By what the candidates would take, in us, from measurements at sizes from 333 by 1001 by 832 to 8192 by 8192 by 8192 (within 15 %
 // of them): a slab of 256 by 256 takes a compute unit to itself for 1.68; two of 128 by 128 share one for 1.01, one
-// alone takes 0.70, a slab of 32 float32 1.1; parts of a sum cost a launch, and their bytes written and read.  (us, 256 by 256 / 128 by 128
-// in one, two, four parts: 4096 cubed 107 / 124; 8192 by 2560 by 1024 64 / 53; 2048 by 2048 by 4096 81 / 45, 49; 1024 by 4096 by
-// 1024 31 / 16, 27; 1024 by 1024 by 4096 - / 47, 32, 25; 333 by 1001 by 832 - / 11, 14, 15.)
+// that is left over takes 0.70, one alone by lone_kernel 0.50, a slab of 32 float32 1.1; parts of a sum cost a launch, and their bytes written and read.  (us, 256 by 256 / 128 by 128
+// in one, two, four parts: 4096 cubed 107 / 124; 8192 by 2560 by 1024 64 / 53; 2048 by 2048 by 4096 81 / 35, 49; 1024 by 4096 by
+// 1024 31 / 14, 27; 1024 by 1024 by 4096 - / -, -, 23; 333 by 1001 by 832 - / 10, -, -.)
 Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, bool turned_p)
 {
     Shape s{};
@@ -1138,7 +1232,7 @@ Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, bool turned_p
                     rounds = 1.68 * double((groups + cus - 1) / cus);
                 } else {
                     const uint64_t rest = groups % (2 * cus);
-                    rounds = 1.01 * double(groups / (2 * cus)) + (!rest ? 0.0 : rest <= cus ? 0.70 : 1.01);
+                    rounds = groups <= cus ? 0.50 : 1.01 * double(groups / (2 * cus)) + (!rest ? 0.0 : rest <= cus ? 0.70 : 1.01);
                 }
                 const double us = rounds * double(each) + (parts > 1 ? 4.5 + double(parts * m * n * 8) / 4e6 : 0.0);
                 if (s.rows && us >= best) continue;
@@ -1266,6 +1360,7 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
             }
         } else {
             if (f.rows == 256) product_kernel<2, 4, 8, 4, PT, QT><<<grid, 512, 0, s>>>(a);
+            else if (f.rows == 128 && grid <= uint32_t(device_cu_count())) lone_kernel<PT, QT><<<grid, 512, 0, s>>>(a);  // (as shape_of has it)
             else if (f.rows == 128) product_kernel<2, 4, 4, 2, PT, QT><<<grid, 512, 0, s>>>(a);
             else if constexpr (!PT) {
                 if (f.rows == 64) product_kernel<1, 4, 4, 2, PT, QT><<<grid, 256, 0, s>>>(a);

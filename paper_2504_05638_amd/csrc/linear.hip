@@ -6,8 +6,8 @@
 //   dw            P = dz, k by k       Q = x, k by k           (k: tokens)
 // An operand lies in memory row by row, with a row's k's next to each other, or k by k, with a k's rows next
 // to each other (`turned`); local memory holds it as it lies, and the transposing read takes it from there.
-// What cannot be read as it lies -- rows off a 16-byte boundary, float32, dz where there is an
-// activation -- is first laid out anew in the workspace by pack_kernel; its cost is in the order of an
+// What cannot be read as it lies -- bfloat16 rows that are no whole pieces of 16 bytes, float32 that many tiles
+// read, dz where there is an activation -- is first laid out anew in the workspace by pack_kernel; its cost is in the order of an
 // operand's bytes, the product's in that of rows times operand.
 #include <math.h>
 #include <string.h>
@@ -335,7 +335,7 @@ struct Product {
     Result result;
 };
 
-// The six products of parts whose sum is a float32 product but for 2^-24 of it, smallest first.
+// The six products of parts whose sum is a float32 product but for 2^-22 of it at most, smallest first.
 __device__ inline uint32_t term_p(uint32_t t) { return (0x001102u >> (4 * t)) & 3; }
 __device__ inline uint32_t term_q(uint32_t t) { return (0x010120u >> (4 * t)) & 3; }
 

@@ -82,21 +82,35 @@ def _flat(t, rows, cols):
         raise ValueError(str(e)) from None
 
 
+def _new(like, shape, dtype, stream):
+    """A tensor that a call writes on `stream` (None: the current one) and hands to its caller.  It is `stream`'s own: memory of
+    the current stream's may still be in use there.  It is not used again before what the current stream does with it is done."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    user = torch.cuda.current_stream(like.device)
+    with torch.cuda.stream(stream):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(user)
+    return t
+
+
 def _work(nbytes, x, stream):
-    """A call's workspace (its tensor and its address); kept from reuse until `stream`, where it is not the current
-    one, is done."""
+    """A call's workspace (its tensor and its address), `stream`'s own: reused behind the call only."""
     if not nbytes:
         return None, None
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-    if stream is not None:
-        ws.record_stream(stream)
+    if stream is None:
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    else:
+        with torch.cuda.stream(stream):
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
     return ws, ws.data_ptr()
 
 
 def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None, pre=None, stream=None):
     """(y, pre): y = activation(x w^T + bias) + residual.  x: [..., in], w: [out, in].  `save`: pre =
     x w^T + bias for linear_backward (else None).  `out` and `pre` may be given; `out` may be
-    the residual.  Tensors made here belong to the current stream."""
+    the residual.  With `stream` the call runs there: what it reads has to be ready there, and stay until it is done; what it
+    makes (results, workspace) is `stream`'s memory."""
     _check_input(x, w, activation)
     n, k = w.shape
     shape, dtype, device = x.shape, x.dtype, x.device
@@ -107,12 +121,12 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     bp = _vector(bias, "bias", n, dtype, device)
     rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
     if out is None:
-        out = x.new_empty((*shape[:-1], n))
+        out = _new(x, (*shape[:-1], n), dtype, stream)
         yp, ldy = out.data_ptr() or None, n
     else:
         yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
     if save and pre is None:
-        pre = x.new_empty((*shape[:-1], n))
+        pre = _new(x, (*shape[:-1], n), dtype, stream)
         pp, ldp = pre.data_ptr() or None, n
     else:
         pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
@@ -126,7 +140,7 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
                     need_dx=True, stream=None):
     """dx (None without need_dx).  With `dw` ([out, in], a view into a bucket's gradient) and `db` ([out])
     given, the weight's and the bias's gradient are written there, or added to what is there
-    (accumulate).  `pre`: what linear(save=True) gave; None without an activation."""
+    (accumulate).  `pre`: what linear(save=True) gave; None without an activation.  `stream`: as for linear."""
     _check_input(x, w, activation)
     n, k = w.shape
     shape, dtype, device = x.shape, x.dtype, x.device
@@ -139,7 +153,7 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
     yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
     if need_dx and dx is None:
-        dx = x.new_empty(shape)
+        dx = _new(x, shape, dtype, stream)
         dp, ldd = dx.data_ptr() or None, k
     else:
         dp, ldd = _rows_of(_flat(dx, m, k), "dx", m, k, dtype, device)
@@ -265,10 +279,7 @@ class AdamW:
 
     def unpack(self, stream=None):
         """(m, v): what 8-bit moments stand for, bfloat16, the tensors one behind the other."""
-        m, v = (torch.empty(self.sizes.n_elems, dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        if stream is not None:
-            m.record_stream(stream)
-            v.record_stream(stream)
+        m, v = (_new(self.table, (self.sizes.n_elems,), torch.bfloat16, stream) for _ in range(2))
         B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None,
                             _stream_of(stream, self.device))
         return m, v

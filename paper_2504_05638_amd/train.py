@@ -208,12 +208,14 @@ class AdamW:
         _need(all(0 <= g < len(self.groups) for g in group_of), "group_of: there are %d groups" % len(self.groups))
         _need(bits in (8, 32), "bits: 8 or 32")
         _need(first_step >= 1, "first_step: 1 or more")
+        made = []
         if self.params is not None and m is None:
             _need(v is None and bases is None, "m, v (and bases) are given together or not at all")
             state = torch.float32 if bits == 32 else torch.uint8
             m, v = ([torch.zeros(g.numel(), dtype=state, device=self.device) for g in grads] for _ in range(2))
             if bits == 8:
                 bases = [torch.zeros(self._blocks(g), dtype=torch.int32, device=self.device) for g in grads]
+            made = [*m, *v, *(bases or ())]
         self.m, self.v, self.bases, self.copies = m, v, bases, copies
         rows = (B.tagc_tensor * n)()
         for i, g in enumerate(grads):
@@ -243,6 +245,8 @@ class AdamW:
         f = self.control.view(torch.float32)
         self.norm, self.factor, self.lr_scale = f[3], f[4], f[5]
         self._table, self._control = self.table.data_ptr(), self.control.data_ptr()
+        # what is made here, and the streams that it has been used on: the one it belongs to first
+        self._made, self._streams = [self.table, self.control, *made], {_stream_ptr()}
         B.tagc_optim_upload(self.plan, self._table, _stream_ptr())
         torch.cuda.current_stream().synchronize()
 
@@ -254,6 +258,17 @@ class AdamW:
         _need(t.dtype in types and t.device == self.device and t.numel() == k and (t.is_contiguous() or k <= 1),
               "%s[%d]: a contiguous tensor of %d, %s on %s, is wanted" % (name, i, k, " or ".join(map(str, types)), self.device))
         return t.data_ptr() if k else None
+
+    def _on(self, stream):
+        """The address of the stream that a call runs on.  What was made here is not handed out again before the streams that
+        used it are done, also where the object goes first."""
+        at = _stream_of(stream, self.device)
+        if at not in self._streams:
+            s = stream if stream is not None else torch.cuda.current_stream(self.device)
+            for t in self._made:
+                t.record_stream(s)
+            self._streams.add(at)
+        return at
 
     @property
     def groups(self):
@@ -268,20 +283,18 @@ class AdamW:
 
     def grad_norm(self, stream=None):
         """Begins a step; (norm, factor): device scalars, views of the control block."""
-        B.tagc_grad_norm(self.plan, self._table, self._control, _stream_of(stream, self.device))
+        B.tagc_grad_norm(self.plan, self._table, self._control, self._on(stream))
         return self.norm, self.factor
 
     def step(self, step=0, stream=None):
         """One step: the one that grad_norm() began, its learning rates times the device scalar
         `lr_scale`; or, with `step` > 0, that one, unclipped, with the groups' learning rates."""
-        B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control,
-                          _stream_of(stream, self.device))
+        B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control, self._on(stream))
 
     def unpack(self, stream=None):
         """(m, v): what 8-bit moments stand for, bfloat16, the tensors one behind the other."""
         m, v = (_new(self.table, (self.sizes.n_elems,), torch.bfloat16, stream) for _ in range(2))
-        B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None,
-                            _stream_of(stream, self.device))
+        B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None, self._on(stream))
         return m, v
 
     def close(self):

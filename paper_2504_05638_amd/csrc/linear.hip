@@ -52,7 +52,7 @@ template <typename T>
 __device__ inline float normal_below(float z, float &bell)
 {
     bell = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
-    if constexpr (sizeof(T) == 4) return 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    if constexpr (sizeof(T) == 4) return 0.5f * erfcf(z * -0.70710678118654752f);  // (1 + erf would lose the left tail's bits)
     const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678118654752f * fabsf(z));
     const float tail = 0.5f * bell * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
     return z < 0 ? tail : 1.0f - tail;

@@ -4,7 +4,8 @@ z below(z), with below(z) = erfc(-z / sqrt(2)) / 2.  An argument off by a relati
 of itself for u > 1, that is (z^2 + 1.5) d, and exp(-z^2 / 2) by z^2 d.  With e = 2^-24, float32: the argument takes two
 roundings and one of the constant, erfc itself 16 ulps at most (2 e each), three products more; the bell's exponent
 two roundings and the constant's, exp2 two ulps.  Slope: below(z) + z bell(z) / sqrt(2 pi), to the left of -2 of opposite signs and
-no cancellation to speak of: z bell is at least 4 times below."""
+no cancellation to speak of: z bell is at least 4 times below.  bfloat16: 2^-12 for the polynomial instead of erfc's own, and the result's
+rounding, 2^-8."""
 import math
 
 import pytest
@@ -34,3 +35,13 @@ def test_float32_left_tail():
     # four thirds of the bell's share and a third of below's
     rel = (4 * (d * d * 3 + 8) + ((d * d + 1.5) * 3 + 36)) / 3 * E
     assert torch.all((slope - slope_ref).abs() <= rel * slope_ref.abs())
+
+
+def test_bfloat16_left_tail():
+    """Every bfloat16 from -2 to -12.5."""
+    z = torch.arange(0x4000, 0x4149, device="cuda", dtype=torch.int32).to(torch.int16).view(torch.bfloat16).neg()
+    assert float(z[0]) == -2.0 and float(z[-1]) == -12.5
+    y, ref, slope, slope_ref, d = _through(z, torch.bfloat16)
+    below, bell, half = 2.0 ** -12 + (3 * d * d + 40) * E, (3 * d * d + 8) * E, 2.0 ** -8
+    assert torch.all((y - ref).abs() <= (below + half) * ref.abs())
+    assert torch.all((slope - slope_ref).abs() <= ((4 * bell + below) / 3 + half) * slope_ref.abs())

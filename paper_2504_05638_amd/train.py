@@ -193,6 +193,7 @@ class AdamW:
                  group_of=None, betas=(0.9, 0.999), eps=1e-8, bits=32, grad_scale=1.0, max_norm=0.0, seed=0,
                  first_step=1):
         self.plan = None
+        self._begun = False
         grads = list(grads)
         n = len(grads)
         _need(n > 0, "no gradients")
@@ -284,11 +285,14 @@ class AdamW:
     def grad_norm(self, stream=None):
         """Begins a step; (norm, factor): device scalars, views of the control block."""
         B.tagc_grad_norm(self.plan, self._table, self._control, self._on(stream))
+        self._begun = True
         return self.norm, self.factor
 
     def step(self, step=0, stream=None):
         """One step: the one that grad_norm() began, its learning rates times the device scalar
         `lr_scale`; or, with `step` > 0, that one, unclipped, with the groups' learning rates."""
+        if not step and not self._begun:  # (the control block would say that there is nothing to apply)
+            raise RuntimeError("step() carries on what grad_norm() began: call that first, or give the step's number")
         B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control, self._on(stream))
 
     def unpack(self, stream=None):

@@ -1,0 +1,21 @@
+"""How the optimizer's calls go together: what would change nothing, or something else than was meant, is refused."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _adamw(**kw):
+    from paper_2504_05638_amd.train import AdamW
+    return AdamW(params=[torch.ones(1000, device="cuda")], grads=[torch.ones(1000, device="cuda")], groups=[(0.5, 0.0)], **kw)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_that_nothing_began(bits):
+    opt = _adamw(bits=bits)
+    with pytest.raises(RuntimeError, match="grad_norm"):
+        opt.step()
+    opt.grad_norm()
+    opt.step()
+    assert torch.allclose(opt.params[0], torch.full_like(opt.params[0], 0.5))
+    assert opt.control[0].item() == 1

@@ -201,7 +201,7 @@ class AdamW:
         _need(self.device.type == "cuda", "libtagc needs a GPU: no CPU path exists")
         group_of = [0] * n if group_of is None else list(group_of)
         self.groups = groups
-        self.bits, self.grads = bits, grads
+        self.bits, self.grads, self._clips = bits, grads, max_norm > 0
         self.params = list(params) if params is not None else None
         lists = {"params": self.params, "copies": copies, "m": m, "v": v, "bases": bases, "group_of": group_of}
         for name, given in lists.items():
@@ -290,7 +290,8 @@ class AdamW:
 
     def step(self, step=0, stream=None):
         """One step: the one that grad_norm() began, its learning rates times the device scalar
-        `lr_scale`; or, with `step` > 0, that one, unclipped, with the groups' learning rates."""
+        `lr_scale`; or, with `step` > 0, that one, with the groups' learning rates (not of an optimizer that clips)."""
+        _need(not step or not self._clips, "a given step is not clipped, and there is a max_norm: grad_norm(), then step()")
         if not step and not self._begun:  # (the control block would say that there is nothing to apply)
             raise RuntimeError("step() carries on what grad_norm() began: call that first, or give the step's number")
         B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control, self._on(stream))

@@ -19,3 +19,13 @@ def test_a_step_that_nothing_began(bits):
     opt.step()
     assert torch.allclose(opt.params[0], torch.full_like(opt.params[0], 0.5))
     assert opt.control[0].item() == 1
+
+
+def test_a_given_step_of_an_optimizer_that_clips():
+    opt = _adamw(max_norm=1.0)
+    with pytest.raises(ValueError, match="max_norm"):
+        opt.step(1)
+    assert torch.equal(opt.params[0], torch.ones_like(opt.params[0]))
+    opt.grad_norm()
+    opt.step()      # clipped from 31.6 to 1: each gradient is 1 / sqrt(1000), m a tenth of that
+    assert torch.allclose(opt.m[0], torch.full_like(opt.m[0], 0.1 * 1000 ** -0.5))

@@ -291,6 +291,7 @@ class AdamW:
     def step(self, step=0, stream=None):
         """One step: the one that grad_norm() began, its learning rates times the device scalar
         `lr_scale`; or, with `step` > 0, that one, with the groups' learning rates (not of an optimizer that clips)."""
+        _need(0 <= step < 1 << 32, "step: 1 or more, less than 2^32, or 0 for the one that grad_norm() began")
         _need(not step or not self._clips, "a given step is not clipped, and there is a max_norm: grad_norm(), then step()")
         if not step and not self._begun:  # (the control block would say that there is nothing to apply)
             raise RuntimeError("step() carries on what grad_norm() began: call that first, or give the step's number")

@@ -29,3 +29,13 @@ def test_a_given_step_of_an_optimizer_that_clips():
     opt.grad_norm()
     opt.step()      # clipped from 31.6 to 1: each gradient is 1 / sqrt(1000), m a tenth of that
     assert torch.allclose(opt.m[0], torch.full_like(opt.m[0], 0.1 * 1000 ** -0.5))
+
+
+@pytest.mark.parametrize("step", [-1, 1 << 32, (1 << 32) + 1])
+def test_a_step_that_does_not_fit_its_word(step):
+    """(cut to 32 bits they would be step 4294967295, the one that grad_norm() began, and step 1)"""
+    opt = _adamw()
+    opt.grad_norm()
+    with pytest.raises(ValueError, match="2\\^32"):
+        opt.step(step)
+    assert torch.equal(opt.params[0], torch.ones_like(opt.params[0]))

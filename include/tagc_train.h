@@ -122,6 +122,7 @@ int tagc_grad_norm(const tagc_optim_t *plan, void *table_dev, tagc_optim_control
  * One AdamW step of all tensors, in float32 (t the step, b1, b2 the betas):
  *   g = factor * grad;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
  *   p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+ * (with eps = 0 where v is 0, too, that is m / 0: gradients under 1e-22 have squares that float32 does not hold).
  * param and copy are rounded to nearest, ties to even, where they are bfloat16.
  * step > 0: that is t, factor is grad_scale, control is not looked at (may be NULL).
  * step = 0: t, factor, lr_scale and whether to do anything come from control.

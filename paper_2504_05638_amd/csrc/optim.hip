@@ -241,20 +241,23 @@ struct Hyper {
 // m, v and p of one element after the step.  Products and sums are rounded one by one (a product that
 // went into a sum unrounded would make the 8-bit moments differ from what the formula gives in
 // float32).
+template <bool SMALL_EPS>
 __device__ inline void adamw(const Hyper &h, float grad, float &m, float &v, float &p)
 {
 #pragma clang fp contract(off)
     const float g = grad * h.factor;
     m = m * h.beta1 + g * h.rest1;
     v = v * h.beta2 + (g * g) * h.rest2;
-    // (root and reciprocal as the hardware has them, within an ulp each: they go nowhere but into the update)
-    p = p * h.decay - m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * h.bias2 + h.eps) * h.size;
+    // (root and reciprocal as the hardware has them, within an ulp each, where what they go into is more than a subnormal
+    // number's root, which the hardware takes for 0: see small_eps)
+    if constexpr (SMALL_EPS) p = p * h.decay - m / (sqrtf(v) * h.bias2 + h.eps) * h.size;
+    else p = p * h.decay - m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * h.bias2 + h.eps) * h.size;
 }
 
 // Bound by bytes: 151 M elements in float32 (28 bytes each) take 713 us, 5.9 TB/s.  All loads of a thread, four times four
 // neighbours of four arrays, go out before the first is used, and none is kept by the caches (with
 // ordinary loads and stores 779 us).
-template <typename P, typename G>
+template <typename P, typename G, bool SMALL_EPS>
 __device__ inline void adamw32_chunk(const TensorDev &t, uint64_t at, const Hyper &h)
 {
     const G *grad = as_global(static_cast<const G *>(t.grad));
@@ -276,7 +279,7 @@ __device__ inline void adamw32_chunk(const TensorDev &t, uint64_t at, const Hype
         const uint64_t i = at + 4 * (k * kOptimThreads + threadIdx.x);
         if (i >= n) break;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) adamw(h, g[k][j], m[k][j], v[k][j], p[k][j]);
+        for (int j = 0; j < 4; ++j) adamw<SMALL_EPS>(h, g[k][j], m[k][j], v[k][j], p[k][j]);
         store_f32(mp, i, n, m[k]);
         store_f32(vp, i, n, v[k]);
         store_f32(param, i, n, p[k]);
@@ -348,7 +351,7 @@ __device__ inline bool zero_byte(uint32_t x) { return ((x - 0x01010101u) & ~x & 
 // the VALU where they are not (10 bytes each, 393 us, 5.1 TB/s): some 50 instructions an element, after root and
 // reciprocal by the hardware (659 -> 587 us, 535 -> 464), the maximum of both moments at once without local memory, and
 // what is seldom behind branches (587 -> 549, 464 -> 401).
-template <typename P, typename G>
+template <typename P, typename G, bool SMALL_EPS>
 __device__ inline void adamw8_chunk(const TensorDev &t, uint64_t at, const Hyper &h, uint32_t key)
 {
     const G *grad = as_global(static_cast<const G *>(t.grad));
@@ -397,7 +400,7 @@ __device__ inline void adamw8_chunk(const TensorDev &t, uint64_t at, const Hyper
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            adamw(h, g[k][j], m[j], v[j], p[k][j]);
+            adamw<SMALL_EPS>(h, g[k][j], m[j], v[j], p[k][j]);
             u[j] = j ? (word >> (8 * j)) | (word << (32 - 8 * j)) : word;
             bits_m[j] = __float_as_uint(m[j]);
             bits_v[j] = __float_as_uint(v[j]);
@@ -445,7 +448,7 @@ __device__ inline void adamw8_chunk(const TensorDev &t, uint64_t at, const Hyper
     }
 }
 
-template <int BITS>
+template <int BITS, bool SMALL_EPS>
 __global__ __launch_bounds__(BITS == 32 ? kOptimThreads : kCodeThreads) void adamw_kernel(StepArgs a)
 {
     const ChunkDev ch = a.chunks[blockIdx.x];
@@ -467,18 +470,18 @@ __global__ __launch_bounds__(BITS == 32 ? kOptimThreads : kCodeThreads) void ada
     const uint64_t at = uint64_t(ch.chunk) * kChunk;
     if constexpr (BITS == 32) {
         switch (t.types) {
-            case 0: return adamw32_chunk<float, float>(t, at, h);
-            case kParamBf16: return adamw32_chunk<uint16_t, float>(t, at, h);
-            case kGradBf16: return adamw32_chunk<float, uint16_t>(t, at, h);
-            default: return adamw32_chunk<uint16_t, uint16_t>(t, at, h);
+            case 0: return adamw32_chunk<float, float, SMALL_EPS>(t, at, h);
+            case kParamBf16: return adamw32_chunk<uint16_t, float, SMALL_EPS>(t, at, h);
+            case kGradBf16: return adamw32_chunk<float, uint16_t, SMALL_EPS>(t, at, h);
+            default: return adamw32_chunk<uint16_t, uint16_t, SMALL_EPS>(t, at, h);
         }
     } else {
         const uint32_t key = mix32(ch.tensor * 0x9E3779B9u + seed_word(a.seed, step));
         switch (t.types) {
-            case 0: return adamw8_chunk<float, float>(t, at, h, key);
-            case kParamBf16: return adamw8_chunk<uint16_t, float>(t, at, h, key);
-            case kGradBf16: return adamw8_chunk<float, uint16_t>(t, at, h, key);
-            default: return adamw8_chunk<uint16_t, uint16_t>(t, at, h, key);
+            case 0: return adamw8_chunk<float, float, SMALL_EPS>(t, at, h, key);
+            case kParamBf16: return adamw8_chunk<uint16_t, float, SMALL_EPS>(t, at, h, key);
+            case kGradBf16: return adamw8_chunk<float, uint16_t, SMALL_EPS>(t, at, h, key);
+            default: return adamw8_chunk<uint16_t, uint16_t, SMALL_EPS>(t, at, h, key);
         }
     }
 }
@@ -527,6 +530,11 @@ __global__ __launch_bounds__(kCodeThreads) void unpack_kernel(const TensorDev *r
 
 bool aligned(const void *p, uint64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 uint64_t type_bytes(uint32_t type) { return type == TAGC_F32 ? 4 : 2; }
+
+// Whether the update's denominator, sqrt(v) / sqrt(1 - beta2^t) + eps, can be changed by more than a rounding, 2^-24, where a subnormal
+// v, whose root is 2^-63 at most, is taken for 0; the first root's divisor is sqrt(1 - beta2) at least.  Then root and quotient
+// are IEEE's.  (An eps of 1e-8 is small for a beta2 from 1 - 3.3e-8 on only.)
+bool small_eps(const tagc_optim_config &cfg) { return cfg.eps * sqrt(1 - cfg.beta2) < 0x1p-39; }
 
 // one tensor's pointers and fields
 int check_tensor(const tagc_optim_config &cfg, const tagc_tensor &t)
@@ -687,10 +695,12 @@ extern "C" int tagc_adamw_step(const tagc_optim_t *p, const void *table, const t
     const uint32_t grid = uint32_t(p->chunks.size());
     if (p->cfg.moment_bits == 32) {
         ProfileScope prof("adamw32", s);
-        adamw_kernel<32><<<grid, kOptimThreads, 0, s>>>(a);
+        if (small_eps(p->cfg)) adamw_kernel<32, true><<<grid, kOptimThreads, 0, s>>>(a);
+        else adamw_kernel<32, false><<<grid, kOptimThreads, 0, s>>>(a);
     } else {
         ProfileScope prof("adamw8", s);
-        adamw_kernel<8><<<grid, kCodeThreads, 0, s>>>(a);
+        if (small_eps(p->cfg)) adamw_kernel<8, true><<<grid, kCodeThreads, 0, s>>>(a);
+        else adamw_kernel<8, false><<<grid, kCodeThreads, 0, s>>>(a);
     }
     return hip_ok(hipGetLastError());
 }

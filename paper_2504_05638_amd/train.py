@@ -12,6 +12,7 @@ marshalling only; all arithmetic is the library's (include/tagc_train.h).
 from __future__ import annotations
 
 import math
+import warnings
 
 import torch
 
@@ -109,9 +110,13 @@ def _work(nbytes, x, stream):
 def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None, pre=None, stream=None):
     """(y, pre): y = activation(x w^T + bias) + residual.  x: [..., in], w: [out, in].  `save`: pre =
     x w^T + bias for linear_backward (else None).  `out` and `pre` may be given; `out` may be
-    the residual.  With `stream` the call runs there: what it reads has to be ready there, and stay until it is done; what it
+    the residual.  No autograd graph is recorded (linear_backward is the gradient): with tensors that require one, outside
+    torch.no_grad(), there is a warning.  With `stream` the call runs there: what it reads has to be ready there, and stay until it is done; what it
     makes (results, workspace) is `stream`'s memory."""
     _check_input(x, w, activation)
+    if (x.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad)
+            or (residual is not None and residual.requires_grad)) and torch.is_grad_enabled():
+        warnings.warn("linear records no autograd graph: gradients are linear_backward's; call it under torch.no_grad()", stacklevel=2)
     n, k = w.shape
     shape, dtype, device = x.shape, x.dtype, x.device
     m = shape[0] if len(shape) == 2 else math.prod(shape[:-1])

@@ -15,6 +15,7 @@ import math
 import warnings
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import binding as B
 from .bucket import _bytes, _stream_ptr
@@ -73,6 +74,16 @@ def _check_input(x, w, activation):
         raise ValueError("activation: one of %s is wanted" % ", ".join(k for k in _ACTS if k))
 
 
+def _counted(tensors):
+    """Of tensors that calls write to those whose version autograd counts, views that share a count once."""
+    once = {}
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            t = t._base if t._is_view() else t
+            once[id(t)] = t
+    return tuple(once.values())
+
+
 def _flat(t, rows, cols):
     """[..., cols] as [rows, cols] without a copy (ValueError if its strides need one)."""
     if t is None or t.dim() == 2:
@@ -125,6 +136,7 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     wp, ldw = _rows_of(w, "w", n, k, dtype, device)
     bp = _vector(bias, "bias", n, dtype, device)
     rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
+    given = (out, pre) if out is not None or pre is not None else None
     if out is None:
         out = _new(x, (*shape[:-1], n), dtype, stream)
         yp, ldy = out.data_ptr() or None, n
@@ -138,6 +150,8 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     a = B.tagc_linear(m, k, n, _TYPES[dtype], _ACTS[activation], xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp)
     ws, at = _work(B.tagc_linear_forward_workspace(a), x, stream)
     B.tagc_linear_forward(a, at, _stream_of(stream, device))
+    if given:  # (as torch's in-place operations do: a graph that kept one of them raises in its backward pass)
+        increment_version(_counted(given))
     return out, pre
 
 
@@ -157,6 +171,7 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     wp, ldw = _rows_of(w, "w", n, k, dtype, device)
     pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
     yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
+    given = (dx, dw, db) if dx is not None or dw is not None or db is not None else None
     if need_dx and dx is None:
         dx = _new(x, shape, dtype, stream)
         dp, ldd = dx.data_ptr() or None, k
@@ -167,6 +182,8 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
                            _vector(db, "db", n, dtype, device), 1 if accumulate else 0, 0)
     ws, at = _work(B.tagc_linear_backward_workspace(a), x, stream)
     B.tagc_linear_backward(a, at, _stream_of(stream, device))
+    if given:
+        increment_version(_counted(given))
     return dx
 
 
@@ -238,6 +255,8 @@ class AdamW:
                 r.bases = self._one(bases[i], "bases", i, self._blocks(g), (torch.int32,))
             if copies is not None and copies[i] is not None:
                 r.copy = self._one(copies[i], "copies", i, k, (torch.bfloat16,))
+        # (a graph that kept a parameter for its backward pass raises there behind a step, as behind torch's own optimizers)
+        self._written = _counted([*(self.params or ()), *(copies or ())])
         cfg = B.tagc_optim_config(beta1=betas[0], beta2=betas[1], eps=eps, grad_scale=grad_scale, max_norm=max_norm,
                                   seed=seed, moment_bits=bits)
         self.plan = B.tagc_optim_plan(cfg, rows)
@@ -301,6 +320,7 @@ class AdamW:
         if not step and not self._begun:  # (the control block would say that there is nothing to apply)
             raise RuntimeError("step() carries on what grad_norm() began: call that first, or give the step's number")
         B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control, self._on(stream))
+        increment_version(self._written)
 
     def unpack(self, stream=None):
         """(m, v): what 8-bit moments stand for, bfloat16, the tensors one behind the other."""

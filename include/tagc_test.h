@@ -28,6 +28,14 @@ void tagc_hash_host(uint32_t i, uint64_t seed, uint32_t j, uint32_t salt, uint32
  */
 uint32_t tagc_dense_pieces_host(uint32_t lo, uint32_t hi, uint32_t *at, uint32_t *n, uint32_t cap);
 
+/*
+ * Whether two matrices share a byte, as the linear layers' calls ask of operands and results:
+ * each `rows` rows of `width` bytes, `ld` bytes (>= width) from one to the next, from address a or
+ * b on (0: no matrix).  Host memory only, and none is read.
+ */
+int tagc_rows_meet_host(uint64_t a, uint64_t a_rows, uint64_t a_width, uint64_t a_ld, uint64_t b,
+                        uint64_t b_rows, uint64_t b_width, uint64_t b_ld);
+
 #ifdef __cplusplus
 }
 #endif

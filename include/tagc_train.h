@@ -166,10 +166,13 @@ typedef struct tagc_linear {
     const void *w; uint64_t ldw;    /* [out, in]                                          */
     const void *bias;               /* [out] or NULL                                      */
     const void *residual; uint64_t ldr; /* [rows, out] or NULL                            */
-    void *y; uint64_t ldy;          /* [rows, out]; may be the residual itself            */
-    void *pre; uint64_t ldp;        /* [rows, out] or NULL: x w^T + bias, for the backward pass */
+    void *y; uint64_t ldy;          /* [rows, out]; may be the residual itself, and must
+                                       share no element with another operand              */
+    void *pre; uint64_t ldp;        /* [rows, out] or NULL: x w^T + bias, for the backward pass; shares
+                                       none either (y only where both are the same numbers) */
 } tagc_linear;
 
+/* Of dx, dw and db none may share an element with another one or with an operand that is read. */
 typedef struct tagc_linear_grad {
     uint64_t rows, in, out;
     uint32_t dtype, activation;

@@ -16,6 +16,7 @@
 
 #include "device_utils.h"
 #include "tagc_internal.h"
+#include "tagc_test.h"
 #include "tagc_train.h"
 
 namespace tagc {
@@ -1388,6 +1389,45 @@ bool aligned_to(const void *p, uint64_t bytes) { return (reinterpret_cast<uintpt
 // a matrix that must or may be there
 bool good(const void *p, uint64_t ld, uint64_t cols, uint64_t bytes) { return !p || (aligned_to(p, bytes) && ld >= cols && ld < (1ull << 40)); }
 
+// Rows of a matrix as bytes in memory.
+struct Rows {
+    const char *p;
+    uint64_t rows, width, ld;
+    Rows(const void *at, uint64_t n, uint64_t bytes, uint64_t step) : p(static_cast<const char *>(at)), rows(at && bytes ? n : 0), width(bytes), ld(step)
+    {
+        if (rows > 1 && ld == width) {  // one row as well
+            width *= rows;
+            rows = 1;
+        }
+    }
+    const char *end() const { return p + (rows - 1) * ld + width; }
+    // whether one of them meets [from, to): the last that begins before `to` ends last
+    bool meets(const char *from, const char *to) const
+    {
+        if (to <= p) return false;
+        const uint64_t before = uint64_t(to - p - 1) / ld, last = before < rows ? before : rows - 1;
+        return p + last * ld + width > from;
+    }
+};
+
+// Whether two matrices share a byte.  Matrices side by side in one buffer, whose rows alternate, do not.
+bool meet(const Rows &a, const Rows &b)
+{
+    if (!a.rows || !b.rows || a.end() <= b.p || b.end() <= a.p) return false;
+    if (a.rows == 1) return b.meets(a.p, a.end());
+    if (b.rows == 1) return a.meets(b.p, b.end());
+    if (a.ld == b.ld) {
+        // row j of b begins `in` bytes into row j + down of a and what lies behind it, and may reach row j + down + 1
+        const int64_t d = b.p - a.p, ld = int64_t(a.ld), down = d >= 0 ? d / ld : -((-d + ld - 1) / ld), in = d - down * ld;
+        const int64_t ra = int64_t(a.rows), rb = int64_t(b.rows);
+        return (in < int64_t(a.width) && down < ra && down + rb > 0) || (in + int64_t(b.width) > ld && down + 1 < ra && down + 1 + rb > 0);
+    }
+    const Rows &few = a.rows < b.rows ? a : b, &many = a.rows < b.rows ? b : a;
+    for (uint64_t i = 0; i < few.rows; ++i)
+        if (many.meets(few.p + i * few.ld, few.p + i * few.ld + few.width)) return true;
+    return false;
+}
+
 int check_sizes(uint64_t rows, uint64_t in, uint64_t out, uint32_t dtype, uint32_t act)
 {
     if (dtype > TAGC_BF16 || act > TAGC_ACT_SILU) return TAGC_EINVAL;
@@ -1497,11 +1537,47 @@ int check_backward(const tagc_linear_grad *l, bool pointers)
     return TAGC_OK;
 }
 
+// Results are written while other workgroups read operands: they lie apart, but that y may be the residual, each of whose elements
+// is read where y's is written, and pre may be y where both are the same numbers.
+int check_apart(const tagc_linear *l)
+{
+    const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2, M = l->rows, K = l->in * e, N = l->out * e;
+    const Rows x(l->x, M, K, l->ldx * e), w(l->w, l->out, K, l->ldw * e), bias(l->bias, 1, N, N), residual(l->residual, M, N, l->ldr * e);
+    const Rows y(l->y, M, N, l->ldy * e), pre(l->pre, M, N, l->ldp * e);
+    const bool over = l->y == l->residual && (M <= 1 || l->ldy == l->ldr);
+    const bool one = l->y == l->pre && (M <= 1 || l->ldy == l->ldp) && l->activation == TAGC_ACT_NONE && !l->residual;
+    if (meet(y, x) || meet(y, w) || meet(y, bias) || (!over && meet(y, residual)) || meet(pre, x) || meet(pre, w) || meet(pre, bias) ||
+        meet(pre, residual) || (!one && meet(pre, y)))
+        return TAGC_EINVAL;
+    return TAGC_OK;
+}
+
+int check_apart(const tagc_linear_grad *l)
+{
+    const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2, M = l->rows, K = l->in * e, N = l->out * e;
+    const Rows in[] = {Rows(l->dw ? l->x : nullptr, M, K, l->ldx * e), Rows(l->dx ? l->w : nullptr, l->out, K, l->ldw * e),
+                       Rows(l->pre, M, N, l->ldp * e), Rows(l->dy, M, N, l->lddy * e)};
+    const Rows out[] = {Rows(l->dx, M, K, l->lddx * e), Rows(l->dw, l->out, K, l->lddw * e), Rows(l->db, 1, N, N)};
+    for (int i = 0; i < 3; ++i) {
+        for (const Rows &r : in)
+            if (meet(out[i], r)) return TAGC_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return TAGC_EINVAL;
+    }
+    return TAGC_OK;
+}
+
 }  // namespace
 
 }  // namespace tagc
 
 using namespace tagc;
+
+extern "C" int tagc_rows_meet_host(uint64_t a, uint64_t a_rows, uint64_t a_width, uint64_t a_ld, uint64_t b, uint64_t b_rows,
+                                   uint64_t b_width, uint64_t b_ld)
+{
+    return meet(Rows(reinterpret_cast<const void *>(a), a_rows, a_width, a_ld), Rows(reinterpret_cast<const void *>(b), b_rows, b_width, b_ld));
+}
 
 extern "C" int tagc_linear_forward_workspace(const tagc_linear *l, uint64_t *bytes)
 {
@@ -1530,7 +1606,8 @@ extern "C" int tagc_linear_backward_workspace(const tagc_linear_grad *l, uint64_
 extern "C" int tagc_linear_forward(const tagc_linear *l, void *workspace, void *stream)
 {
     uint64_t need = 0;
-    const int rc = tagc_linear_forward_workspace(l, &need);
+    int rc = tagc_linear_forward_workspace(l, &need);
+    if (!rc) rc = check_apart(l);
     if (rc) return rc;
     if (need && (!workspace || !aligned_to(workspace, 256))) return TAGC_EINVAL;
     Places w(workspace);
@@ -1541,7 +1618,8 @@ extern "C" int tagc_linear_forward(const tagc_linear *l, void *workspace, void *
 extern "C" int tagc_linear_backward(const tagc_linear_grad *l, void *workspace, void *stream)
 {
     uint64_t need = 0;
-    const int rc = tagc_linear_backward_workspace(l, &need);
+    int rc = tagc_linear_backward_workspace(l, &need);
+    if (!rc) rc = check_apart(l);
     if (rc) return rc;
     if (need && (!workspace || !aligned_to(workspace, 256))) return TAGC_EINVAL;
     Places w(workspace);

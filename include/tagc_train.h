@@ -96,7 +96,7 @@ typedef struct tagc_optim_s tagc_optim_t; /* opaque, host memory, immutable */
  * Builds the host-side plan of an optimizer over `tensors` (host, copied).  Errors: TAGC_EINVAL
  * (null or misaligned pointers, unknown type, group, bits, a value out of its range, bases
  * missing or given with 32-bit moments), TAGC_ESIZE (a tensor of 2^34 elements or more, 2^24 chunks of 4096
- * elements or more), TAGC_ENOMEM.  *out is owned by the caller: tagc_optim_destroy.
+ * elements or more, 2^23 with 8-bit moments), TAGC_ENOMEM.  *out is owned by the caller: tagc_optim_destroy.
  */
 int tagc_optim_plan(const tagc_optim_config *config, const tagc_tensor *tensors, uint32_t n_tensors,
                     tagc_optim_t **out);

@@ -29,6 +29,8 @@ constexpr uint64_t kMaxLength = 1ull << 34;                      // an element's
 // are the slower ones, 151 M 717 -> 733 us)
 constexpr uint32_t kCodeThreads = 512, kCodeSteps = 2;
 static_assert(kCodeThreads * 4 * kCodeSteps == kChunk, "the same chunks");
+// a launch has fewer than 2^32 threads: chunks of a plan are fewer than these, the norm's workgroups take many each
+constexpr uint64_t kMaxChunks = (1ull << 32) / kOptimThreads, kMaxCodeChunks = (1ull << 32) / kCodeThreads;
 static_assert(kChunk % TAGC_MOMENT_BLOCK == 0 && TAGC_MOMENT_BLOCK == 4 * 64, "a wave's step is a block");
 
 struct TensorDev {
@@ -572,11 +574,12 @@ extern "C" int tagc_optim_plan(const tagc_optim_config *cfg, const tagc_tensor *
     p->has_params = true;
     int rc = TAGC_OK;
     try {
-        uint64_t chunks = 0;
+        uint64_t chunks = 0, most = kMaxChunks;
         for (uint32_t i = 0; i < n_tensors && !rc; ++i) {
             rc = check_tensor(*cfg, tensors[i]);
             chunks += (tensors[i].length + kChunk - 1) / kChunk;
-            if (!rc && chunks >= (1ull << 24)) rc = TAGC_ESIZE;
+            if (tensors[i].param && cfg->moment_bits == 8) most = kMaxCodeChunks;
+            if (!rc && chunks >= most) rc = TAGC_ESIZE;
         }
         if (rc) {
             delete p;

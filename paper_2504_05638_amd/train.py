@@ -11,6 +11,7 @@ marshalling only; all arithmetic is the library's (include/tagc_train.h).
 """
 from __future__ import annotations
 
+import contextlib
 import math
 import warnings
 
@@ -41,6 +42,15 @@ def _stream_of(stream, device):
     return _stream_ptr(stream)
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _at(device):
+    """Calls are made with the tensors' device as the current one: launches go to its streams, and the library cuts work by
+    its compute units."""
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
 def _rows_of(t, name, rows, cols, dtype, device):
     """(address, elements from row to row) of a [rows, cols] matrix; (None, 0) for None."""
     if t is None:
@@ -65,7 +75,12 @@ def _vector(t, name, n, dtype, device):
     return t.data_ptr() or None
 
 
-def _check_input(x, w, activation):
+def _check_stream(stream, device):
+    _need(stream is None or stream.device == device, "stream: one of the tensors' device is wanted")
+
+
+def _check_input(x, w, activation, stream):
+    _check_stream(stream, x.device)
     if not x.is_cuda or x.dtype not in _TYPES:
         raise ValueError("x: a CUDA tensor of float32 or bfloat16 is wanted")
     if w.dim() != 2 or x.dim() < 2 or x.shape[-1] != w.shape[1]:
@@ -124,7 +139,7 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     the residual.  No autograd graph is recorded (linear_backward is the gradient): with tensors that require one, outside
     torch.no_grad(), there is a warning.  With `stream` the call runs there: what it reads has to be ready there, and stay until it is done; what it
     makes (results, workspace) is `stream`'s memory."""
-    _check_input(x, w, activation)
+    _check_input(x, w, activation, stream)
     if (x.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad)
             or (residual is not None and residual.requires_grad)) and torch.is_grad_enabled():
         warnings.warn("linear records no autograd graph: gradients are linear_backward's; call it under torch.no_grad()", stacklevel=2)
@@ -148,8 +163,9 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     else:
         pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
     a = B.tagc_linear(m, k, n, _TYPES[dtype], _ACTS[activation], xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp)
-    ws, at = _work(B.tagc_linear_forward_workspace(a), x, stream)
-    B.tagc_linear_forward(a, at, _stream_of(stream, device))
+    with _at(device):
+        ws, at = _work(B.tagc_linear_forward_workspace(a), x, stream)
+        B.tagc_linear_forward(a, at, _stream_of(stream, device))
     if given:  # (as torch's in-place operations do: a graph that kept one of them raises in its backward pass)
         increment_version(_counted(given))
     return out, pre
@@ -160,7 +176,7 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     """dx (None without need_dx).  With `dw` ([out, in], a view into a bucket's gradient) and `db` ([out])
     given, the weight's and the bias's gradient are written there, or added to what is there
     (accumulate).  `pre`: what linear(save=True) gave; None without an activation.  `stream`: as for linear."""
-    _check_input(x, w, activation)
+    _check_input(x, w, activation, stream)
     n, k = w.shape
     shape, dtype, device = x.shape, x.dtype, x.device
     m = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
@@ -180,8 +196,9 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     gp, ldg = _rows_of(dw, "dw", n, k, dtype, device)
     a = B.tagc_linear_grad(m, k, n, _TYPES[dtype], act, xp, ldx, wp, ldw, pp, ldp, yp, ldy, dp, ldd, gp, ldg,
                            _vector(db, "db", n, dtype, device), 1 if accumulate else 0, 0)
-    ws, at = _work(B.tagc_linear_backward_workspace(a), x, stream)
-    B.tagc_linear_backward(a, at, _stream_of(stream, device))
+    with _at(device):
+        ws, at = _work(B.tagc_linear_backward_workspace(a), x, stream)
+        B.tagc_linear_backward(a, at, _stream_of(stream, device))
     if given:
         increment_version(_counted(given))
     return dx
@@ -271,9 +288,11 @@ class AdamW:
         self.norm, self.factor, self.lr_scale = f[3], f[4], f[5]
         self._table, self._control = self.table.data_ptr(), self.control.data_ptr()
         # what is made here, and the streams that it has been used on: the one it belongs to first
-        self._made, self._streams = [self.table, self.control, *made], {_stream_ptr()}
-        B.tagc_optim_upload(self.plan, self._table, _stream_ptr())
-        torch.cuda.current_stream().synchronize()
+        home = torch.cuda.current_stream(self.device)
+        self._made, self._streams = [self.table, self.control, *made], {home.cuda_stream}
+        with _at(self.device):
+            B.tagc_optim_upload(self.plan, self._table, home.cuda_stream)
+        home.synchronize()
 
     @staticmethod
     def _blocks(g):
@@ -287,6 +306,7 @@ class AdamW:
     def _on(self, stream):
         """The address of the stream that a call runs on.  What was made here is not handed out again before the streams that
         used it are done, also where the object goes first."""
+        _check_stream(stream, self.device)
         at = _stream_of(stream, self.device)
         if at not in self._streams:
             s = stream if stream is not None else torch.cuda.current_stream(self.device)
@@ -308,7 +328,8 @@ class AdamW:
 
     def grad_norm(self, stream=None):
         """Begins a step; (norm, factor): device scalars, views of the control block."""
-        B.tagc_grad_norm(self.plan, self._table, self._control, self._on(stream))
+        with _at(self.device):
+            B.tagc_grad_norm(self.plan, self._table, self._control, self._on(stream))
         self._begun = True
         return self.norm, self.factor
 
@@ -319,13 +340,16 @@ class AdamW:
         _need(not step or not self._clips, "a given step is not clipped, and there is a max_norm: grad_norm(), then step()")
         if not step and not self._begun:  # (the control block would say that there is nothing to apply)
             raise RuntimeError("step() carries on what grad_norm() began: call that first, or give the step's number")
-        B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control, self._on(stream))
+        with _at(self.device):
+            B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control, self._on(stream))
         increment_version(self._written)
 
     def unpack(self, stream=None):
         """(m, v): what 8-bit moments stand for, bfloat16, the tensors one behind the other."""
+        _check_stream(stream, self.device)
         m, v = (_new(self.table, (self.sizes.n_elems,), torch.bfloat16, stream) for _ in range(2))
-        B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None, self._on(stream))
+        with _at(self.device):
+            B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None, self._on(stream))
         return m, v
 
     def close(self):

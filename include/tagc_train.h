@@ -32,6 +32,8 @@ extern "C" {
 
 /*
  * One tensor (all pointers dev, each aligned to its element).  A tensor with length 0 needs none.
+ * What is written (param, m, v, bases, copy) must share no element with anything else of the plan, but for the
+ * tensor's own gradient where that lies in the same place with the same bytes to an element.
  * Gradients may be what a layer's backward pass left (a segment of the flat gradient), or the
  * decoder's dense output from the segment's c-offset on (TAGC_F32).
  */

@@ -226,7 +226,8 @@ class AdamW:
     the updated parameters, or None (for single ones too).  `bits`: 32, or 8 (m, v: uint8 of the tensor's
     length; bases: int32, one per 256 elements).  `groups`: (lr, weight_decay) pairs, `group_of`: each
     tensor's.  `opt.groups = ...` changes them between steps.  Without params only grad_norm() can be
-    called.  The tensors must stay where they are: a gradient is written into, not replaced."""
+    called.  The tensors must stay where they are: a gradient is written into, not replaced.  What a step
+    writes must lie apart: each parameter is given once."""
 
     def __init__(self, params=None, grads=(), m=None, v=None, bases=None, copies=None, groups=((1e-3, 0.01),),
                  group_of=None, betas=(0.9, 0.999), eps=1e-8, bits=32, grad_scale=1.0, max_norm=0.0, seed=0,
@@ -272,6 +273,7 @@ class AdamW:
                 r.bases = self._one(bases[i], "bases", i, self._blocks(g), (torch.int32,))
             if copies is not None and copies[i] is not None:
                 r.copy = self._one(copies[i], "copies", i, k, (torch.bfloat16,))
+        self._check_apart(rows)
         # (a graph that kept a parameter for its backward pass raises there behind a step, as behind torch's own optimizers)
         self._written = _counted([*(self.params or ()), *(copies or ())])
         cfg = B.tagc_optim_config(beta1=betas[0], beta2=betas[1], eps=eps, grad_scale=grad_scale, max_norm=max_norm,
@@ -302,6 +304,29 @@ class AdamW:
         _need(t.dtype in types and t.device == self.device and t.numel() == k and (t.is_contiguous() or k <= 1),
               "%s[%d]: a contiguous tensor of %d, %s on %s, is wanted" % (name, i, k, " or ".join(map(str, types)), self.device))
         return t.data_ptr() if k else None
+
+    def _check_apart(self, rows):
+        """What a step writes is written by the workgroup that has read it, and by no other one: no parameter twice, no moments
+        of two.  (A gradient may lie in the place of something of its tensor's that it is replaced by element by element.)"""
+        spans = []
+        for r in rows:
+            if not r.length or not r.param:
+                continue
+            size, grad_size = (4, 2)[r.param_type], (4, 2)[r.grad_type]
+            own = [(r.param, r.length * size), (r.copy, r.length * 2), (r.bases, -(-r.length // B.TAGC_MOMENT_BLOCK) * 4)]
+            own += [(p, r.length * (self.bits // 8)) for p in (r.m, r.v)]
+            spans += [(p, p + n, True) for p, n in own if p]
+            if (r.grad, r.length * grad_size) not in own:
+                spans.append((r.grad, r.grad + r.length * grad_size, False))
+        spans.sort()
+        written = read = 0      # the ends of what began before
+        for start, end, write in spans:
+            _need(start >= written and not (write and start < read),
+                  "params, m, v, bases, copies and grads: what is written must lie apart from everything else")
+            if write:
+                written = max(written, end)
+            else:
+                read = max(read, end)
 
     def _on(self, stream):
         """The address of the stream that a call runs on.  What was made here is not handed out again before the streams that

@@ -39,3 +39,26 @@ def test_a_step_that_does_not_fit_its_word(step):
     with pytest.raises(ValueError, match="2\\^32"):
         opt.step(step)
     assert torch.equal(opt.params[0], torch.ones_like(opt.params[0]))
+
+
+def test_tensors_that_share_memory():
+    """Two workgroups would update the same elements, in no order."""
+    from paper_2504_05638_amd.train import AdamW
+    flat = torch.zeros(4 * 600, device="cuda")
+    g, h = torch.ones(600, device="cuda"), torch.ones(600, device="cuda")
+    a, b, c, d = torch.split(flat, 600)
+    half = torch.zeros(2 * 600, device="cuda", dtype=torch.bfloat16)
+    shared = half.view(torch.float32)       # 600 words under 1200 halves
+    for kw in (dict(params=[a, a], grads=[g, h]), dict(params=[flat[:600], flat[599:1199]], grads=[g, h]), dict(params=[a], grads=[g], m=[b], v=[b]),
+               dict(params=[a, b], grads=[g, h], m=[c, c], v=[d, flat.clone()[:600]]), dict(params=[a], grads=[flat[1:601]]),
+               dict(params=[shared], grads=[g], copies=[half[300:900]]), dict(params=[a, b], grads=[b, a])):
+        with pytest.raises(ValueError, match="apart"):
+            AdamW(**kw)
+    # one gradient of two parameters, empty tensors anywhere, neighbours, and a gradient that its parameter replaces
+    AdamW(params=[a, b], grads=[g, g], m=[c, d], v=[h, h.clone()])
+    AdamW(params=[a, a[:0], b], grads=[g, g[:0], h])
+    AdamW(grads=[g, g])
+    opt = AdamW(params=[d], grads=[d], groups=[(0.5, 0.0)], eps=0.25)
+    d.fill_(2.0)
+    opt.step(1)
+    assert torch.allclose(d, torch.full_like(d, 2.0 - 0.5 * 2 / 2.25))

@@ -36,6 +36,16 @@ uint32_t tagc_dense_pieces_host(uint32_t lo, uint32_t hi, uint32_t *at, uint32_t
 int tagc_rows_meet_host(uint64_t a, uint64_t a_rows, uint64_t a_width, uint64_t a_ld, uint64_t b,
                         uint64_t b_rows, uint64_t b_width, uint64_t b_ld);
 
+/*
+ * Which way a linear layer's product goes where its operands' rows lie one behind the other: path[0]
+ * is the kernel, path[1] the rows of its tiles, path[2] the parts of the sum (tiles and parts are 0 for
+ * TAGC_PATH_FEW).  Host memory only; without a device, for 256 compute units.
+ */
+enum { TAGC_PASS_FORWARD = 0, TAGC_PASS_DX = 1, TAGC_PASS_DW = 2 };
+enum { TAGC_PATH_FEW = 0, TAGC_PATH_PRODUCT = 1, TAGC_PATH_LONE = 2, TAGC_PATH_PRODUCT3 = 3, TAGC_PATH_RAW3 = 4 };
+int tagc_linear_path_host(uint32_t pass, uint64_t rows, uint64_t in, uint64_t out, uint32_t dtype,
+                          uint32_t *path);
+
 #ifdef __cplusplus
 }
 #endif

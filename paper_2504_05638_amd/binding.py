@@ -33,7 +33,8 @@ TAGC_ACT_NONE, TAGC_ACT_RELU, TAGC_ACT_GELU, TAGC_ACT_GELU_TANH, TAGC_ACT_SILU =
 EXPORTS = ["tagc_plan", "tagc_plan_destroy", "tagc_plan_sizes",
            "tagc_plan_upload", "tagc_compress", "tagc_compress_ranks", "tagc_compress_static", "tagc_feedback_apply", "tagc_aggregate",
            "tagc_decompress", "tagc_reduce_decompress", "tagc_profile_enable", "tagc_profile_read",
-           "tagc_hash_host", "tagc_dense_pieces_host", "tagc_rows_meet_host", "tagc_strerror",
+           "tagc_hash_host", "tagc_dense_pieces_host", "tagc_rows_meet_host",
+           "tagc_linear_path_host", "tagc_strerror",
            "tagc_optim_plan", "tagc_optim_destroy", "tagc_optim_plan_sizes", "tagc_optim_upload",
            "tagc_grad_norm", "tagc_adamw_step", "tagc_adamw_unpack",
            "tagc_linear_forward_workspace", "tagc_linear_backward_workspace",
@@ -233,6 +234,9 @@ def lib():
         L.tagc_linear_backward.argtypes = [C.POINTER(tagc_linear_grad), vp, vp]
         L.tagc_rows_meet_host.restype = C.c_int
         L.tagc_rows_meet_host.argtypes = [C.c_uint64] * 8
+        L.tagc_linear_path_host.restype = C.c_int
+        L.tagc_linear_path_host.argtypes = [C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint32,
+                                            C.POINTER(C.c_uint32)]
         L.tagc_strerror.restype = C.c_char_p
         L.tagc_strerror.argtypes = [C.c_int]
         _lib = L
@@ -367,6 +371,13 @@ def tagc_dense_pieces_host(lo, hi, cap=256):
 def tagc_rows_meet_host(a, b) -> bool:
     """a, b: (address, rows, width, ld) in bytes."""
     return bool(lib().tagc_rows_meet_host(*a, *b))
+
+
+def tagc_linear_path_host(which, rows, in_, out, dtype):
+    """(kernel, rows of a tile, parts of the sum) of pass `which` (0 forward, 1 dx, 2 dw)."""
+    path = (C.c_uint32 * 3)()
+    _check(lib().tagc_linear_path_host(which, rows, in_, out, dtype, path), "tagc_linear_path_host")
+    return tuple(path)
 
 
 # ------------------------------------------------- include/tagc_train.h

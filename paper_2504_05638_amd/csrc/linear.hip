@@ -1199,6 +1199,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void few_kernel(FewArgs a)
 // How a product is cut: tiles of `rows` by 256 (256 rows) or 128, and the parts of the sum that make up for few tiles.
 struct Shape {
     uint32_t rows, tiles_m, tiles_n, slabs, splits;
+    bool lone;  // bfloat16 tiles of 128 that each have a compute unit to themselves: lone_kernel
 };
 
 // By what the candidates would take, in us, from measurements at sizes from 333 by 1001 by 832 to 8192 by 8192 by 8192 (within 15 %
@@ -1248,6 +1249,7 @@ Shape shape_of(uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, bool turned_p
     }
     s.slabs = uint32_t((slabs + splits - 1) / splits);
     s.splits = uint32_t((slabs + s.slabs - 1) / s.slabs);
+    s.lone = dtype == TAGC_BF16 && s.rows == 128 && uint64_t(s.tiles_m) * s.tiles_n * s.splits <= cus;
     return s;
 }
 
@@ -1362,7 +1364,7 @@ void launch_product(const Operand &p, const Operand &q, uint64_t m, uint64_t n, 
             }
         } else {
             if (f.rows == 256) product_kernel<2, 4, 8, 4, PT, QT><<<grid, 512, 0, s>>>(a);
-            else if (f.rows == 128 && grid <= uint32_t(device_cu_count())) lone_kernel<PT, QT><<<grid, 512, 0, s>>>(a);  // (as shape_of has it)
+            else if (f.lone) lone_kernel<PT, QT><<<grid, 512, 0, s>>>(a);
             else if (f.rows == 128) product_kernel<2, 4, 4, 2, PT, QT><<<grid, 512, 0, s>>>(a);
             else if constexpr (!PT) {
                 if (f.rows == 64) product_kernel<1, 4, 4, 2, PT, QT><<<grid, 256, 0, s>>>(a);
@@ -1577,6 +1579,23 @@ extern "C" int tagc_rows_meet_host(uint64_t a, uint64_t a_rows, uint64_t a_width
                                    uint64_t b_width, uint64_t b_ld)
 {
     return meet(Rows(reinterpret_cast<const void *>(a), a_rows, a_width, a_ld), Rows(reinterpret_cast<const void *>(b), b_rows, b_width, b_ld));
+}
+
+extern "C" int tagc_linear_path_host(uint32_t pass, uint64_t rows, uint64_t in, uint64_t out, uint32_t dtype, uint32_t *path)
+{
+    if (!path || pass > TAGC_PASS_DW) return TAGC_EINVAL;
+    const int rc = check_sizes(rows, in, out, dtype, TAGC_ACT_NONE);
+    if (rc) return rc;
+    path[0] = path[1] = path[2] = 0;
+    if (pass == TAGC_PASS_FORWARD && rows <= kFewRows) return TAGC_OK;
+    const Shape f = pass == TAGC_PASS_FORWARD ? shape_of(rows, out, in, dtype, false)
+                    : pass == TAGC_PASS_DX    ? shape_of(rows, in, out, dtype, false)
+                                              : shape_of(out, in, rows, dtype, true);
+    if (dtype == TAGC_BF16) path[0] = f.lone ? TAGC_PATH_LONE : TAGC_PATH_PRODUCT;
+    else path[0] = pass == TAGC_PASS_FORWARD && raw_pays(rows, out) ? TAGC_PATH_RAW3 : TAGC_PATH_PRODUCT3;
+    path[1] = f.rows;
+    path[2] = f.splits;
+    return TAGC_OK;
 }
 
 extern "C" int tagc_linear_forward_workspace(const tagc_linear *l, uint64_t *bytes)

@@ -34,6 +34,7 @@ def _need(condition, what):
 # (the address of the device's current stream, without the object around it where torch offers that: a
 # third of what a small call costs the host)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream_of(stream, device):
@@ -45,10 +46,20 @@ def _stream_of(stream, device):
 _HERE = contextlib.nullcontext()
 
 
-def _at(device):
+def _at(device, stream=None):
     """Calls are made with the tensors' device as the current one: launches go to its streams, and the library cuts work by
-    its compute units."""
-    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    its compute units.  Under a given stream what they make is that stream's own: memory of the current stream's may still
+    be in use there."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return _HERE if _current_device() == device.index else torch.cuda.device(device)
+
+
+def _hand_over(user, *made):
+    """What was made under a given stream is not used again there before what `user`, the caller's stream, does with it is done."""
+    for t in made:
+        if t is not None:
+            t.record_stream(user)
 
 
 def _rows_of(t, name, rows, cols, dtype, device):
@@ -76,11 +87,12 @@ def _vector(t, name, n, dtype, device):
 
 
 def _check_stream(stream, device):
-    _need(stream is None or stream.device == device, "stream: one of the tensors' device is wanted")
+    _need(stream.device == device, "stream: one of the tensors' device is wanted")
 
 
 def _check_input(x, w, activation, stream):
-    _check_stream(stream, x.device)
+    if stream is not None:
+        _check_stream(stream, x.device)
     if not x.is_cuda or x.dtype not in _TYPES:
         raise ValueError("x: a CUDA tensor of float32 or bfloat16 is wanted")
     if w.dim() != 2 or x.dim() < 2 or x.shape[-1] != w.shape[1]:
@@ -109,27 +121,11 @@ def _flat(t, rows, cols):
         raise ValueError(str(e)) from None
 
 
-def _new(like, shape, dtype, stream):
-    """A tensor that a call writes on `stream` (None: the current one) and hands to its caller.  It is `stream`'s own: memory of
-    the current stream's may still be in use there.  It is not used again before what the current stream does with it is done."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    user = torch.cuda.current_stream(like.device)
-    with torch.cuda.stream(stream):
-        t = like.new_empty(shape, dtype=dtype)
-    t.record_stream(user)
-    return t
-
-
-def _work(nbytes, x, stream):
-    """A call's workspace (its tensor and its address), `stream`'s own: reused behind the call only."""
+def _work(nbytes, x):
+    """A call's workspace (its tensor and its address), the current stream's own: reused behind the call only."""
     if not nbytes:
         return None, None
-    if stream is None:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-    else:
-        with torch.cuda.stream(stream):
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
     return ws, ws.data_ptr()
 
 
@@ -137,8 +133,8 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     """(y, pre): y = activation(x w^T + bias) + residual.  x: [..., in], w: [out, in].  `save`: pre =
     x w^T + bias for linear_backward (else None).  `out` and `pre` may be given; `out` may be
     the residual.  No autograd graph is recorded (linear_backward is the gradient): with tensors that require one, outside
-    torch.no_grad(), there is a warning.  With `stream` the call runs there: what it reads has to be ready there, and stay until it is done; what it
-    makes (results, workspace) is `stream`'s memory."""
+    torch.no_grad(), there is a warning.  With `stream` the call runs there: what it reads has to be ready there, and stay
+    until it is done; what it makes (results, workspace) is `stream`'s memory."""
     _check_input(x, w, activation, stream)
     if (x.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad)
             or (residual is not None and residual.requires_grad)) and torch.is_grad_enabled():
@@ -151,22 +147,23 @@ def linear(x, w, bias=None, residual=None, activation=None, save=False, out=None
     wp, ldw = _rows_of(w, "w", n, k, dtype, device)
     bp = _vector(bias, "bias", n, dtype, device)
     rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
-    given = (out, pre) if out is not None or pre is not None else None
-    if out is None:
-        out = _new(x, (*shape[:-1], n), dtype, stream)
-        yp, ldy = out.data_ptr() or None, n
-    else:
-        yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
-    if save and pre is None:
-        pre = _new(x, (*shape[:-1], n), dtype, stream)
-        pp, ldp = pre.data_ptr() or None, n
-    else:
-        pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
-    a = B.tagc_linear(m, k, n, _TYPES[dtype], _ACTS[activation], xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp)
-    with _at(device):
-        ws, at = _work(B.tagc_linear_forward_workspace(a), x, stream)
+    yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
+    pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
+    given, user = (out, pre), torch.cuda.current_stream(device) if stream is not None else None
+    with _at(device, stream):
+        if out is None:
+            out = x.new_empty((*shape[:-1], n))
+            yp, ldy = out.data_ptr() or None, n
+        if save and pre is None:
+            pre = x.new_empty((*shape[:-1], n))
+            pp, ldp = pre.data_ptr() or None, n
+        a = B.tagc_linear(m, k, n, _TYPES[dtype], _ACTS[activation], xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp)
+        ws, at = _work(B.tagc_linear_forward_workspace(a), x)
         B.tagc_linear_forward(a, at, _stream_of(stream, device))
-    if given:  # (as torch's in-place operations do: a graph that kept one of them raises in its backward pass)
+    if stream is not None:
+        _hand_over(user, out if given[0] is None else None, pre if given[1] is None else None)
+    if given[0] is not None or given[1] is not None:
+        # (as torch's in-place operations do: a graph that kept one of them raises in its backward pass)
         increment_version(_counted(given))
     return out, pre
 
@@ -187,19 +184,21 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     wp, ldw = _rows_of(w, "w", n, k, dtype, device)
     pp, ldp = _rows_of(_flat(pre, m, n), "pre", m, n, dtype, device)
     yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
-    given = (dx, dw, db) if dx is not None or dw is not None or db is not None else None
-    if need_dx and dx is None:
-        dx = _new(x, shape, dtype, stream)
-        dp, ldd = dx.data_ptr() or None, k
-    else:
-        dp, ldd = _rows_of(_flat(dx, m, k), "dx", m, k, dtype, device)
+    dp, ldd = _rows_of(_flat(dx, m, k), "dx", m, k, dtype, device)
     gp, ldg = _rows_of(dw, "dw", n, k, dtype, device)
-    a = B.tagc_linear_grad(m, k, n, _TYPES[dtype], act, xp, ldx, wp, ldw, pp, ldp, yp, ldy, dp, ldd, gp, ldg,
-                           _vector(db, "db", n, dtype, device), 1 if accumulate else 0, 0)
-    with _at(device):
-        ws, at = _work(B.tagc_linear_backward_workspace(a), x, stream)
+    bp = _vector(db, "db", n, dtype, device)
+    given, user = (dx, dw, db), torch.cuda.current_stream(device) if stream is not None else None
+    with _at(device, stream):
+        if need_dx and dx is None:
+            dx = x.new_empty(shape)
+            dp, ldd = dx.data_ptr() or None, k
+        a = B.tagc_linear_grad(m, k, n, _TYPES[dtype], act, xp, ldx, wp, ldw, pp, ldp, yp, ldy, dp, ldd, gp, ldg, bp,
+                               1 if accumulate else 0, 0)
+        ws, at = _work(B.tagc_linear_backward_workspace(a), x)
         B.tagc_linear_backward(a, at, _stream_of(stream, device))
-    if given:
+    if stream is not None:
+        _hand_over(user, dx if given[0] is None else None)
+    if given[0] is not None or dw is not None or db is not None:
         increment_version(_counted(given))
     return dx
 
@@ -331,7 +330,8 @@ class AdamW:
     def _on(self, stream):
         """The address of the stream that a call runs on.  What was made here is not handed out again before the streams that
         used it are done, also where the object goes first."""
-        _check_stream(stream, self.device)
+        if stream is not None:
+            _check_stream(stream, self.device)
         at = _stream_of(stream, self.device)
         if at not in self._streams:
             s = stream if stream is not None else torch.cuda.current_stream(self.device)
@@ -361,9 +361,10 @@ class AdamW:
     def step(self, step=0, stream=None):
         """One step: the one that grad_norm() began, its learning rates times the device scalar
         `lr_scale`; or, with `step` > 0, that one, with the groups' learning rates (not of an optimizer that clips)."""
-        _need(0 <= step < 1 << 32, "step: 1 or more, less than 2^32, or 0 for the one that grad_norm() began")
-        _need(not step or not self._clips, "a given step is not clipped, and there is a max_norm: grad_norm(), then step()")
-        if not step and not self._begun:  # (the control block would say that there is nothing to apply)
+        if step:
+            _need(0 < step < 1 << 32, "step: 1 or more, less than 2^32, or 0 for the one that grad_norm() began")
+            _need(not self._clips, "a given step is not clipped, and there is a max_norm: grad_norm(), then step()")
+        elif not self._begun:  # (the control block would say that there is nothing to apply)
             raise RuntimeError("step() carries on what grad_norm() began: call that first, or give the step's number")
         with _at(self.device):
             B.tagc_adamw_step(self.plan, self._table, self._group_array, step, self._control, self._on(stream))
@@ -371,10 +372,12 @@ class AdamW:
 
     def unpack(self, stream=None):
         """(m, v): what 8-bit moments stand for, bfloat16, the tensors one behind the other."""
-        _check_stream(stream, self.device)
-        m, v = (_new(self.table, (self.sizes.n_elems,), torch.bfloat16, stream) for _ in range(2))
-        with _at(self.device):
-            B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None, self._on(stream))
+        at, user = self._on(stream), torch.cuda.current_stream(self.device)
+        with _at(self.device, stream):
+            m, v = (torch.empty(self.sizes.n_elems, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            B.tagc_adamw_unpack(self.plan, self._table, m.data_ptr() or None, v.data_ptr() or None, at)
+        if stream is not None:
+            _hand_over(user, m, v)
         return m, v
 
     def close(self):

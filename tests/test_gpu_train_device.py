@@ -25,7 +25,7 @@ def test_calls_are_made_with_the_tensors_device(monkeypatch):
 
     x, w, dy = torch.randn(70, 30, device="cuda"), torch.randn(20, 30, device="cuda"), torch.randn(70, 20, device="cuda")
     g = torch.randn(500, device="cuda")
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: on[-1])
+    monkeypatch.setattr(train, "_current_device", lambda: on[-1])
     monkeypatch.setattr(torch.cuda, "device", Device)
     for name in CALLS:
         call = getattr(train.B, name)

@@ -174,7 +174,8 @@ typedef struct tagc_linear {
                                        none either (y only where both are the same numbers) */
 } tagc_linear;
 
-/* Of dx, dw and db none may share an element with another one or with an operand that is read. */
+/* Of dx, dw and db none may share an element with another one or with an operand that is read, but for
+ * dy and pre where there is an activation, and for float32 operands. */
 typedef struct tagc_linear_grad {
     uint64_t rows, in, out;
     uint32_t dtype, activation;

@@ -1554,11 +1554,13 @@ int check_apart(const tagc_linear *l)
     return TAGC_OK;
 }
 
+// What is laid out anew has been read before the first result is written: float32 operands, and dy and pre behind an activation.
 int check_apart(const tagc_linear_grad *l)
 {
     const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2, M = l->rows, K = l->in * e, N = l->out * e;
-    const Rows in[] = {Rows(l->dw ? l->x : nullptr, M, K, l->ldx * e), Rows(l->dx ? l->w : nullptr, l->out, K, l->ldw * e),
-                       Rows(l->pre, M, N, l->ldp * e), Rows(l->dy, M, N, l->lddy * e)};
+    const bool lies = l->dtype == TAGC_BF16;
+    const Rows in[] = {Rows(lies && l->dw ? l->x : nullptr, M, K, l->ldx * e), Rows(lies && l->dx ? l->w : nullptr, l->out, K, l->ldw * e),
+                       Rows(lies && !l->pre ? l->dy : nullptr, M, N, l->lddy * e)};
     const Rows out[] = {Rows(l->dx, M, K, l->lddx * e), Rows(l->dw, l->out, K, l->lddw * e), Rows(l->db, 1, N, N)};
     for (int i = 0; i < 3; ++i) {
         for (const Rows &r : in)

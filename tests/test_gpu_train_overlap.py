@@ -34,8 +34,8 @@ def test_side_by_side(dtype):
 def test_over_one_another():
     from paper_2504_05638_amd.binding import TagcError
     from paper_2504_05638_amd.train import linear, linear_backward
-    x, w = torch.randn(64, 48, device="cuda"), torch.randn(48, 48, device="cuda")
-    buf = torch.randn(65, 48, device="cuda")
+    x, w = torch.randn(64, 48, device="cuda").bfloat16(), torch.randn(48, 48, device="cuda").bfloat16()
+    buf = torch.randn(65, 48, device="cuda").bfloat16()
     before = [t.clone() for t in (x, w, buf)]
     for kw in (dict(out=x), dict(residual=buf[:64], out=buf[1:]), dict(save=True, pre=buf[1:], out=buf[:64]), dict(save=True, pre=x)):
         with pytest.raises(TagcError):
@@ -44,3 +44,30 @@ def test_over_one_another():
         with pytest.raises(TagcError):
             linear_backward(buf[1:], x, w, **kw)
     assert all(torch.equal(a, b) for a, b in zip(before, (x, w, buf)))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_in_the_place_of_what_has_been_read(dtype, shift):
+    """Behind an activation dx may lie over dy or pre; in float32 gradients may lie over operands."""
+    from paper_2504_05638_amd.train import linear_backward
+    M, K = 500, 320
+
+    def make():
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(4)
+        return [torch.randn(n * K + shift, generator=gen, device="cuda").to(dtype)[shift:].view(n, K) for n in (M, M, M, K)]
+
+    def run(place, act):
+        dy, pre, x, w = make()
+        dx = {"dy": dy, "pre": pre, "x": x, "none": None}[place]
+        dw = w if place == "x" else torch.empty_like(w)
+        db = torch.empty(K, device="cuda", dtype=dtype)
+        return linear_backward(dy, x, w, pre if act else None, activation=act, dx=dx, dw=dw, db=db), dw, db
+
+    want = run("none", "gelu")
+    for place in ("dy", "pre"):
+        assert all(torch.equal(a, b) for a, b in zip(run(place, "gelu"), want))
+    if dtype == torch.float32:
+        for act in (None, "silu"):
+            assert all(torch.equal(a, b) for a, b in zip(run("x", act), run("none", act)))

@@ -42,10 +42,21 @@ def test_forward(bad):
     assert _refused(B.tagc_linear_forward, B.tagc_linear(**d))
 
 
-@pytest.mark.parametrize("bad", [dict(dx=X), dict(dx=W), dict(dx=D), dict(dx=P), dict(dw=W), dict(dw=X), dict(dw=D + 2), dict(db=P), dict(db=Y), dict(db=R + 100),
-                                 dict(dw=Y + 512), dict(dx=D + 99 * 128)])
-def test_backward(bad):
-    d = dict(rows=100, in_=128, out=64, dtype=B.TAGC_BF16, activation=1, x=X, ldx=128, w=W, ldw=128, pre=P, ldp=64, dy=D, lddy=64, dx=Y, lddx=128,
-             dw=R, lddw=128, db=7 << 30)
+OVER = [dict(dx=X), dict(dx=W), dict(dw=W), dict(dw=X), dict(db=Y), dict(db=R + 100), dict(dw=Y + 512)]
+OVER_DY = [dict(dx=D), dict(dw=D + 2), dict(dx=D + 99 * 128)]      # (behind an activation dy and pre have been read before)
+
+
+@pytest.mark.parametrize("bad,activation", [(o, 0) for o in OVER + OVER_DY] + [(o, 1) for o in OVER])
+def test_backward(bad, activation):
+    d = dict(rows=100, in_=128, out=64, dtype=B.TAGC_BF16, x=X, ldx=128, w=W, ldw=128, dy=D, lddy=64, dx=Y, lddx=128, dw=R, lddw=128, db=7 << 30)
+    if activation:
+        d.update(activation=activation, pre=P, ldp=64)
+    d.update(bad)
+    assert _refused(B.tagc_linear_backward, B.tagc_linear_grad(**d))
+
+
+@pytest.mark.parametrize("bad", [dict(dx=R), dict(db=Y), dict(db=R + 100)])
+def test_backward_float32(bad):
+    d = dict(rows=100, in_=128, out=64, dtype=B.TAGC_F32, x=X, ldx=128, w=W, ldw=128, dy=D, lddy=64, dx=Y, lddx=128, dw=R, lddw=128, db=7 << 30)
     d.update(bad)
     assert _refused(B.tagc_linear_backward, B.tagc_linear_grad(**d))

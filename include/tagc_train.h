@@ -198,7 +198,7 @@ int tagc_linear_backward_workspace(const tagc_linear_grad *l, uint64_t *bytes);
  * z = x w^T + bias with float32 sums; pre = z; y = act(z) + residual, each rounded once.  bfloat16
  * products are exact.  float32 operands are taken as three bfloat16 numbers each, of which six products are
  * added: what is left out is at most 2^-22 of a product and mostly 2^-24, of either sign, like a
- * rounding; an infinity in x or w makes the sums it enters NaN.
+ * rounding; an infinity in x or w makes the sums it enters NaN, and operands under some 2^-100 lose their last bits.
  */
 int tagc_linear_forward(const tagc_linear *l, void *workspace, void *stream);
 

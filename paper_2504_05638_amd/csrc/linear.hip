@@ -31,7 +31,7 @@ constexpr uint32_t kSlab = 64;        // k's of a stage in local memory: 128 byt
 constexpr uint32_t kPackRows = 64;
 constexpr uint32_t kParts = 3;        // bfloat16 numbers that a float32 is taken apart into
 // rows up to which few_kernel goes; from there on tiles are faster (weights of 4096 by 11008, 17, 32, 64 rows, us: bfloat16
-// 32, 35, 48, as tiles 23, 24, 26; float32 76, 95, 164, as tiles 80, 80, 84)
+// 32, 35, 48, as tiles 23, 24, 26; float32 76, 95, 164, as tiles 74, 75, 80)
 constexpr uint32_t kFewRows = 16;
 
 constexpr uint64_t kMaxSide = 1u << 22;  // rows, features (in float32 a quarter) and strides as they lie are fewer
@@ -538,8 +538,8 @@ struct Side<true, R, THREADS> {
 // part: by then all have read the slab's last pieces, its stage is free for the slab after the next, and
 // the next one has come.
 //
-// Bound by the matrix units, and by the power they draw: at 8192 by 8192 by 8192 they are busy for 72 % of the cycles,
-// and the clock falls to some 1.6 GHz: 844 us, 1302 TFLOP/s.  What was measured on the way (TFLOP/s there): products in the order the
+// Bound by the matrix units, and by the power they draw: at 8192 by 8192 by 8192 they are busy for 71 % of the cycles,
+// and the clock falls to some 1.7 GHz: 833 us, 1320 TFLOP/s.  What was measured on the way (TFLOP/s there): products in the order the
 // compiler found 1113, woven with the reads 1196; 32 x 32 x 16 instructions, which move their sums twice as often, 1196, 16 x 16 x 32 1236;
 // four waves of 128 by 128 1163; eight waves in two groups that take turns at reading and multiplying 1041; slabs
 // of 32 in a ring of four stages, whose loads take half a cache line, 1172.
@@ -843,7 +843,7 @@ __device__ inline __attribute__((always_inline)) void six_products(f32x4 (&acc)[
 // products run, from three stages, two of which are on their way while the third is multiplied.
 //
 // Bound by the matrix units and their power at large sizes (4096 by 4096 by 4096: 677 us, 203
-// TFLOP/s, 1220 of bfloat16 products).  A bfloat16
+// TFLOP/s, 1220 of bfloat16 products; the units are busy for 69 % of the cycles at 1.8 GHz).  A bfloat16
 // product of six times as many k's, tile of 256 by 256, fetches and reads each part two or three times: 616 us there, but 70
 // instead of 56 at 1024 by 4096 by 1024, 146 instead of 114 for both gradients at 1024 by 1024 by 4096, and 755 instead of 665 for
 // those at 8192 by 1024 by 4096.

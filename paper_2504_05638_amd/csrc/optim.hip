@@ -350,7 +350,7 @@ __device__ inline bool zero_byte(uint32_t x) { return ((x - 0x01010101u) & ~x & 
 // A wave's step is a block: its 64 lanes hold four neighbours each, and the base takes one maximum over the wave.
 //
 // Bound by bytes where weights are float32 (202 M with bfloat16 gradients and copies, 16 bytes each, 540 us, 6.0 TB/s), by
-// the VALU where they are not (10 bytes each, 393 us, 5.1 TB/s): some 50 instructions an element, after root and
+// the VALU where they are not (10 bytes each, 363 us, 5.6 TB/s): some 50 instructions an element, after root and
 // reciprocal by the hardware (659 -> 587 us, 535 -> 464), the maximum of both moments at once without local memory, and
 // what is seldom behind branches (587 -> 549, 464 -> 401).
 template <typename P, typename G, bool SMALL_EPS>

@@ -1,10 +1,16 @@
 /*
  * libtagc -- the two ends of a data-parallel step that the exchange (tagc.h) lies between, for
- * AMD MI355X (gfx950): the linear layers whose weight gradients fill a bucket, and the
- * optimizer that takes the summed gradient.
+ * AMD MI355X (gfx950): the layers whose weight gradients fill a bucket -- linear ones, norms, the
+ * tokens' table, the loss over the vocabulary --, and the optimizer that takes the summed gradient.
  *
  *   tagc_linear_forward     y = act(x w^T + b) + r
  *   tagc_linear_backward    dx, and dw and db written into (or added to) the bucket's gradient
+ *   tagc_norm_forward       layer norm or RMS norm of rows, and their statistics
+ *   tagc_norm_backward      dx, with the gradient that came around the layer, dw and db
+ *   tagc_embedding_forward  rows of a table, scaled
+ *   tagc_embedding_backward the table's gradient
+ *   tagc_loss_forward       cross entropy, or a teacher's divergence, of x w^T over a vocabulary
+ *   tagc_loss_backward      dx and dw of it
  *   tagc_grad_norm          2-norm over all gradients, clip factor, step count, on the device
  *   tagc_adamw_step         AdamW over many tensors in one launch, moments in 32 bits or in 8
  *   tagc_adamw_unpack       what 8-bit moments stand for
@@ -208,6 +214,155 @@ int tagc_linear_forward(const tagc_linear *l, void *workspace, void *stream);
  * gradient is dy.
  */
 int tagc_linear_backward(const tagc_linear_grad *l, void *workspace, void *stream);
+
+/* ------------------------------------------------------------------ norms */
+
+enum { TAGC_NORM_LAYER = 0, TAGC_NORM_RMS = 1 };
+
+#define TAGC_MAX_NORM_WIDTH 16384u
+
+/*
+ * Rows of one type (TAGC_F32 | TAGC_BF16), contiguous, `ld*` elements from one to the next; w and b of
+ * the same type.  Pointers are dev, aligned to their element.  y may be x itself; otherwise what is
+ * written shares no element with another operand.
+ */
+typedef struct tagc_norm {
+    uint64_t rows, width;           /* rows < 2^31, width <= TAGC_MAX_NORM_WIDTH           */
+    uint32_t dtype, kind;           /* TAGC_NORM_*                                        */
+    double eps;                     /* >= 0, finite                                       */
+    const void *x; uint64_t ldx;    /* [rows, width]                                      */
+    const void *w, *b;              /* [width] or NULL: 1 and 0; no b with TAGC_NORM_RMS   */
+    void *y; uint64_t ldy;          /* [rows, width]                                      */
+    float *stats;                   /* [rows][2] or NULL: mean (0 with TAGC_NORM_RMS) and 1 / sqrt(variance
+                                       + eps), for the backward pass                      */
+} tagc_norm;
+
+/* dx may be dy, x or the residual itself; otherwise what is written shares no element with another operand. */
+typedef struct tagc_norm_grad {
+    uint64_t rows, width;
+    uint32_t dtype, kind;
+    const void *x; uint64_t ldx;    /* [rows, width]                                      */
+    const void *w;                  /* [width] or NULL: 1                                 */
+    const float *stats;             /* [rows][2] as forward left it                       */
+    const void *dy; uint64_t lddy;  /* [rows, width]                                      */
+    const void *residual; uint64_t ldr; /* [rows, width] or NULL: added to dx             */
+    void *dx; uint64_t lddx;        /* [rows, width] or NULL                              */
+    void *dw, *db;                  /* [width] or NULL: places in the bucket's gradient; no db with
+                                       TAGC_NORM_RMS                                      */
+    uint32_t accumulate;            /* 1: dw and db are added to what is there            */
+    uint32_t reserved;              /* must be 0                                          */
+} tagc_norm_grad;
+
+/* y = (x - mean) * r * w + b, r = 1 / sqrt(mean of (x - mean)^2 + eps), mean 0 with TAGC_NORM_RMS: in float32, rounded once. */
+int tagc_norm_forward(const tagc_norm *n, void *stream);
+
+/* Bytes of workspace (dev, 256-byte aligned, contents do not matter) that the call needs. */
+int tagc_norm_backward_workspace(const tagc_norm_grad *n, uint64_t *bytes);
+
+/*
+ * h = (x - mean) r, u = dy w: dx = r (u - mean u - h mean(u h)) + residual (without mean u with TAGC_NORM_RMS);
+ * dw (+)= the sum of dy h over the rows, db (+)= that of dy.  Sums in float32, in an order that depends on nothing but
+ * the sizes and the number of compute units.
+ */
+int tagc_norm_backward(const tagc_norm_grad *n, void *workspace, void *stream);
+
+/* ------------------------------------------------------------------ embeddings */
+
+enum { TAGC_ID_I32 = 0, TAGC_ID_I64 = 1 };
+
+/*
+ * Rows of a table.  Table, y and residual are of one type (TAGC_F32 | TAGC_BF16), rows contiguous.  Ids are int32 or int64,
+ * one behind the other; one outside [0, vocab) is no token: its row of the table counts as zeros, and it has no part in a gradient.
+ */
+typedef struct tagc_embedding {
+    uint64_t rows, width, vocab;    /* ids, features, rows of the table; each < 2^22       */
+    uint32_t dtype, id_type;        /* TAGC_F32 | TAGC_BF16; TAGC_ID_*                    */
+    double scale;                   /* finite                                             */
+    const void *ids;                /* [rows]                                             */
+    const void *table; uint64_t ldt; /* [vocab, width]                                    */
+    const void *residual; uint64_t ldr; /* [rows, width] or NULL                          */
+    void *y; uint64_t ldy;          /* [rows, width]; may be the residual itself, and shares no element
+                                       with another operand otherwise                     */
+} tagc_embedding;
+
+typedef struct tagc_embedding_grad {
+    uint64_t rows, width, vocab;
+    uint32_t dtype, id_type;
+    double scale;
+    const void *ids;                /* [rows]                                             */
+    const void *dy; uint64_t lddy;  /* [rows, width]                                      */
+    void *dtable; uint64_t ldt;     /* [vocab, width]: a place in the bucket's gradient; shares no
+                                       element with dy or ids                             */
+    uint32_t accumulate;            /* 1: added to what is there                          */
+    uint32_t reserved;              /* must be 0                                          */
+} tagc_embedding_grad;
+
+/* y[t] = scale * table[ids[t]] + residual[t], rounded once. */
+int tagc_embedding_forward(const tagc_embedding *e, void *stream);
+
+int tagc_embedding_backward_workspace(const tagc_embedding_grad *e, uint64_t *bytes);
+
+/*
+ * dtable[v] (+)= scale * the sum of dy[t] over the t with ids[t] = v, in float32, in an order that the ids alone decide (no
+ * atomics): results repeat bit for bit.  Rows of tokens that there are none of become zeros, or stay with accumulate.
+ */
+int tagc_embedding_backward(const tagc_embedding_grad *e, void *workspace, void *stream);
+
+/* ------------------------------------------------------------------ losses over a vocabulary */
+
+#define TAGC_MAX_TERMS 1024u
+
+/*
+ * The loss of a layer's output x [rows, in] against a vocabulary w [vocab, in], both of one type (TAGC_F32 | TAGC_BF16), whose
+ * scores s = x w^T / temperature are held nowhere as a whole.  Every row has `terms` tokens that its target distribution q is on:
+ *   logits NULL   one term, q = 1: softmax cross entropy
+ *   logits given  q = softmax(logits / temperature) over the row's terms: distillation
+ * A term outside [0, vocab), or one whose logit is -infinity, is none; a token that is a row's term twice has both weights.  A row
+ * without a term has loss 0, `saved` 0 and no part in a gradient; its x is not looked at and may be anything.
+ */
+typedef struct tagc_loss {
+    uint64_t rows, in, vocab;       /* in, vocab >= 1; limits as for tagc_linear          */
+    uint32_t terms;                 /* 1 .. TAGC_MAX_TERMS; 1 without logits              */
+    uint32_t dtype, id_type;        /* TAGC_F32 | TAGC_BF16; TAGC_ID_*                    */
+    uint32_t reserved;              /* must be 0                                          */
+    double temperature;             /* > 0, finite; 1 for plain cross entropy             */
+    const void *x; uint64_t ldx;    /* [rows, in]                                         */
+    const void *w; uint64_t ldw;    /* [vocab, in]                                        */
+    const void *ids;                /* [rows, terms], contiguous                          */
+    const float *logits;            /* [rows, terms], contiguous, or NULL                 */
+    float *loss;                    /* [rows]: the sum of q (log q - s + lse)             */
+    float *saved;                   /* [rows][1 + terms] or NULL: lse = log of the sum of e^s over the
+                                       vocabulary, and the terms' s (0 for none), for the backward pass */
+} tagc_loss;
+
+typedef struct tagc_loss_grad {
+    uint64_t rows, in, vocab;
+    uint32_t terms, dtype, id_type;
+    uint32_t accumulate;            /* 1: dw is added to what is there                    */
+    double temperature;
+    const void *x; uint64_t ldx;
+    const void *w; uint64_t ldw;
+    const void *ids;
+    const float *logits;
+    const float *saved;             /* as forward left it                                 */
+    const float *dloss;             /* [rows], or one number for all rows: ...            */
+    uint32_t dloss_step;            /* ... 1 or 0 elements from a row to the next         */
+    uint32_t reserved;              /* must be 0                                          */
+    void *dx; uint64_t lddx;        /* [rows, in] or NULL                                 */
+    void *dw; uint64_t lddw;        /* [vocab, in] or NULL: a place in the bucket's gradient */
+} tagc_loss_grad;
+
+int tagc_loss_forward_workspace(const tagc_loss *l, uint64_t *bytes);
+int tagc_loss_backward_workspace(const tagc_loss_grad *l, uint64_t *bytes);
+
+/* Products as tagc_linear_forward's, scores and sums in float32; what is written shares no element with an operand. */
+int tagc_loss_forward(const tagc_loss *l, void *workspace, void *stream);
+
+/*
+ * ds = dloss (e^(s - lse) - q) / temperature, by pieces of the vocabulary, each rounded to the operands' type once; dx = ds w;
+ * dw (+)= ds^T x.  dx is summed in float32 over the pieces.  What is written shares no element with an operand or another result.
+ */
+int tagc_loss_backward(const tagc_loss_grad *l, void *workspace, void *stream);
 
 #ifdef __cplusplus
 }

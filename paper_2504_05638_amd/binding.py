@@ -28,6 +28,8 @@ TAGC_CELL_F32, TAGC_CELL_BF16 = 0, 1
 TAGC_FLAG_OVERFLOW = 2
 TAGC_STATIC_WORKSPACE_BYTES = 16 << 20
 TAGC_MOMENT_BLOCK, TAGC_MAX_GROUPS = 256, 16
+TAGC_NORM_LAYER, TAGC_NORM_RMS = 0, 1
+TAGC_ID_I32, TAGC_ID_I64 = 0, 1
 TAGC_ACT_NONE, TAGC_ACT_RELU, TAGC_ACT_GELU, TAGC_ACT_GELU_TANH, TAGC_ACT_SILU = 0, 1, 2, 3, 4
 
 EXPORTS = ["tagc_plan", "tagc_plan_destroy", "tagc_plan_sizes",
@@ -38,7 +40,10 @@ EXPORTS = ["tagc_plan", "tagc_plan_destroy", "tagc_plan_sizes",
            "tagc_optim_plan", "tagc_optim_destroy", "tagc_optim_plan_sizes", "tagc_optim_upload",
            "tagc_grad_norm", "tagc_adamw_step", "tagc_adamw_unpack",
            "tagc_linear_forward_workspace", "tagc_linear_backward_workspace",
-           "tagc_linear_forward", "tagc_linear_backward"]
+           "tagc_linear_forward", "tagc_linear_backward",
+           "tagc_norm_forward", "tagc_norm_backward_workspace", "tagc_norm_backward",
+           "tagc_embedding_forward", "tagc_embedding_backward_workspace", "tagc_embedding_backward",
+           "tagc_loss_forward_workspace", "tagc_loss_backward_workspace", "tagc_loss_forward", "tagc_loss_backward"]
 
 
 class tagc_segment(C.Structure):
@@ -134,6 +139,46 @@ class tagc_linear_grad(C.Structure):
                 ("pre", C.c_void_p), ("ldp", C.c_uint64), ("dy", C.c_void_p), ("lddy", C.c_uint64),
                 ("dx", C.c_void_p), ("lddx", C.c_uint64), ("dw", C.c_void_p), ("lddw", C.c_uint64),
                 ("db", C.c_void_p), ("accumulate", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tagc_norm(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("width", C.c_uint64), ("dtype", C.c_uint32), ("kind", C.c_uint32), ("eps", C.c_double),
+                ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("b", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_uint64),
+                ("stats", C.c_void_p)]
+
+
+class tagc_norm_grad(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("width", C.c_uint64), ("dtype", C.c_uint32), ("kind", C.c_uint32),
+                ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("stats", C.c_void_p), ("dy", C.c_void_p), ("lddy", C.c_uint64),
+                ("residual", C.c_void_p), ("ldr", C.c_uint64), ("dx", C.c_void_p), ("lddx", C.c_uint64),
+                ("dw", C.c_void_p), ("db", C.c_void_p), ("accumulate", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tagc_embedding(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("width", C.c_uint64), ("vocab", C.c_uint64), ("dtype", C.c_uint32), ("id_type", C.c_uint32),
+                ("scale", C.c_double), ("ids", C.c_void_p), ("table", C.c_void_p), ("ldt", C.c_uint64),
+                ("residual", C.c_void_p), ("ldr", C.c_uint64), ("y", C.c_void_p), ("ldy", C.c_uint64)]
+
+
+class tagc_embedding_grad(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("width", C.c_uint64), ("vocab", C.c_uint64), ("dtype", C.c_uint32), ("id_type", C.c_uint32),
+                ("scale", C.c_double), ("ids", C.c_void_p), ("dy", C.c_void_p), ("lddy", C.c_uint64),
+                ("dtable", C.c_void_p), ("ldt", C.c_uint64), ("accumulate", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tagc_loss(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("in_", C.c_uint64), ("vocab", C.c_uint64), ("terms", C.c_uint32), ("dtype", C.c_uint32),
+                ("id_type", C.c_uint32), ("reserved", C.c_uint32), ("temperature", C.c_double),
+                ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("ldw", C.c_uint64), ("ids", C.c_void_p), ("logits", C.c_void_p),
+                ("loss", C.c_void_p), ("saved", C.c_void_p)]
+
+
+class tagc_loss_grad(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("in_", C.c_uint64), ("vocab", C.c_uint64), ("terms", C.c_uint32), ("dtype", C.c_uint32),
+                ("id_type", C.c_uint32), ("accumulate", C.c_uint32), ("temperature", C.c_double),
+                ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("ldw", C.c_uint64), ("ids", C.c_void_p), ("logits", C.c_void_p),
+                ("saved", C.c_void_p), ("dloss", C.c_void_p), ("dloss_step", C.c_uint32), ("reserved", C.c_uint32),
+                ("dx", C.c_void_p), ("lddx", C.c_uint64), ("dw", C.c_void_p), ("lddw", C.c_uint64)]
 
 
 class TagcError(RuntimeError):
@@ -232,6 +277,16 @@ def lib():
         L.tagc_linear_forward.argtypes = [C.POINTER(tagc_linear), vp, vp]
         L.tagc_linear_backward.restype = C.c_int
         L.tagc_linear_backward.argtypes = [C.POINTER(tagc_linear_grad), vp, vp]
+        for name, t in (("norm_backward", tagc_norm_grad), ("embedding_backward", tagc_embedding_grad),
+                        ("loss_forward", tagc_loss), ("loss_backward", tagc_loss_grad)):
+            f = getattr(L, "tagc_%s_workspace" % name)
+            f.restype, f.argtypes = C.c_int, [C.POINTER(t), C.POINTER(C.c_uint64)]
+            f = getattr(L, "tagc_" + name)
+            f.restype, f.argtypes = C.c_int, [C.POINTER(t), vp, vp]
+        L.tagc_norm_forward.restype = C.c_int
+        L.tagc_norm_forward.argtypes = [C.POINTER(tagc_norm), vp]
+        L.tagc_embedding_forward.restype = C.c_int
+        L.tagc_embedding_forward.argtypes = [C.POINTER(tagc_embedding), vp]
         L.tagc_rows_meet_host.restype = C.c_int
         L.tagc_rows_meet_host.argtypes = [C.c_uint64] * 8
         L.tagc_linear_path_host.restype = C.c_int
@@ -440,3 +495,49 @@ def tagc_linear_forward(l: tagc_linear, workspace=None, stream: int = 0):
 
 def tagc_linear_backward(l: tagc_linear_grad, workspace=None, stream: int = 0):
     _check(lib().tagc_linear_backward(C.byref(l), workspace, stream), "tagc_linear_backward")
+
+
+def _workspace(f, name, a) -> int:
+    n = C.c_uint64()
+    _check(f(C.byref(a), C.byref(n)), name)
+    return int(n.value)
+
+
+def tagc_norm_forward(n: tagc_norm, stream: int = 0):
+    _check(lib().tagc_norm_forward(C.byref(n), stream), "tagc_norm_forward")
+
+
+def tagc_norm_backward_workspace(n: tagc_norm_grad) -> int:
+    return _workspace(lib().tagc_norm_backward_workspace, "tagc_norm_backward_workspace", n)
+
+
+def tagc_norm_backward(n: tagc_norm_grad, workspace=None, stream: int = 0):
+    _check(lib().tagc_norm_backward(C.byref(n), workspace, stream), "tagc_norm_backward")
+
+
+def tagc_embedding_forward(e: tagc_embedding, stream: int = 0):
+    _check(lib().tagc_embedding_forward(C.byref(e), stream), "tagc_embedding_forward")
+
+
+def tagc_embedding_backward_workspace(e: tagc_embedding_grad) -> int:
+    return _workspace(lib().tagc_embedding_backward_workspace, "tagc_embedding_backward_workspace", e)
+
+
+def tagc_embedding_backward(e: tagc_embedding_grad, workspace=None, stream: int = 0):
+    _check(lib().tagc_embedding_backward(C.byref(e), workspace, stream), "tagc_embedding_backward")
+
+
+def tagc_loss_forward_workspace(l: tagc_loss) -> int:
+    return _workspace(lib().tagc_loss_forward_workspace, "tagc_loss_forward_workspace", l)
+
+
+def tagc_loss_backward_workspace(l: tagc_loss_grad) -> int:
+    return _workspace(lib().tagc_loss_backward_workspace, "tagc_loss_backward_workspace", l)
+
+
+def tagc_loss_forward(l: tagc_loss, workspace=None, stream: int = 0):
+    _check(lib().tagc_loss_forward(C.byref(l), workspace, stream), "tagc_loss_forward")
+
+
+def tagc_loss_backward(l: tagc_loss_grad, workspace=None, stream: int = 0):
+    _check(lib().tagc_loss_backward(C.byref(l), workspace, stream), "tagc_loss_backward")

@@ -1,0 +1,427 @@
+// Token embeddings: rows of a table, and the table's gradient.
+//
+//   y[t] = scale * table[ids[t]] + residual[t]            dtable[v] (+)= scale * sum over t with ids[t] = v of dy[t]
+//
+// The gradient's sums have an order of their own: tokens are sorted by id, and by place where ids are equal, so that
+// a row's terms lie one behind the other.  Sorting is counting: a token's place among kChunk tokens is the number of those
+// before it, which all compute units count at once; chunks are then merged by searching each one for every token of the
+// others.  Pieces of kPiece sorted tokens are summed side by side; a run of one id that goes on into the next piece leaves a partial sum
+// there, and these are joined in order.  No atomics, nothing to clear.
+//
+// Bound by bytes: the rows looked up, or dy and the table's gradient, most of which is zeros.
+#include <math.h>
+
+#include "device_utils.h"
+#include "elements.h"
+#include "tagc_internal.h"
+#include "tagc_train.h"
+
+namespace tagc {
+
+namespace {
+
+constexpr uint32_t kChunk = 4096;      // tokens sorted together
+constexpr uint32_t kRankThreads = 512, kRankSlices = kRankThreads / 64;
+constexpr uint32_t kPiece = 16;        // sorted tokens summed by a workgroup
+constexpr uint32_t kSumThreads = 256;
+constexpr uint32_t kZeroRows = 16;     // table rows that a workgroup looks after for want of tokens
+
+// An id, or `vocab` for what is no token.
+__device__ inline uint32_t id_at(const void *ids, uint32_t wide, uint64_t t, uint32_t vocab)
+{
+    const uint64_t id = wide ? static_cast<const uint64_t *>(ids)[t] : uint64_t(int64_t(static_cast<const int32_t *>(ids)[t]));
+    return id < vocab ? uint32_t(id) : vocab;
+}
+
+// ------------------------------------------------------------------ forward
+
+struct Lookup {
+    const void *ids, *table, *residual;
+    void *y;
+    uint64_t ldt, ldr, ldy;
+    uint32_t rows, width, vocab, wide, spans;
+    float scale;
+};
+
+// A wave takes kSteps pieces of 16 bytes to a lane of one row.
+constexpr uint32_t kSteps = 4;
+template <typename T>
+__global__ __launch_bounds__(256) void lookup_kernel(Lookup a)
+{
+    constexpr uint32_t V = 16 / sizeof(T), kSpan = 64 * V * kSteps;
+    const uint64_t job = uint64_t(blockIdx.x) * 4 + threadIdx.x / 64;
+    const uint64_t t = job / a.spans;
+    if (t >= a.rows) return;
+    const uint32_t from = uint32_t(job % a.spans) * kSpan + threadIdx.x % 64 * V;
+    const uint32_t id = id_at(a.ids, a.wide, t, a.vocab);
+    const T *row = static_cast<const T *>(a.table) + (id < a.vocab ? id : 0) * a.ldt, *res = static_cast<const T *>(a.residual) + t * a.ldr;
+    T *y = static_cast<T *>(a.y) + t * a.ldy;
+    const bool token = id < a.vocab;
+    Lane<T, V> in[kSteps] = {}, add[kSteps] = {};
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; ++s) {
+        const uint32_t c = from + s * 64 * V;
+        if (c + V > a.width) continue;
+        if (token) in[s].load(row + c);
+        if (a.residual) add[s].load(res + c);
+    }
+#pragma unroll
+    for (uint32_t s = 0; s < kSteps; ++s) {
+        const uint32_t c = from + s * 64 * V;
+        if (c >= a.width) break;
+        if (c + V <= a.width) {
+            float z[V];
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) z[j] = a.residual ? a.scale * in[s][j] + add[s][j] : a.scale * in[s][j];
+            if (!token)
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j) z[j] = add[s][j];
+            store_n<T, V>(y + c, z);
+        } else {
+            for (uint32_t j = c; j < a.width; ++j) {
+                const float z = token ? a.scale * widen(row[j]) : 0.0f;
+                y[j] = narrow<T>(a.residual ? z + widen(res[j]) : z);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ sorting
+
+struct Sorted {
+    uint32_t *keys, *order;  // [rows] ids in order, and the tokens that have them
+};
+
+// Ranks 64 tokens among their chunk's: a lane has a token, a wave an eighth of the chunk.  Ids that are as large count if they
+// stand before it.
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(const void *ids, uint32_t wide, uint32_t rows, uint32_t vocab, Sorted to)
+{
+    __shared__ __attribute__((aligned(16))) uint32_t keys[kChunk];
+    __shared__ uint32_t counts[kRankSlices][64];
+    const uint32_t group = blockIdx.x, chunk = group * 64 / kChunk * kChunk, have = min(kChunk, rows - chunk);
+    for (uint32_t i = threadIdx.x; i < kChunk; i += kRankThreads) keys[i] = i < have ? id_at(ids, wide, chunk + i, vocab) : 0xFFFFFFFFu;
+    __syncthreads();
+    const uint32_t lane = threadIdx.x % 64, slice = threadIdx.x / 64, at = group * 64 - chunk + lane;
+    const uint32_t key = keys[at];
+    constexpr uint32_t kEach = kChunk / kRankSlices;
+    const uint32_t begin = slice * kEach, end = min(begin + kEach, (have + 63) / 64 * 64), own = at / 64 * 64;
+    uint32_t count = 0;
+    // (a wave's tokens are 64 neighbours: what lies before them counts if it is at most the key, what lies behind if it is under it)
+    for (uint32_t i = begin; i < end; i += 64) {
+        if (i == own) {
+#pragma unroll 8
+            for (uint32_t j = 0; j < 64; ++j) {
+                const uint32_t k = keys[i + j];
+                count += k < key || (k == key && i + j < at);
+            }
+        } else {
+            const uint32_t under = key + (i < own);
+#pragma unroll
+            for (uint32_t j = 0; j < 64; j += 4) {
+                const uint4 k = *reinterpret_cast<const uint4 *>(&keys[i + j]);
+                count += (k.x < under) + (k.y < under) + (k.z < under) + (k.w < under);
+            }
+        }
+    }
+    counts[slice][lane] = count;
+    __syncthreads();
+    if (slice || at >= have) return;
+    count = 0;
+#pragma unroll
+    for (uint32_t s = 0; s < kRankSlices; ++s) count += counts[s][lane];
+    to.keys[chunk + count] = key;
+    to.order[chunk + count] = chunk + at;
+}
+
+// How many of `n` sorted keys are under `key`.
+__device__ inline uint32_t under(const uint32_t *keys, uint32_t n, uint32_t key)
+{
+    uint32_t lo = 0;
+    while (n) {
+        const uint32_t half = n / 2;
+        const bool less = keys[lo + half] < key;
+        lo = less ? lo + half + 1 : lo;
+        n = less ? n - half - 1 : half;
+    }
+    return lo;
+}
+
+__global__ __launch_bounds__(256) void merge_kernel(Sorted from, uint32_t rows, Sorted to)
+{
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows) return;
+    const uint32_t own = i / kChunk, key = from.keys[i];
+    uint32_t at = i % kChunk;
+    for (uint32_t c = 0; c * kChunk < rows; ++c)
+        if (c != own) at += under(from.keys + c * kChunk, min(kChunk, rows - c * kChunk), key + (c < own));
+    to.keys[at] = key;
+    to.order[at] = from.order[i];
+}
+
+// ------------------------------------------------------------------ sums
+
+struct Sums {
+    Sorted sorted;
+    const void *dy;
+    void *dtable;
+    float *partial;  // [pieces][2][width]: of a piece the sum of its first run, if that began before it, and of the run that goes on behind it
+    uint64_t lddy, ldt;
+    uint32_t rows, width, vocab, pieces, spans, accumulate;
+    float scale;
+};
+
+template <typename T>
+__device__ inline void finish_row(const Sums &a, uint32_t key, uint32_t c, uint32_t have, const float (&sum)[16 / sizeof(T)])
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    T *to = static_cast<T *>(a.dtable) + key * a.ldt + c;
+    if (have == V) {
+        float z[V], was[V];
+        if (a.accumulate) load_n<T, V>(to, was);
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) z[j] = a.accumulate ? a.scale * sum[j] + was[j] : a.scale * sum[j];
+        store_n<T, V>(to, z);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j)
+            if (j < have) to[j] = narrow<T>(a.accumulate ? a.scale * sum[j] + widen(to[j]) : a.scale * sum[j]);
+    }
+}
+
+// The first workgroups sum pieces of sorted tokens, 256 * V columns each; the rest writes zeros where a row has no token.
+template <typename T>
+__global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    const uint32_t span = blockIdx.x % a.spans, c = (span * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
+    const uint32_t piece = blockIdx.x / a.spans;
+    if (piece >= a.pieces) {
+        const uint32_t first = (piece - a.pieces) * kZeroRows;
+        __shared__ uint32_t found[kZeroRows];
+        if (threadIdx.x < kZeroRows) {
+            const uint32_t v = first + threadIdx.x, at = under(a.sorted.keys, a.rows, v);
+            found[threadIdx.x] = at < a.rows && a.sorted.keys[at] == v;
+        }
+        __syncthreads();
+        if (!have) return;
+        const float zeros[V] = {};
+        for (uint32_t r = 0; r < kZeroRows && first + r < a.vocab; ++r) {
+            if (found[r]) continue;
+            T *to = static_cast<T *>(a.dtable) + (first + r) * a.ldt + c;
+            if (have == V) {
+                store_n<T, V>(to, zeros);
+            } else {
+                for (uint32_t j = 0; j < have; ++j) to[j] = T(0);
+            }
+        }
+        return;
+    }
+    const uint32_t begin = piece * kPiece, end = min(begin + kPiece, a.rows);
+    const uint32_t before = begin ? a.sorted.keys[begin - 1] : 0xFFFFFFFFu, behind = end < a.rows ? a.sorted.keys[end] : 0xFFFFFFFFu;
+    float sum[V] = {};
+    uint32_t now = a.sorted.keys[begin];
+    bool began = now == before;
+    auto flush = [&](bool goes_on) {
+        if (now >= a.vocab || !have) return;
+        if (!began && !goes_on) return finish_row<T>(a, now, c, have, sum);
+        // (a run that fills its piece and goes on both ways has the first place)
+        float *to = a.partial + (uint64_t(piece) * 2 + (began ? 0 : 1)) * a.width + c;
+        if (have == V) {
+            store_n<float, V>(to, sum);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j)
+                if (j < have) to[j] = sum[j];
+        }
+    };
+    // tokens' rows come four at a time
+    constexpr uint32_t kAhead = 4;
+    for (uint32_t i = begin; i < end; i += kAhead) {
+        uint32_t key[kAhead];
+        float x[kAhead][V];
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k) {
+            const uint32_t at = min(i + k, end - 1);
+            key[k] = a.sorted.keys[at];
+            const T *row = static_cast<const T *>(a.dy) + a.sorted.order[at] * a.lddy + c;
+            if (have == V) {
+                load_n<T, V>(row, x[k]);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j) x[k][j] = j < have ? widen(row[j]) : 0.0f;
+            }
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k) {
+            if (i + k >= end) break;
+            if (key[k] != now) {
+                flush(false);
+                now = key[k];
+                began = false;
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j) sum[j] = x[k][j];
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j) sum[j] += x[k][j];
+            }
+        }
+    }
+    flush(now == behind);
+}
+
+// Runs that go on behind the piece that they begin in: their partial sums in order.
+template <typename T>
+__global__ __launch_bounds__(kSumThreads) void run_kernel(Sums a)
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    const uint32_t piece = blockIdx.x / a.spans, c = (blockIdx.x % a.spans * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
+    const uint32_t begin = piece * kPiece, next = begin + kPiece;
+    if (next >= a.rows) return;
+    const uint32_t key = a.sorted.keys[next];
+    if (key >= a.vocab || a.sorted.keys[next - 1] != key || (begin && a.sorted.keys[begin - 1] == key)) return;
+    if (!have) return;
+    const uint32_t end = under(a.sorted.keys, a.rows, key + 1), last = (end - 1) / kPiece;
+    float sum[V];
+    auto part = [&](uint32_t p, uint32_t which, float (&x)[V]) {
+        const float *from = a.partial + (uint64_t(p) * 2 + which) * a.width + c;
+        if (have == V) {
+            load_n<float, V>(from, x);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) x[j] = j < have ? from[j] : 0.0f;
+        }
+    };
+    part(piece, 1, sum);
+#pragma unroll 4
+    for (uint32_t p = piece + 1; p <= last; ++p) {
+        float x[V];
+        part(p, 0, x);
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) sum[j] += x[j];
+    }
+    finish_row<T>(a, key, c, have, sum);
+}
+
+// ------------------------------------------------------------------ host
+
+int check(uint64_t rows, uint64_t width, uint64_t vocab, uint32_t dtype, uint32_t id_type, double scale)
+{
+    if (dtype > TAGC_BF16 || id_type > TAGC_ID_I64 || !isfinite(scale) || !isfinite(float(scale))) return TAGC_EINVAL;
+    if (rows >= kMaxSide || width >= kMaxSide || vocab >= kMaxSide) return TAGC_ESIZE;
+    // a launch has fewer than 2^32 threads: a workgroup of 256 to 16 rows and 1024 columns at least
+    if ((up(rows, 16) / 16 + up(vocab, 16) / 16 + 1) * (up(width, 1024) / 1024) >= (1ull << 24) || up(rows, 4) * (up(width, 1024) / 1024) >= (1ull << 25)) return TAGC_ESIZE;
+    return TAGC_OK;
+}
+
+int check(const tagc_embedding *l)
+{
+    if (!l) return TAGC_EINVAL;
+    const int rc = check(l->rows, l->width, l->vocab, l->dtype, l->id_type, l->scale);
+    if (rc) return rc;
+    const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2, id = l->id_type == TAGC_ID_I64 ? 8 : 4, M = l->rows, bytes = l->width * e;
+    if (M && l->width && (!l->ids || !l->y || (l->vocab && !l->table))) return TAGC_EINVAL;
+    if (!aligned_to(l->ids, id) || !good(l->table, l->ldt, l->width, e) || !good(l->residual, l->ldr, l->width, e) || !good(l->y, l->ldy, l->width, e)) return TAGC_EINVAL;
+    const Rows y(l->y, M, bytes, l->ldy * e), table(l->table, l->vocab, bytes, l->ldt * e), res(l->residual, M, bytes, l->ldr * e), ids(l->ids, 1, M * id, M * id);
+    const bool over = l->y == l->residual && (M <= 1 || l->ldy == l->ldr);
+    return meet(y, table) || meet(y, ids) || (!over && meet(y, res)) ? TAGC_EINVAL : TAGC_OK;
+}
+
+int check(const tagc_embedding_grad *l)
+{
+    if (!l || l->reserved || l->accumulate > 1) return TAGC_EINVAL;
+    const int rc = check(l->rows, l->width, l->vocab, l->dtype, l->id_type, l->scale);
+    if (rc) return rc;
+    const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2, id = l->id_type == TAGC_ID_I64 ? 8 : 4, M = l->rows, bytes = l->width * e;
+    if (l->vocab && l->width && (!l->dtable || (M && (!l->ids || !l->dy)))) return TAGC_EINVAL;
+    if (!aligned_to(l->ids, id) || !good(l->dy, l->lddy, l->width, e) || !good(l->dtable, l->ldt, l->width, e)) return TAGC_EINVAL;
+    const Rows dtable(l->dtable, l->vocab, bytes, l->ldt * e), dy(l->dy, M, bytes, l->lddy * e), ids(l->ids, 1, M * id, M * id);
+    return meet(dtable, dy) || meet(dtable, ids) ? TAGC_EINVAL : TAGC_OK;
+}
+
+template <typename T>
+int forward(const tagc_embedding *l, hipStream_t s)
+{
+    if (!l->rows || !l->width) return TAGC_OK;
+    constexpr uint32_t kSpan = 64 * (16 / sizeof(T)) * kSteps;
+    const uint32_t spans = uint32_t((l->width + kSpan - 1) / kSpan);
+    const Lookup a{l->ids, l->table, l->residual, l->y, l->ldt, l->ldr, l->ldy, uint32_t(l->rows), uint32_t(l->width), uint32_t(l->vocab), l->id_type, spans, float(l->scale)};
+    ProfileScope prof("embed_lookup", s);
+    lookup_kernel<T><<<uint32_t((l->rows * spans + 3) / 4), 256, 0, s>>>(a);
+    return hip_ok(hipGetLastError());
+}
+
+template <typename T>
+int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t s)
+{
+    const uint64_t M = l->rows;
+    if (!l->vocab || !l->width || (!M && l->accumulate)) return TAGC_OK;
+    const uint32_t chunks = uint32_t((M + kChunk - 1) / kChunk), pieces = uint32_t((M + kPiece - 1) / kPiece);
+    constexpr uint32_t V = 16 / sizeof(T);
+    Sorted sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)};
+    const Sorted first = chunks > 1 ? Sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)} : sorted;
+    Sums a{};
+    a.partial = w.take<float>(uint64_t(pieces) * 2 * l->width);
+    if (!enqueue) return TAGC_OK;
+    a.sorted = sorted;
+    a.dy = l->dy;
+    a.dtable = l->dtable;
+    a.lddy = l->lddy;
+    a.ldt = l->ldt;
+    a.rows = uint32_t(M);
+    a.width = uint32_t(l->width);
+    a.vocab = uint32_t(l->vocab);
+    a.pieces = pieces;
+    a.spans = uint32_t((l->width + kSumThreads * V - 1) / (kSumThreads * V));
+    a.accumulate = l->accumulate;
+    a.scale = float(l->scale);
+    if (M) {
+        ProfileScope prof("embed_sort", s);
+        rank_kernel<<<uint32_t((M + 63) / 64), kRankThreads, 0, s>>>(l->ids, l->id_type, a.rows, a.vocab, first);
+        if (chunks > 1) merge_kernel<<<uint32_t((M + 255) / 256), 256, 0, s>>>(first, a.rows, sorted);
+    }
+    ProfileScope prof("embed_sum", s);
+    const uint32_t zeros = l->accumulate ? 0 : uint32_t((l->vocab + kZeroRows - 1) / kZeroRows);
+    sum_kernel<T><<<(pieces + zeros) * a.spans, kSumThreads, 0, s>>>(a);
+    if (pieces > 1) run_kernel<T><<<(pieces - 1) * a.spans, kSumThreads, 0, s>>>(a);
+    return hip_ok(hipGetLastError());
+}
+
+int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t s)
+{
+    return l->dtype == TAGC_F32 ? backward<float>(l, w, enqueue, s) : backward<uint16_t>(l, w, enqueue, s);
+}
+
+}  // namespace
+
+}  // namespace tagc
+
+using namespace tagc;
+
+extern "C" int tagc_embedding_forward(const tagc_embedding *e, void *stream)
+{
+    const int rc = check(e);
+    if (rc) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return e->dtype == TAGC_F32 ? forward<float>(e, s) : forward<uint16_t>(e, s);
+}
+
+extern "C" int tagc_embedding_backward_workspace(const tagc_embedding_grad *e, uint64_t *bytes)
+{
+    if (!bytes) return TAGC_EINVAL;
+    const int rc = check(e);
+    if (rc) return rc;
+    Places w(nullptr);
+    backward(e, w, false, nullptr);
+    *bytes = w.at;
+    return TAGC_OK;
+}
+
+extern "C" int tagc_embedding_backward(const tagc_embedding_grad *e, void *workspace, void *stream)
+{
+    uint64_t need = 0;
+    const int rc = tagc_embedding_backward_workspace(e, &need);
+    if (rc) return rc;
+    if (need && (!workspace || !aligned_to(workspace, 256))) return TAGC_EINVAL;
+    Places w(workspace);
+    return backward(e, w, true, static_cast<hipStream_t>(stream));
+}

@@ -1,0 +1,878 @@
+// Losses over a vocabulary, and their gradients, without the scores.
+//
+//   s = x w^T / T,  lse = log of the sum of e^s;  loss = sum over a row's terms of q (log q - s + lse)
+//   ds = dloss (e^(s - lse) - q) / T;  dx = ds w,  dw = ds^T x
+//
+// Forward, the scores stay in the registers of the product that makes them: of every row a wave leaves its columns' largest score
+// and the sum of exponentials against it, and these are put together when the product is done.  Terms' own scores are products of
+// two rows each, taken by themselves.  Backward, the product is made again, a piece of the vocabulary at a time, and ends in ds of that piece,
+// which the two products behind it read; the terms' few elements are put right between them.  What is held of a piece is bounded, whatever the
+// vocabulary.
+//
+// Rows without a term take no part: the others are laid out one behind the other, and how many there are is a number on the
+// device that cuts the products short.
+#include <math.h>
+
+#include "product.h"
+#include "tagc_train.h"
+
+namespace tagc {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLeast = 1.17549435e-38f;
+
+// What a piece of the vocabulary may hold (ds, operands laid out, the waves' sums), and its fewest rows.
+constexpr uint64_t kPieceBytes = 256ull << 20, kPieceRows = 1024;
+
+// ------------------------------------------------------------------ terms and rows
+
+__device__ inline uint32_t id_at(const void *ids, uint32_t wide, uint64_t at, uint32_t vocab)
+{
+    const uint64_t id = wide ? static_cast<const uint64_t *>(ids)[at] : uint64_t(int64_t(static_cast<const int32_t *>(ids)[at]));
+    return id < vocab ? uint32_t(id) : vocab;
+}
+
+struct Terms {
+    const void *ids;
+    const float *logits;
+    float *q;        // [rows, terms] with logits: a term's share, 0 for none
+    uint8_t *any;    // [rows] with logits: whether a row has a term
+    uint32_t rows, terms, vocab, wide;
+    float over;      // 1 / temperature
+};
+
+__device__ inline float wave_max(float x)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    return x;
+}
+
+// A teacher's shares, a row to a wave.
+__global__ __launch_bounds__(256) void terms_kernel(Terms a)
+{
+    const uint64_t row = uint64_t(blockIdx.x) * 4 + threadIdx.x / 64;
+    if (row >= a.rows) return;
+    const uint32_t lane = threadIdx.x & 63;
+    const float *logits = a.logits + row * a.terms;
+    float top = -INFINITY, sum = 0;
+    bool any = false;
+    for (uint32_t k = lane; k < a.terms; k += 64) {
+        const float x = logits[k];
+        if (id_at(a.ids, a.wide, row * a.terms + k, a.vocab) == a.vocab || x == -INFINITY) continue;
+        any = true;
+        top = fmaxf(top, x * a.over);
+    }
+    top = wave_max(top);
+    if (top == -INFINITY) top = 0;  // (all there is is NaN)
+    for (uint32_t k = lane; k < a.terms; k += 64) {
+        const float x = logits[k];
+        if (id_at(a.ids, a.wide, row * a.terms + k, a.vocab) == a.vocab || x == -INFINITY) continue;
+        sum += __builtin_amdgcn_exp2f((x * a.over - top) * kLog2e);
+    }
+    sum = wave_sum(sum);
+    for (uint32_t k = lane; k < a.terms; k += 64) {
+        const float x = logits[k];
+        const bool none = id_at(a.ids, a.wide, row * a.terms + k, a.vocab) == a.vocab || x == -INFINITY;
+        float q = __builtin_amdgcn_exp2f((x * a.over - top) * kLog2e) / sum;
+        if (q < kLeast) q = kLeast;  // (a term, if one that does not count: its score is saved)
+        a.q[row * a.terms + k] = none ? 0.0f : q;
+    }
+    any = __any(any);
+    if (lane == 0) a.any[row] = any;
+}
+
+// A row's weight of a term, 0 for none.
+__device__ inline float share(const Terms &a, uint64_t at, uint32_t id) { return a.q ? a.q[at] : id < a.vocab ? 1.0f : 0.0f; }
+
+struct List {
+    uint32_t *rows;   // those with a term in order, then the others
+    uint32_t *count;  // of the first
+    const float *saved, *dloss;
+    float2 *row;      // backward: of each of the first the log2 of its sum of exponentials, and dloss / temperature
+    uint32_t step;
+};
+
+constexpr uint32_t kListThreads = 1024, kListEach = 8;
+__global__ __launch_bounds__(kListThreads) void list_kernel(Terms a, List l)
+{
+    __shared__ uint32_t room[kListThreads / 64];
+    uint32_t done = 0;
+    for (uint32_t first = 0; first < a.rows; first += kListThreads * kListEach) {
+        const uint32_t from = first + threadIdx.x * kListEach;
+        uint32_t bits = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kListEach; ++i)
+            if (from + i < a.rows) bits |= uint32_t(a.logits ? a.any[from + i] != 0 : id_at(a.ids, a.wide, from + i, a.vocab) < a.vocab) << i;
+        uint32_t total;
+        uint32_t at = done + block_excl_scan<uint32_t, kListThreads / 64>(__popc(bits), &total, room);
+#pragma unroll
+        for (uint32_t i = 0; i < kListEach; ++i) {
+            const uint32_t row = from + i;
+            if (row >= a.rows) break;
+            if (!(bits >> i & 1)) {
+                l.rows[a.rows - 1 - (row - at)] = row;  // (row - at: those without a term before it)
+                continue;
+            }
+            l.rows[at] = row;
+            if (l.row) l.row[at] = make_float2(l.saved[uint64_t(row) * (1 + a.terms)] * kLog2e, l.dloss[uint64_t(row) * l.step] * a.over);
+            ++at;
+        }
+        done += total;
+    }
+    if (threadIdx.x == 0) *l.count = done;
+}
+
+// ------------------------------------------------------------------ operands laid out
+
+struct Gather {
+    const void *src;       // rows of `cols`, ld elements apart
+    void *to;
+    const uint32_t *rows;  // which rows, or NULL: all
+    const uint32_t *count; // how many, or NULL: all
+    uint64_t ld, to_ld;
+    uint32_t n, cols, part;  // part: float32 taken apart, elements from one part to the next; 0: as they are
+    uint32_t across;         // pieces of eight elements to a row, zeros behind cols
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void gather_kernel(Gather a)
+{
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t r = uint32_t(i / a.across), c = uint32_t(i % a.across) * 8;
+    if (r >= (a.count ? *a.count : a.n)) return;
+    const T *src = static_cast<const T *>(a.src) + (a.rows ? a.rows[r] : r) * a.ld + c;
+    float x[8];
+    if (c + 8 <= a.cols) {
+        load_n<T, 8>(src, x);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) x[j] = c + j < a.cols ? widen(src[j]) : 0.0f;
+    }
+    if (sizeof(T) == 4 && a.part) {
+        uint16_t *to = static_cast<uint16_t *>(a.to) + r * a.to_ld + c;
+        u32x4 out[kParts];
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            uint32_t s[2][kParts];
+            split(x[2 * j], s[0]);
+            split(x[2 * j + 1], s[1]);
+#pragma unroll
+            for (uint32_t q = 0; q < kParts; ++q) out[q][j] = __builtin_amdgcn_perm(s[1][q], s[0][q], 0x07060302);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kParts; ++q) *reinterpret_cast<u32x4 *>(to + q * a.part) = out[q];
+    } else {
+        store_n<T, 8>(static_cast<T *>(a.to) + r * a.to_ld + c, x);
+    }
+}
+
+// ------------------------------------------------------------------ ends of the products
+
+// A wave's sums in rows, eight neighbours at a time, by way of its strip: f(m, n, z) for rows under `rows` and columns, by eights, under
+// `cols`.
+template <int RM, int RN, typename F>
+__device__ inline __attribute__((always_inline)) void in_rows(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t rows,
+                                                              uint32_t cols, F f)
+{
+    constexpr uint32_t kRow = RN * 16 + 4, across = RN * 2, lines = 64 / across;
+    const uint32_t ln = lane % across * 8, n = n0 + ln;
+#pragma unroll 1
+    for (int i = 0; i < RM; i += 2) {
+#pragma unroll
+        for (int at = 0; at < RM; at += 2)
+            if (at == i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < RN; ++j)
+                        *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[at + h][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const uint32_t m = m0 + i * 16 + lane / across;
+#pragma unroll
+        for (uint32_t l = 0; l < 32 / lines; ++l) {
+            if (m + l * lines >= rows || n >= cols) continue;
+            float z[8];
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(strip + (l * lines + lane / across) * kRow + ln + h);
+                z[h] = v.x;
+                z[h + 1] = v.y;
+                z[h + 2] = v.z;
+                z[h + 3] = v.w;
+            }
+            f(m + l * lines, n, z);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// Forward: of a row's scores in a wave's columns the largest, and the sum of 2^(score - largest), scores times log2(e) / T.
+struct Scores : Counted {
+    static constexpr bool kCounted = true;
+    float2 *stats;  // [strips of columns][rows]
+    uint32_t rows;
+    float over2;    // log2(e) / T
+    template <int RM, int RN>
+    __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
+    {
+        float2 *to = stats + uint64_t(n0 / (RN * 16)) * rows;
+        const uint32_t c0 = n0 + 4 * (lane >> 4);
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+            const uint32_t row = m0 + i * 16 + (lane & 15);
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < RN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c0 + 16 * j + e < n) top = fmaxf(top, acc[i][j][e] * over2);
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float against = top == -INFINITY ? 0.0f : top;  // (no column, or nothing but -infinity and NaN)
+            float sum = 0;
+#pragma unroll
+            for (int j = 0; j < RN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c0 + 16 * j + e < n) sum += __builtin_amdgcn_exp2f(acc[i][j][e] * over2 - against);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (lane < 16 && row < m) to[row] = make_float2(top, sum);
+        }
+    }
+};
+
+// Backward: ds of a piece of the vocabulary but for the terms' weights, as an operand: bfloat16, or float32 taken apart.
+template <typename T>
+struct Slopes : Counted {
+    static constexpr bool kCounted = true;
+    uint16_t *ds;
+    uint64_t ld;
+    uint32_t part;
+    const float2 *row;
+    float over2;
+    template <int RM, int RN>
+    __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
+    {
+        in_rows(acc, strip, lane, m0, n0, m, part, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) {
+            const float2 by = row[r];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) z[j] = c + j < n ? by.y * __builtin_amdgcn_exp2f(z[j] * over2 - by.x) : 0.0f;
+            uint16_t *to = ds + r * ld + c;
+            if constexpr (sizeof(T) == 2) {
+                store_n<uint16_t, 8>(to, z);
+            } else {
+                u32x4 out[kParts];
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    uint32_t s[2][kParts];
+                    split(z[2 * j], s[0]);
+                    split(z[2 * j + 1], s[1]);
+#pragma unroll
+                    for (uint32_t q = 0; q < kParts; ++q) out[q][j] = __builtin_amdgcn_perm(s[1][q], s[0][q], 0x07060302);
+                }
+#pragma unroll
+                for (uint32_t q = 0; q < kParts; ++q) *reinterpret_cast<u32x4 *>(to + q * part) = out[q];
+            }
+        });
+    }
+};
+
+// Elements of a float32 result as far as there are columns.
+__device__ inline void put_f32(float *to, uint32_t have, const float (&z)[8])
+{
+    if (have >= 8) {
+        store_n<float, 8>(to, z);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (j < have) to[j] = z[j];
+    }
+}
+
+// dx of the rows that have a term, in float32: a plane for each part of the sum, added to from piece to piece.
+struct Planes : Counted {
+    static constexpr bool kCounted = true;
+    float *planes;  // [parts][rows][n]
+    uint32_t rows, add;
+    template <int RM, int RN>
+    __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t p) const
+    {
+        in_rows(acc, strip, lane, m0, n0, m, n, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) {
+            float *to = planes + (uint64_t(p) * rows + r) * n + c;
+            const uint32_t have = n - c;
+            if (add) {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j)
+                    if (j < have) z[j] += to[j];
+            }
+            put_f32(to, have, z);
+        });
+    }
+};
+
+// dw of a piece, or parts of its sum.
+template <typename T>
+__device__ inline void put_dw(T *to, uint32_t have, uint32_t add, float (&z)[8])
+{
+    if (have >= 8) {
+        if (add) {
+            float was[8];
+            load_n<T, 8>(to, was);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] += was[j];
+        }
+        store_n<T, 8>(to, z);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (j < have) to[j] = narrow<T>(add ? z[j] + widen(to[j]) : z[j]);
+    }
+}
+
+template <typename T>
+struct Weights : Counted {
+    static constexpr bool kCounted = true;
+    T *dw;
+    uint64_t ld;
+    float *partial;  // [parts][m][n] where there are several
+    uint32_t add;
+    template <int RM, int RN>
+    __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t p) const
+    {
+        in_rows(acc, strip, lane, m0, n0, m, n, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) {
+            if (splits > 1) put_f32(partial + (uint64_t(p) * m + r) * n + c, n - c, z);
+            else put_dw<T>(dw + r * ld + c, n - c, add, z);
+        });
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void weights_join_kernel(Weights<T> a)
+{
+    const uint32_t across = (a.n + 7) / 8;
+    for (uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x; i < uint64_t(a.m) * across; i += uint64_t(gridDim.x) * 256) {
+        const uint32_t r = uint32_t(i / across), c = uint32_t(i % across) * 8, have = a.n - c;
+        float z[8] = {};
+        for (uint32_t p = 0; p < a.splits; ++p) {
+            const float *from = a.partial + (uint64_t(p) * a.m + r) * a.n + c;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j)
+                if (j < have) z[j] += from[j];
+        }
+        put_dw<T>(a.dw + r * a.ld + c, have, a.add, z);
+    }
+}
+
+// ------------------------------------------------------------------ between and behind the products
+
+struct Chosen {
+    Terms terms;
+    List list;
+    const void *x, *w;
+    uint64_t ldx, ldw;
+    uint32_t in;
+    float *scores;  // [rows, terms]: s of every term, 0 for none
+};
+
+// A term's own score: two rows' product, a wave each.
+template <typename T>
+__global__ __launch_bounds__(256) void chosen_kernel(Chosen a)
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    const uint64_t job = uint64_t(blockIdx.x) * 4 + threadIdx.x / 64;
+    const uint32_t i = uint32_t(job / a.terms.terms), k = uint32_t(job % a.terms.terms), lane = threadIdx.x & 63;
+    if (i >= *a.list.count) return;
+    const uint32_t row = a.list.rows[i];
+    const uint64_t at = uint64_t(row) * a.terms.terms + k;
+    const uint32_t id = id_at(a.terms.ids, a.terms.wide, at, a.terms.vocab);
+    float sum = 0;
+    if (id < a.terms.vocab && share(a.terms, at, id) != 0.0f) {
+        const T *x = static_cast<const T *>(a.x) + row * a.ldx, *w = static_cast<const T *>(a.w) + id * a.ldw;
+        for (uint32_t c = lane * V; c < a.in; c += 64 * V) {
+            if (c + V <= a.in) {
+                Lane<T, V> p, q;
+                p.load(x + c);
+                q.load(w + c);
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j) sum = fmaf(p[j], q[j], sum);
+            } else {
+                for (uint32_t j = c; j < a.in; ++j) sum = fmaf(widen(x[j]), widen(w[j]), sum);
+            }
+        }
+        sum = wave_sum(sum) * a.terms.over;
+    }
+    if (lane == 0) a.scores[at] = sum;
+}
+
+struct Close {
+    Terms terms;
+    List list;
+    const float2 *stats;  // [strips][rows]
+    float2 *run;          // [rows]: what earlier pieces of the vocabulary left, or this one leaves
+    uint32_t strips, earlier, last;
+    const float *scores;
+    float *loss, *saved;
+};
+
+// Puts the waves' sums together, 16 rows to a workgroup, and ends in the loss where the piece is the last one.
+__global__ __launch_bounds__(256) void close_kernel(Close a)
+{
+    __shared__ float2 parts[16][17];
+    const uint32_t r = threadIdx.x % 16, slice = threadIdx.x / 16, count = *a.list.count, i = blockIdx.x * 16 + r;
+    float top = -INFINITY, sum = 0;
+    auto join = [&](float2 by) {
+        const float most = fmaxf(top, by.x), against = most == -INFINITY ? 0.0f : most;
+        sum = sum * __builtin_amdgcn_exp2f(top - against) + by.y * __builtin_amdgcn_exp2f(by.x - against);
+        top = most;
+    };
+    if (i < count) {
+        if (a.earlier && slice == 0) join(a.run[i]);
+#pragma unroll 4
+        for (uint32_t s = slice; s < a.strips; s += 16) join(a.stats[uint64_t(s) * a.terms.rows + i]);
+    }
+    parts[slice][r] = make_float2(top, sum);
+    __syncthreads();
+    const uint32_t row_in = threadIdx.x / 16, at = threadIdx.x % 16, j = blockIdx.x * 16 + row_in;
+    if (j >= a.terms.rows) return;
+    top = -INFINITY;
+    sum = 0;
+#pragma unroll
+    for (uint32_t s = 0; s < 16; ++s) join(parts[s][row_in]);
+    const bool there = j < count;
+    if (!a.last) {
+        if (there && at == 0) a.run[j] = make_float2(top, sum);
+        return;
+    }
+    // sixteen threads to a row
+    const uint32_t row = a.list.rows[j], K = a.terms.terms;
+    const float lse = there ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : 0.0f;
+    float loss = 0;
+    for (uint32_t k = at; k < K; k += 16) {
+        const uint64_t t = uint64_t(row) * K + k;
+        float s = 0;
+        if (there) {
+            const float q = share(a.terms, t, id_at(a.terms.ids, a.terms.wide, t, a.terms.vocab));
+            s = a.scores[t];
+            if (q != 0) loss += q * (__builtin_amdgcn_logf(q) * kLn2 + (lse - s));
+        }
+        if (a.saved) a.saved[uint64_t(row) * (1 + K) + 1 + k] = s;
+    }
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) loss += __shfl_xor(loss, d, 64);
+    if (at == 0) {
+        a.loss[row] = loss;
+        if (a.saved) a.saved[uint64_t(row) * (1 + K)] = lse;
+    }
+}
+
+// ds where a row has a term, in its place: from the score that the forward pass saved, so that 1 - q's difference is taken before
+// anything is rounded.  A token that is a row's term twice gets the same value twice.
+template <typename T>
+__global__ __launch_bounds__(256) void terms_slope_kernel(Terms a, List l, uint16_t *ds, uint64_t ld, uint32_t part, uint32_t begin, uint32_t end)
+{
+    const uint64_t job = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t i = uint32_t(job / a.terms), k = uint32_t(job % a.terms);
+    if (i >= *l.count) return;
+    const uint32_t row = l.rows[i];
+    const uint64_t first = uint64_t(row) * a.terms;
+    const uint32_t id = id_at(a.ids, a.wide, first + k, a.vocab);
+    if (id < begin || id >= end || share(a, first + k, id) == 0.0f) return;
+    float q = 0;
+    for (uint32_t j = 0; j < a.terms; ++j)
+        if (id_at(a.ids, a.wide, first + j, a.vocab) == id) q += share(a, first + j, id);
+    const float2 by = l.row[i];
+    const float x = by.y * (__builtin_amdgcn_exp2f(l.saved[first + row + 1 + k] * kLog2e - by.x) - q);
+    uint16_t *to = ds + i * ld + (id - begin);
+    if constexpr (sizeof(T) == 2) {
+        *to = narrow<uint16_t>(x);
+    } else {
+        uint32_t s[kParts];
+        split(x, s);
+#pragma unroll
+        for (uint32_t p = 0; p < kParts; ++p) to[p * part] = uint16_t(s[p] >> 16);
+    }
+}
+
+// dx in the rows' own places: the planes' sum, zeros where a row has no term.
+template <typename T>
+__global__ __launch_bounds__(256) void place_kernel(const float *planes, uint32_t n_planes, List l, uint32_t rows, uint32_t cols, T *dx, uint64_t ld)
+{
+    const uint32_t across = (cols + 7) / 8, count = *l.count;
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t r = uint32_t(i / across), c = uint32_t(i % across) * 8, have = min(8u, cols - c);
+    if (r >= rows) return;
+    float z[8] = {};
+    if (r < count)
+        for (uint32_t p = 0; p < n_planes; ++p) {
+            const float *from = planes + (uint64_t(p) * rows + r) * cols + c;
+            if (have == 8) {
+                float x[8];
+                load_n<float, 8>(from, x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] += x[j];
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j)
+                    if (j < have) z[j] += from[j];
+            }
+        }
+    T *to = dx + l.rows[r] * ld + c;
+    if (have == 8) {
+        store_n<T, 8>(to, z);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (j < have) to[j] = narrow<T>(z[j]);
+    }
+}
+
+// ------------------------------------------------------------------ host
+
+int check_sizes(uint64_t rows, uint64_t in, uint64_t vocab, uint32_t terms, uint32_t dtype, uint32_t id_type, double temperature, const float *logits)
+{
+    if (dtype > TAGC_BF16 || id_type > TAGC_ID_I64 || !in || !vocab || !terms || (!logits && terms != 1)) return TAGC_EINVAL;
+    if (!(temperature > 0) || !isfinite(temperature) || !(float(1 / temperature) > 0) || !isfinite(float(kLog2e / temperature))) return TAGC_EINVAL;
+    const uint64_t most = dtype == TAGC_F32 ? kMaxSide / 4 : kMaxSide;
+    if (rows >= most || in >= most || vocab >= most || terms > TAGC_MAX_TERMS) return TAGC_ESIZE;
+    // a launch has fewer than 2^32 threads: one to eight elements of a row, a wave to a term, a workgroup to a tile of 64 by 64
+    const uint64_t r = up(rows, 64) / 64, i = up(in, 64) / 64, v = up(vocab, 64) / 64;
+    if (r * i + r * v + i * v >= (1ull << 24) || rows * terms >= (1ull << 25) || up(rows, 64) * up(in, 64) >= (1ull << 34) || up(vocab, 64) * up(in, 64) >= (1ull << 34))
+        return TAGC_ESIZE;
+    return TAGC_OK;
+}
+
+// The operands as the products take them: rows with a term, and a piece of the vocabulary at a time.
+struct Operands {
+    bool raw;      // float32 as it lies
+    bool lay;      // whether w's pieces are laid out anew
+};
+
+template <typename T>
+Operands operands_of(uint64_t M, uint64_t D, uint64_t V, const void *w, uint64_t ldw, bool forward)
+{
+    if (sizeof(T) == 2) return Operands{false, !as_it_lies(TAGC_BF16, w, ldw, D, false)};
+    const bool raw = forward && raw_pays(M, V) && ldw < kMaxSide;
+    return Operands{raw, !raw};
+}
+
+// Rows of a piece of the vocabulary that holds so many bytes a row: whole tiles, pieces alike.
+uint64_t piece_rows(uint64_t vocab, uint64_t bytes)
+{
+    uint64_t n = kPieceBytes / (bytes ? bytes : 1);
+    if (n < kPieceRows) n = kPieceRows;
+    const uint64_t pieces = (vocab + n - 1) / n;
+    return up((vocab + pieces - 1) / pieces, 256);
+}
+
+template <typename T>
+Gather gather(const void *src, uint64_t ld, uint64_t n, uint64_t cols, const Operand &to)
+{
+    Gather a{};
+    a.src = src;
+    a.to = const_cast<void *>(to.p);
+    a.ld = ld;
+    a.to_ld = to.ld;
+    a.n = uint32_t(n);
+    a.cols = uint32_t(cols);
+    a.part = to.part;
+    a.across = uint32_t((sizeof(T) == 4 && to.part ? to.part : to.ld) / 8);
+    return a;
+}
+
+template <typename T>
+void launch_gather(const Gather &a, hipStream_t s)
+{
+    ProfileScope prof("loss_lay", s);
+    gather_kernel<T><<<uint32_t((uint64_t(a.n) * a.across + 255) / 256), 256, 0, s>>>(a);
+}
+
+// x's rows that have a term, laid out: an operand for products, zeros behind a row's last element up to a whole slab.
+template <typename T>
+Operand room_for_x(Places &w, uint64_t M, uint64_t D, bool raw)
+{
+    if (sizeof(T) == 4 && raw) return Operand{w.take<float>(M * up(D, 8)), up(D, 8), 0};
+    Operand to = room(w, sizeof(T) == 4 ? TAGC_F32 : TAGC_BF16, M, D);
+    if (sizeof(T) == 2) to.part = 0;
+    return to;
+}
+
+template <typename G>
+Terms terms_of(const G *l, Places &w)
+{
+    Terms t{l->ids, l->logits, nullptr, nullptr, uint32_t(l->rows), l->terms, uint32_t(l->vocab), l->id_type, float(1 / l->temperature)};
+    if (l->logits) {
+        t.q = w.take<float>(l->rows * l->terms);
+        t.any = w.take<uint8_t>(l->rows);
+    }
+    return t;
+}
+
+void launch_terms(const Terms &t, const List &l, hipStream_t s)
+{
+    ProfileScope prof("loss_terms", s);
+    if (t.logits && t.rows) terms_kernel<<<(t.rows + 3) / 4, 256, 0, s>>>(t);
+    list_kernel<<<1, kListThreads, 0, s>>>(t, l);
+}
+
+template <typename T>
+int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
+{
+    const uint64_t M = l->rows, D = l->in, V = l->vocab;
+    constexpr uint32_t dtype = sizeof(T) == 4 ? TAGC_F32 : TAGC_BF16;
+    if (!M) return TAGC_OK;
+    Chosen chosen{};
+    Close close{};
+    const Terms terms = terms_of(l, w);
+    List list{w.take<uint32_t>(M), w.take<uint32_t>(1), nullptr, nullptr, nullptr, 0};
+    const Operands ops = operands_of<T>(M, D, V, l->w, l->ldw, true);
+    const Operand x = room_for_x<T>(w, M, D, ops.raw);
+    // (a wave's strip of columns has 32 at least)
+    const uint64_t piece = piece_rows(V, M * 8 / 32 + (ops.lay ? up(D, 64) * (sizeof(T) == 4 ? 6 : 2) : 0));
+    Operand wq{};
+    if (ops.lay) {
+        wq = room(w, dtype, piece, D);
+        if (sizeof(T) == 2) wq.part = 0;
+    }
+    float2 *stats = w.take<float2>(up(piece, 256) / 32 * M);
+    float2 *run = w.take<float2>(piece < V ? M : 0);
+    float *scores = w.take<float>(M * l->terms);
+    if (!enqueue) return TAGC_OK;
+
+    launch_terms(terms, list, s);
+    Gather gx = gather<T>(l->x, l->ldx, M, D, x);
+    gx.rows = list.rows;
+    gx.count = list.count;
+    launch_gather<T>(gx, s);
+    {
+        ProfileScope prof("loss_terms", s);
+        chosen = Chosen{terms, list, l->x, l->w, l->ldx, l->ldw, uint32_t(D), scores};
+        chosen_kernel<T><<<uint32_t((M * l->terms + 3) / 4), 256, 0, s>>>(chosen);
+    }
+    for (uint64_t v = 0; v < V; v += piece) {
+        const uint64_t n = V - v < piece ? V - v : piece;
+        const T *from = static_cast<const T *>(l->w) + v * l->ldw;
+        Operand q{from, l->ldw, 0};
+        if (ops.lay) {
+            launch_gather<T>(gather<T>(from, l->ldw, n, D, wq), s);
+            q = wq;
+        }
+        Scores a{};
+        const Shape f = shape_of(M, n, D, dtype, false, 1);
+        aim(a, x, q, M, n, D, f);
+        a.there = list.count;
+        a.stats = stats;
+        a.rows = uint32_t(M);
+        a.over2 = float(kLog2e / l->temperature);
+        {
+            ProfileScope prof("loss_product", s);
+            launch<T, false, false>(a, f, s);
+        }
+        ProfileScope prof("loss_close", s);
+        // (four waves share a tile's columns, whatever its size)
+        close = Close{terms, list, stats, run, 4 * f.tiles_n, uint32_t(v > 0), uint32_t(v + n == V), scores, l->loss, l->saved};
+        close_kernel<<<uint32_t((M + 15) / 16), 256, 0, s>>>(close);
+    }
+    return hip_ok(hipGetLastError());
+}
+
+template <typename T>
+int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
+{
+    const uint64_t M = l->rows, D = l->in, V = l->vocab;
+    constexpr uint32_t dtype = sizeof(T) == 4 ? TAGC_F32 : TAGC_BF16;
+    if ((!l->dx && !l->dw) || (!M && (l->accumulate || !l->dw))) return TAGC_OK;
+    const uint64_t rows = M ? M : 1;  // (no rows: dw becomes zeros by a product without terms)
+    const Terms terms = terms_of(l, w);
+    const List list{w.take<uint32_t>(rows), w.take<uint32_t>(1), l->saved, l->dloss, w.take<float2>(rows), l->dloss_step};
+    const Operands ops = operands_of<T>(rows, D, V, l->w, l->ldw, false);
+    const Operand x = room_for_x<T>(w, rows, D, false);
+    const uint64_t e = sizeof(T) == 4 ? 6 : 2, piece = piece_rows(V, (rows + (ops.lay ? up(D, 64) : 0)) * e);
+    Operand wq{};
+    if (ops.lay) {
+        wq = room(w, dtype, piece, D);
+        if (sizeof(T) == 2) wq.part = 0;
+    }
+    const Operand ds = room(w, dtype, rows, piece);
+    const Shape fx = shape_of(rows, D, piece, dtype, false), fw = shape_of(piece, D, rows, dtype, true);
+    float *planes = w.take<float>(l->dx ? fx.splits * rows * D : 0), *partial = w.take<float>(l->dw && fw.splits > 1 ? fw.splits * piece * D : 0);
+    if (!enqueue) return TAGC_OK;
+
+    launch_terms(terms, list, s);
+    if (M) {
+        Gather gx = gather<T>(l->x, l->ldx, M, D, x);
+        gx.rows = list.rows;
+        gx.count = list.count;
+        launch_gather<T>(gx, s);
+    }
+    for (uint64_t v = 0; v < V; v += piece) {
+        const uint64_t n = V - v < piece ? V - v : piece;
+        const T *from = static_cast<const T *>(l->w) + v * l->ldw;
+        Operand q{from, l->ldw, 0};
+        if (ops.lay) {
+            launch_gather<T>(gather<T>(from, l->ldw, n, D, wq), s);
+            q = wq;
+        }
+        if (M) {
+            Slopes<T> a{};
+            const Shape f = shape_of(M, n, D, dtype, false, 1);
+            aim(a, x, q, M, n, D, f);
+            a.there = list.count;
+            a.ds = static_cast<uint16_t *>(const_cast<void *>(ds.p));
+            a.ld = ds.ld;
+            a.part = ds.part;
+            a.row = list.row;
+            a.over2 = float(kLog2e / l->temperature);
+            {
+                ProfileScope prof("loss_slopes", s);
+                launch<T, false, false>(a, f, s);
+            }
+            ProfileScope prof("loss_terms", s);
+            terms_slope_kernel<T><<<uint32_t((M * l->terms + 255) / 256), 256, 0, s>>>(terms, list, a.ds, ds.ld, ds.part, uint32_t(v), uint32_t(v + n));
+        }
+        Operand p = ds;
+        if (sizeof(T) == 2) p.part = 0;
+        if (l->dx && M) {
+            Planes a{};
+            aim(a, p, q, M, D, n, fx);
+            const uint64_t slab = dtype == TAGC_F32 ? kSlab3 : kSlab;
+            a.slabs = uint32_t((up(n, slab) / slab + fx.splits - 1) / fx.splits);
+            a.there = list.count;
+            a.planes = planes;
+            a.rows = uint32_t(M);
+            a.add = v > 0;
+            ProfileScope prof("loss_dx", s);
+            launch<T, false, true>(a, fx, s);
+        }
+        if (l->dw) {
+            Weights<T> a{};
+            Shape f = fw;
+            f.tiles_m = uint32_t((n + f.rows - 1) / f.rows);
+            aim(a, p, x, n, D, rows, f);
+            a.there = list.count;
+            a.of_k = true;
+            a.dw = static_cast<T *>(l->dw) + v * l->lddw;
+            a.ld = l->lddw;
+            a.partial = partial;
+            a.add = l->accumulate;
+            {
+                ProfileScope prof("loss_dw", s);
+                launch<T, true, true>(a, f, s);
+            }
+            if (f.splits > 1) {
+                ProfileScope prof("loss_dw_join", s);
+                const uint64_t groups = (n * ((D + 7) / 8) + 255) / 256;
+                weights_join_kernel<T><<<uint32_t(groups < 65536 ? groups : 65536), 256, 0, s>>>(a);
+            }
+        }
+    }
+    if (l->dx && M) {
+        ProfileScope prof("loss_place", s);
+        place_kernel<T><<<uint32_t((M * ((D + 7) / 8) + 255) / 256), 256, 0, s>>>(planes, fx.splits, list, uint32_t(M), uint32_t(D), static_cast<T *>(l->dx), l->lddx);
+    }
+    return hip_ok(hipGetLastError());
+}
+
+template <typename G>
+bool good_operands(const G *l)
+{
+    const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2;
+    return good(l->x, l->ldx, l->in, e) && good(l->w, l->ldw, l->in, e) && aligned_to(l->ids, l->id_type == TAGC_ID_I64 ? 8 : 4) && aligned_to(l->logits, 4);
+}
+
+// Whether [at, at + bytes) or rows of a result meet an operand of the call.
+template <typename G>
+bool meets_operands(const G *l, const Rows &r)
+{
+    const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2, row = l->in * e, K = l->rows * l->terms, id = l->id_type == TAGC_ID_I64 ? 8 : 4;
+    const Rows in[] = {Rows(l->x, l->rows, row, l->ldx * e), Rows(l->w, l->vocab, row, l->ldw * e), Rows(l->ids, 1, K * id, K * id), Rows(l->logits, 1, K * 4, K * 4)};
+    for (const Rows &i : in)
+        if (meet(r, i)) return true;
+    return false;
+}
+
+int check(const tagc_loss *l)
+{
+    if (!l || l->reserved) return TAGC_EINVAL;
+    const int rc = check_sizes(l->rows, l->in, l->vocab, l->terms, l->dtype, l->id_type, l->temperature, l->logits);
+    if (rc) return rc;
+    if (l->rows && (!l->x || !l->w || !l->ids || !l->loss)) return TAGC_EINVAL;
+    if (!good_operands(l) || !aligned_to(l->loss, 4) || !aligned_to(l->saved, 4)) return TAGC_EINVAL;
+    const uint64_t n = l->rows * 4, m = n * (1 + l->terms);
+    const Rows loss(l->loss, 1, n, n), saved(l->saved, 1, m, m);
+    return meets_operands(l, loss) || meets_operands(l, saved) || meet(loss, saved) ? TAGC_EINVAL : TAGC_OK;
+}
+
+int check(const tagc_loss_grad *l)
+{
+    if (!l || l->reserved || l->accumulate > 1 || l->dloss_step > 1) return TAGC_EINVAL;
+    const int rc = check_sizes(l->rows, l->in, l->vocab, l->terms, l->dtype, l->id_type, l->temperature, l->logits);
+    if (rc) return rc;
+    const uint64_t e = l->dtype == TAGC_F32 ? 4 : 2, M = l->rows, row = l->in * e;
+    if (M && (!l->x || !l->w || !l->ids || !l->saved || !l->dloss)) return TAGC_EINVAL;
+    if (!good_operands(l) || !aligned_to(l->saved, 4) || !aligned_to(l->dloss, 4) || !good(l->dx, l->lddx, l->in, e) || !good(l->dw, l->lddw, l->in, e)) return TAGC_EINVAL;
+    const uint64_t m = M * 4 * (1 + l->terms), n = M ? 4 * (1 + (M - 1) * l->dloss_step) : 0;
+    const Rows saved(l->saved, 1, m, m), dloss(l->dloss, 1, n, n), dx(l->dx, M, row, l->lddx * e), dw(l->dw, l->vocab, row, l->lddw * e);
+    if (meets_operands(l, dx) || meets_operands(l, dw) || meet(dx, saved) || meet(dw, saved) || meet(dx, dloss) || meet(dw, dloss) || meet(dx, dw)) return TAGC_EINVAL;
+    return TAGC_OK;
+}
+
+int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
+{
+    return l->dtype == TAGC_F32 ? forward<float>(l, w, enqueue, s) : forward<uint16_t>(l, w, enqueue, s);
+}
+
+int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
+{
+    return l->dtype == TAGC_F32 ? backward<float>(l, w, enqueue, s) : backward<uint16_t>(l, w, enqueue, s);
+}
+
+}  // namespace
+
+}  // namespace tagc
+
+using namespace tagc;
+
+extern "C" int tagc_loss_forward_workspace(const tagc_loss *l, uint64_t *bytes)
+{
+    if (!bytes) return TAGC_EINVAL;
+    const int rc = check(l);
+    if (rc) return rc;
+    Places w(nullptr);
+    forward(l, w, false, nullptr);
+    *bytes = w.at;
+    return TAGC_OK;
+}
+
+extern "C" int tagc_loss_backward_workspace(const tagc_loss_grad *l, uint64_t *bytes)
+{
+    if (!bytes) return TAGC_EINVAL;
+    const int rc = check(l);
+    if (rc) return rc;
+    Places w(nullptr);
+    backward(l, w, false, nullptr);
+    *bytes = w.at;
+    return TAGC_OK;
+}
+
+extern "C" int tagc_loss_forward(const tagc_loss *l, void *workspace, void *stream)
+{
+    uint64_t need = 0;
+    const int rc = tagc_loss_forward_workspace(l, &need);
+    if (rc) return rc;
+    if (need && (!workspace || !aligned_to(workspace, 256))) return TAGC_EINVAL;
+    Places w(workspace);
+    return forward(l, w, true, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int tagc_loss_backward(const tagc_loss_grad *l, void *workspace, void *stream)
+{
+    uint64_t need = 0;
+    const int rc = tagc_loss_backward_workspace(l, &need);
+    if (rc) return rc;
+    if (need && (!workspace || !aligned_to(workspace, 256))) return TAGC_EINVAL;
+    Places w(workspace);
+    return backward(l, w, true, static_cast<hipStream_t>(stream));
+}

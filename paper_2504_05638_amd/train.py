@@ -1,9 +1,16 @@
-"""The two ends of a data-parallel step around the exchange: linear layers whose backward pass
-writes into a bucket's gradient, and the optimizer behind it.  Device memory and argument
-marshalling only; all arithmetic is the library's (include/tagc_train.h).
+"""The two ends of a data-parallel step around the exchange: the layers whose backward pass
+writes into a bucket's gradient -- linear ones, norms, the tokens' table, the loss over the vocabulary --,
+and the optimizer behind it.  Device memory and argument marshalling only; all arithmetic is the library's
+(include/tagc_train.h).
 
+    x = embedding(ids, table)
+    h, stats = norm(x, gain, kind="rms", save=True)
     y, pre = linear(x, w, b, activation="gelu", save=True)
-    dx = linear_backward(dy, x, w, pre, activation="gelu", dw=bucket_grad_view, db=...)
+    loss, saved = cross_entropy(y, head, targets, save=True)
+    dy = cross_entropy_backward(dloss, y, head, targets, saved, dw=bucket_grad_view)
+    dh = linear_backward(dy, h, w, pre, activation="gelu", dw=bucket_grad_view, db=...)
+    dx = norm_backward(dh, x, gain, stats, kind="rms", residual=dy, dw=...)
+    embedding_backward(dx, ids, bucket_grad_view)
     ...                                # the exchange: bucket.TagcBucket
     opt = AdamW(params=..., grads=dense_views(bucket), max_norm=1.0, bits=8)
     opt.grad_norm()                    # norm, clip factor and step count, on the device
@@ -201,6 +208,246 @@ def linear_backward(dy, x, w, pre=None, activation=None, dx=None, dw=None, db=No
     if given[0] is not None or dw is not None or db is not None:
         increment_version(_counted(given))
     return dx
+
+
+_KINDS = {"layer": B.TAGC_NORM_LAYER, "rms": B.TAGC_NORM_RMS}
+_IDS = {torch.int32: B.TAGC_ID_I32, torch.int64: B.TAGC_ID_I64}
+
+
+def _check_tensor(x, name, stream):
+    if stream is not None:
+        _check_stream(stream, x.device)
+    if not x.is_cuda or x.dtype not in _TYPES:
+        raise ValueError("%s: a CUDA tensor of float32 or bfloat16 is wanted" % name)
+
+
+def _no_graph(what, *tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        warnings.warn("%s records no autograd graph: gradients are %s_backward's; call it under torch.no_grad()" % (what, what), stacklevel=3)
+
+
+def _all_ids(t, name, shape, device):
+    """(address, type) of ids that lie one behind the other."""
+    if t.dtype not in _IDS or t.device != device or t.shape != shape or not (t.is_contiguous() or t.numel() <= 1):
+        raise ValueError("%s: contiguous int32 or int64 of %s on %s are wanted" % (name, tuple(shape), device))
+    return t.data_ptr() or None, _IDS[t.dtype]
+
+
+def _floats(t, name, shape, device):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != device or t.shape != shape or not (t.is_contiguous() or t.numel() <= 1):
+        raise ValueError("%s: contiguous float32 of %s on %s are wanted" % (name, tuple(shape), device))
+    return t.data_ptr() or None
+
+
+def norm(x, w=None, b=None, kind="layer", eps=1e-5, save=False, out=None, stream=None):
+    """(y, stats): y = (x - mean) / sqrt(variance + eps) * w + b over the last dimension, or, kind "rms", without mean
+    and b.  `save`: stats, float32 [rows, 2], for norm_backward (else None).  `out` may be given, and be x.  No autograd graph is
+    recorded; `stream`: as for linear."""
+    _check_tensor(x, "x", stream)
+    _need(x.dim() >= 1, "x: a row at least is wanted")
+    _need(kind in _KINDS, "kind: one of layer, rms is wanted")
+    _no_graph("norm", x, w, b)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    n = shape[-1]
+    m = math.prod(shape[:-1])
+    xp, ldx = _rows_of(_flat(x, m, n), "x", m, n, dtype, device)
+    wp, bp = _vector(w, "w", n, dtype, device), _vector(b, "b", n, dtype, device)
+    _need(out is None or out.shape == shape, "out: x's shape is wanted")
+    yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
+    given, stats, sp, user = out, None, None, torch.cuda.current_stream(device) if stream is not None else None
+    with _at(device, stream):
+        if out is None:
+            out = x.new_empty(shape)
+            yp, ldy = out.data_ptr() or None, n
+        if save:
+            stats = torch.empty((m, 2), dtype=torch.float32, device=device)
+            sp = stats.data_ptr() or None
+        B.tagc_norm_forward(B.tagc_norm(m, n, _TYPES[dtype], _KINDS[kind], eps, xp, ldx, wp, bp, yp, ldy, sp), _stream_of(stream, device))
+    if stream is not None:
+        _hand_over(user, out if given is None else None, stats)
+    if given is not None:
+        increment_version(_counted((given,)))
+    return out, stats
+
+
+def norm_backward(dy, x, w, stats, kind="layer", residual=None, dx=None, dw=None, db=None, accumulate=False, need_dx=True, stream=None):
+    """dx (None without need_dx), plus `residual`, the gradient that came around the layer.  With `dw` and `db` ([width], views
+    into a bucket's gradient) given, the weight's and the bias's gradient are written there, or added to what is there (accumulate).
+    `w` may be None; `stats`: what norm(save=True) gave; `dx` may be dy, x or the residual.  `stream`: as for linear."""
+    _check_tensor(x, "x", stream)
+    _need(x.dim() >= 1, "x: a row at least is wanted")
+    _need(kind in _KINDS, "kind: one of layer, rms is wanted")
+    _need(need_dx or (dx is None and residual is None), "dx or residual is given, but need_dx is not")
+    shape, dtype, device = x.shape, x.dtype, x.device
+    n = shape[-1]
+    m = math.prod(shape[:-1])
+    xp, ldx = _rows_of(_flat(x, m, n), "x", m, n, dtype, device)
+    yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
+    rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
+    dp, ldd = _rows_of(_flat(dx, m, n), "dx", m, n, dtype, device)
+    wp, gp, bp = (_vector(t, name, n, dtype, device) for t, name in ((w, "w"), (dw, "dw"), (db, "db")))
+    sp = _floats(stats, "stats", (m, 2), device)
+    given, user = (dx, dw, db), torch.cuda.current_stream(device) if stream is not None else None
+    with _at(device, stream):
+        if need_dx and dx is None:
+            dx = x.new_empty(shape)
+            dp, ldd = dx.data_ptr() or None, n
+        a = B.tagc_norm_grad(m, n, _TYPES[dtype], _KINDS[kind], xp, ldx, wp, sp, yp, ldy, rp, ldr, dp, ldd, gp, bp, 1 if accumulate else 0, 0)
+        ws, at = _work(B.tagc_norm_backward_workspace(a), x)
+        B.tagc_norm_backward(a, at, _stream_of(stream, device))
+    if stream is not None:
+        _hand_over(user, dx if given[0] is None else None)
+    if given[0] is not None or dw is not None or db is not None:
+        increment_version(_counted(given))
+    return dx
+
+
+def embedding(ids, table, scale=1.0, residual=None, out=None, stream=None):
+    """scale * table[ids] + residual, [*ids.shape, width].  ids: int32 or int64; one outside the table is no token, and its row of
+    the table counts as zeros.  `out` may be given, and be the residual.  No autograd graph is recorded; `stream`: as for linear."""
+    _check_tensor(table, "table", stream)
+    _need(table.dim() == 2, "table: [vocab, width] is wanted")
+    _no_graph("embedding", table, residual)
+    v, n = table.shape
+    dtype, device = table.dtype, table.device
+    m, shape = ids.numel(), (*ids.shape, n)
+    ip, wide = _all_ids(ids, "ids", ids.shape, device)
+    tp, ldt = _rows_of(table, "table", v, n, dtype, device)
+    for t, name in ((residual, "residual"), (out, "out")):
+        _need(t is None or t.shape == shape, "%s: the shape %s is wanted" % (name, shape))
+    rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
+    yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
+    given, user = out, torch.cuda.current_stream(device) if stream is not None else None
+    with _at(device, stream):
+        if out is None:
+            out = table.new_empty(shape)
+            yp, ldy = out.data_ptr() or None, n
+        a = B.tagc_embedding(m, n, v, _TYPES[dtype], wide, scale, ip, tp, ldt, rp, ldr, yp, ldy)
+        B.tagc_embedding_forward(a, _stream_of(stream, device))
+    if stream is not None:
+        _hand_over(user, out if given is None else None)
+    if given is not None:
+        increment_version(_counted((given,)))
+    return out
+
+
+def embedding_backward(dy, ids, dtable, scale=1.0, accumulate=False, stream=None):
+    """The table's gradient, written into `dtable` ([vocab, width], a view into a bucket's gradient; zeros where a row has no
+    token), or added to what is there (accumulate).  Sums are taken in the tokens' order: results repeat.  `stream`: as for linear."""
+    _check_tensor(dtable, "dtable", stream)
+    _need(dtable.dim() == 2, "dtable: [vocab, width] is wanted")
+    v, n = dtable.shape
+    dtype, device = dtable.dtype, dtable.device
+    m = ids.numel()
+    ip, wide = _all_ids(ids, "ids", ids.shape, device)
+    _need(dy.shape == (*ids.shape, n), "dy: the shape %s is wanted" % ((*ids.shape, n),))
+    yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
+    tp, ldt = _rows_of(dtable, "dtable", v, n, dtype, device)
+    with _at(device, stream):
+        a = B.tagc_embedding_grad(m, n, v, _TYPES[dtype], wide, scale, ip, yp, ldy, tp, ldt, 1 if accumulate else 0, 0)
+        ws, at = _work(B.tagc_embedding_backward_workspace(a), dtable)
+        B.tagc_embedding_backward(a, at, _stream_of(stream, device))
+    increment_version(_counted((dtable,)))
+
+
+def _loss_operands(x, w, ids, logits, temperature, stream):
+    """What both passes of a loss have: (rows, in, vocab, terms), the operands' fields, the shape of a number for each row."""
+    _check_tensor(x, "x", stream)
+    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
+        raise ValueError("x is [..., in] and w [vocab, in]: got %s and %s" % (tuple(x.shape), tuple(w.shape)))
+    _need(temperature > 0 and math.isfinite(temperature), "temperature: over 0 is wanted")
+    dtype, device, shape = x.dtype, x.device, x.shape[:-1]
+    v, k = w.shape
+    m = math.prod(shape)
+    if logits is None:
+        terms = 1
+        ip, wide = _all_ids(ids, "targets", shape, device)
+        ap = None
+    else:
+        _need(ids.dim() == len(shape) + 1 and ids.shape[:-1] == shape, "ids: [..., terms] of x's rows are wanted")
+        terms = ids.shape[-1]
+        ip, wide = _all_ids(ids, "ids", ids.shape, device)
+        ap = _floats(logits, "logits", ids.shape, device)
+    xp, ldx = _rows_of(_flat(x, m, k) if x.dim() != 1 else x.view(1, k), "x", m, k, dtype, device)
+    wp, ldw = _rows_of(w, "w", v, k, dtype, device)
+    return (m, k, v, terms), wide, (xp, ldx, wp, ldw, ip, ap), shape
+
+
+def _loss(x, w, ids, logits, temperature, save, stream):
+    size, wide, operands, shape = _loss_operands(x, w, ids, logits, temperature, stream)
+    device, saved, sp, user = x.device, None, None, torch.cuda.current_stream(x.device) if stream is not None else None
+    with _at(device, stream):
+        loss = torch.empty(shape, dtype=torch.float32, device=device)
+        if save:
+            saved = torch.empty((size[0], 1 + size[3]), dtype=torch.float32, device=device)
+            sp = saved.data_ptr() or None
+        a = B.tagc_loss(*size, _TYPES[x.dtype], wide, 0, temperature, *operands, loss.data_ptr() or None, sp)
+        ws, at = _work(B.tagc_loss_forward_workspace(a), x)
+        B.tagc_loss_forward(a, at, _stream_of(stream, device))
+    if stream is not None:
+        _hand_over(user, loss, saved)
+    return loss, saved
+
+
+def _loss_backward(dloss, x, w, ids, logits, saved, temperature, dx, dw, accumulate, need_dx, stream):
+    size, wide, operands, shape = _loss_operands(x, w, ids, logits, temperature, stream)
+    m, k, v, terms = size
+    dtype, device = x.dtype, x.device
+    _need(need_dx or dx is None, "dx is given, but need_dx is not")
+    sp = _floats(saved, "saved", (m, 1 + terms), device)
+    one = dloss.numel() == 1 and dloss.dim() <= 1
+    gp = _floats(dloss, "dloss", dloss.shape if one else shape, device)
+    _need(dx is None or dx.shape == x.shape, "dx: x's shape is wanted")
+    dp, ldd = _rows_of((_flat(dx, m, k) if x.dim() != 1 else dx.view(1, k)) if dx is not None else None, "dx", m, k, dtype, device)
+    wp, ldw = _rows_of(dw, "dw", v, k, dtype, device)
+    given, user = (dx, dw), torch.cuda.current_stream(device) if stream is not None else None
+    with _at(device, stream):
+        if need_dx and dx is None:
+            dx = x.new_empty(x.shape)
+            dp, ldd = dx.data_ptr() or None, k
+        a = B.tagc_loss_grad(*size, _TYPES[dtype], wide, 1 if accumulate else 0, temperature, *operands, sp, gp, 0 if one else 1, 0, dp, ldd, wp, ldw)
+        ws, at = _work(B.tagc_loss_backward_workspace(a), x)
+        B.tagc_loss_backward(a, at, _stream_of(stream, device))
+    if stream is not None:
+        _hand_over(user, dx if given[0] is None else None)
+    if given[0] is not None or dw is not None:
+        increment_version(_counted(given))
+    return dx
+
+
+def cross_entropy(x, w, targets, save=False, stream=None):
+    """(loss, saved): of every row of x [..., in] the softmax cross entropy of its scores x w^T over a vocabulary w [vocab, in] against
+    its target (int32 or int64), float32; the scores are kept nowhere.  A target outside [0, vocab) is ignored: loss 0, no gradient.
+    `save`: saved, float32 [rows, 2] (the log-sum of the scores' exponentials, the target's score), for cross_entropy_backward (else
+    None).  No autograd graph is recorded; `stream`: as for linear."""
+    _no_graph("cross_entropy", x, w)
+    return _loss(x, w, targets, None, 1.0, save, stream)
+
+
+def cross_entropy_backward(dloss, x, w, targets, saved, dx=None, dw=None, accumulate=False, need_dx=True, stream=None):
+    """dx (None without need_dx).  `dloss`: float32, a number for each row, or one for all (such as 1 / the rows that count).  With `dw`
+    ([vocab, in], a view into a bucket's gradient) given, w's gradient is written there, or added to what is there (accumulate).
+    `saved`: what cross_entropy(save=True) gave.  `stream`: as for linear."""
+    return _loss_backward(dloss, x, w, targets, None, saved, 1.0, dx, dw, accumulate, need_dx, stream)
+
+
+def distill(x, w, ids, logits, temperature=1.0, save=False, stream=None):
+    """(loss, saved): of every row of x [..., in] the Kullback-Leibler divergence of softmax(x w^T / temperature) over a vocabulary w
+    [vocab, in] from a teacher's distribution, which is softmax(logits / temperature) over the row's tokens ids [..., terms] (the teacher's
+    largest scores; int32 or int64, logits float32).  A token outside [0, vocab), or one with the logit -inf, is none; a row
+    without any has loss 0 and no gradient.  `saved`: [rows, 1 + terms], as for cross_entropy.  (To have gradients of
+    the usual size at a temperature, weigh dloss by its square.)"""
+    _no_graph("distill", x, w)
+    _need(logits is not None, "logits: the teacher's are wanted")
+    return _loss(x, w, ids, logits, temperature, save, stream)
+
+
+def distill_backward(dloss, x, w, ids, logits, saved, temperature=1.0, dx=None, dw=None, accumulate=False, need_dx=True, stream=None):
+    """dx and dw of distill, as cross_entropy_backward's; none for the teacher."""
+    _need(logits is not None, "logits: the teacher's are wanted")
+    return _loss_backward(dloss, x, w, ids, logits, saved, temperature, dx, dw, accumulate, need_dx, stream)
 
 
 def dense_views(bucket):

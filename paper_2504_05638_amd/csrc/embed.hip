@@ -5,11 +5,14 @@
 // The gradient's sums have an order of their own: tokens are sorted by id, and by place where ids are equal, so that
 // a row's terms lie one behind the other.  Sorting is counting: a token's place among kChunk tokens is the number of those
 // before it, which all compute units count at once; chunks are then merged by searching each one for every token of the
-// others.  Pieces of kPiece sorted tokens are summed side by side; a run of one id that goes on into the next piece leaves a partial sum
-// there, and these are joined in order.  No atomics, nothing to clear.
+// others, kMerge of them at a time.  Pieces of sorted tokens are summed side by side; a run of one id that goes on into the next piece
+// leaves a partial sum there, and these are joined in order.  No atomics on sums, nothing to clear.
 //
-// Bound by bytes: the rows looked up, or dy and the table's gradient, most of which is zeros.
+// Bound by bytes: the rows looked up, or dy and the table's gradient, most of which is zeros; these are written while the tokens are
+// sorted.
 #include <math.h>
+
+#include <type_traits>
 
 #include "device_utils.h"
 #include "elements.h"
@@ -20,11 +23,15 @@ namespace tagc {
 
 namespace {
 
-constexpr uint32_t kChunk = 4096;      // tokens sorted together
+// Tokens sorted together: ranking costs each of them a pass over the chunk, merging a launch.  (us of sorting 16384: 13 + 9, as one chunk 41.)
+constexpr uint32_t kChunk = 4096;
+constexpr uint32_t kMerge = 16;        // sorted lists merged at once
 constexpr uint32_t kRankThreads = 512, kRankSlices = kRankThreads / 64;
-constexpr uint32_t kPiece = 16;        // sorted tokens summed by a workgroup
-constexpr uint32_t kSumThreads = 256;
-constexpr uint32_t kZeroRows = 16;     // table rows that a workgroup looks after for want of tokens
+// Sorted tokens summed by a workgroup: many leave fewer partial sums behind, few make more workgroups of a short batch.  (us, eight / 16 /
+// 32: 16384 tokens into 32000 by 4096 in bfloat16 133 / 126 / 123, 1023 into 50257 by 768 in float32 38 / 41 / 45.)
+constexpr uint32_t kShortPiece = 8, kLongPiece = 32, kShort = 8192;
+constexpr uint32_t kSumThreads = 256, kRunSlices = kSumThreads / 64;
+constexpr uint32_t kZeroRows = 64;     // most table rows that a workgroup looks after for want of tokens
 
 // An id, or `vocab` for what is no token.
 __device__ inline uint32_t id_at(const void *ids, uint32_t wide, uint64_t t, uint32_t vocab)
@@ -92,19 +99,59 @@ struct Sorted {
     uint32_t *keys, *order;  // [rows] ids in order, and the tokens that have them
 };
 
-// Ranks 64 tokens among their chunk's: a lane has a token, a wave an eighth of the chunk.  Ids that are as large count if they
-// stand before it.
-__global__ __launch_bounds__(kRankThreads) void rank_kernel(const void *ids, uint32_t wide, uint32_t rows, uint32_t vocab, Sorted to)
+struct Tokens {
+    const void *ids;
+    Sorted to;
+    void *dtable;        // NULL: no zeros are wanted
+    uint64_t ldt;
+    uint32_t rows, width, vocab, wide, groups;
+    uint32_t zero_rows;  // table rows of a workgroup
+};
+
+// The first workgroups rank 64 tokens each among their chunk's: a lane has a token, a wave an eighth of the chunk.  Ids that are as
+// large count if they stand before it.  The others look for tokens of some rows of the table, and write zeros where there
+// are none: bytes that keep the memory busy meanwhile (16384 tokens into 32000 by 4096 in bfloat16: 222 MB beside
+// ranking take 40 us, 5.5 TB/s; ranking alone 13).
+template <typename T>
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(Tokens a)
 {
     __shared__ __attribute__((aligned(16))) uint32_t keys[kChunk];
     __shared__ uint32_t counts[kRankSlices][64];
-    const uint32_t group = blockIdx.x, chunk = group * 64 / kChunk * kChunk, have = min(kChunk, rows - chunk);
-    for (uint32_t i = threadIdx.x; i < kChunk; i += kRankThreads) keys[i] = i < have ? id_at(ids, wide, chunk + i, vocab) : 0xFFFFFFFFu;
+    const uint32_t group = blockIdx.x;
+    if (group >= a.groups) {
+        constexpr uint32_t V = 16 / sizeof(T);
+        const uint32_t first = (group - a.groups) * a.zero_rows;
+        uint32_t *found = keys;
+        if (threadIdx.x < a.zero_rows) found[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll 4
+        for (uint32_t t = threadIdx.x; t < a.rows; t += kRankThreads) {
+            const uint32_t v = id_at(a.ids, a.wide, t, a.vocab) - first;
+            if (v < a.zero_rows) found[v] = 1;
+        }
+        __syncthreads();
+        const float zeros[V] = {};
+        for (uint32_t r = 0; r < a.zero_rows && first + r < a.vocab; ++r) {
+            if (found[r]) continue;
+            T *to = static_cast<T *>(a.dtable) + (first + r) * a.ldt;
+            for (uint32_t c = threadIdx.x * V; c < a.width; c += kRankThreads * V) {
+                if (c + V <= a.width) {
+                    store_n<T, V>(to + c, zeros);
+                } else {
+                    for (uint32_t j = c; j < a.width; ++j) to[j] = T(0);
+                }
+            }
+        }
+        return;
+    }
+    const uint32_t chunk = group * 64 / kChunk * kChunk, have = min(kChunk, a.rows - chunk), whole = (have + 63) / 64 * 64;
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < whole; i += kRankThreads) keys[i] = i < have ? id_at(a.ids, a.wide, chunk + i, a.vocab) : 0xFFFFFFFFu;
     __syncthreads();
     const uint32_t lane = threadIdx.x % 64, slice = threadIdx.x / 64, at = group * 64 - chunk + lane;
     const uint32_t key = keys[at];
-    constexpr uint32_t kEach = kChunk / kRankSlices;
-    const uint32_t begin = slice * kEach, end = min(begin + kEach, (have + 63) / 64 * 64), own = at / 64 * 64;
+    const uint32_t each = (whole / 64 + kRankSlices - 1) / kRankSlices * 64;
+    const uint32_t begin = slice * each, end = min(begin + each, whole), own = at / 64 * 64;
     uint32_t count = 0;
     // (a wave's tokens are 64 neighbours: what lies before them counts if it is at most the key, what lies behind if it is under it)
     for (uint32_t i = begin; i < end; i += 64) {
@@ -129,8 +176,8 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(const void *ids, uin
     count = 0;
 #pragma unroll
     for (uint32_t s = 0; s < kRankSlices; ++s) count += counts[s][lane];
-    to.keys[chunk + count] = key;
-    to.order[chunk + count] = chunk + at;
+    a.to.keys[chunk + count] = key;
+    a.to.order[chunk + count] = chunk + at;
 }
 
 // How many of `n` sorted keys are under `key`.
@@ -146,16 +193,21 @@ __device__ inline uint32_t under(const uint32_t *keys, uint32_t n, uint32_t key)
     return lo;
 }
 
-__global__ __launch_bounds__(256) void merge_kernel(Sorted from, uint32_t rows, Sorted to)
+// Sorted lists of `run` tokens, kMerge of them to one: a token's place is its own list's, and what the others have before it.
+__global__ __launch_bounds__(256) void merge_kernel(Sorted from, uint32_t rows, uint32_t run, Sorted to)
 {
     const uint32_t i = blockIdx.x * 256 + threadIdx.x;
     if (i >= rows) return;
-    const uint32_t own = i / kChunk, key = from.keys[i];
-    uint32_t at = i % kChunk;
-    for (uint32_t c = 0; c * kChunk < rows; ++c)
-        if (c != own) at += under(from.keys + c * kChunk, min(kChunk, rows - c * kChunk), key + (c < own));
-    to.keys[at] = key;
-    to.order[at] = from.order[i];
+    const uint32_t own = i / run, first = own / kMerge * kMerge, key = from.keys[i];
+    uint32_t at = i % run;
+#pragma unroll 4
+    for (uint32_t k = 0; k < kMerge; ++k) {
+        const uint32_t c = first + k;
+        if (c == own || uint64_t(c) * run >= rows) continue;
+        at += under(from.keys + c * run, min(run, rows - c * run), key + (c < own));
+    }
+    to.keys[first * run + at] = key;
+    to.order[first * run + at] = from.order[i];
 }
 
 // ------------------------------------------------------------------ sums
@@ -170,12 +222,13 @@ struct Sums {
     float scale;
 };
 
-template <typename T>
+// WHOLE: rows are whole pieces of V elements.
+template <typename T, bool WHOLE>
 __device__ inline void finish_row(const Sums &a, uint32_t key, uint32_t c, uint32_t have, const float (&sum)[16 / sizeof(T)])
 {
     constexpr uint32_t V = 16 / sizeof(T);
     T *to = static_cast<T *>(a.dtable) + key * a.ldt + c;
-    if (have == V) {
+    if (WHOLE || have == V) {
         float z[V], was[V];
         if (a.accumulate) load_n<T, V>(to, was);
 #pragma unroll
@@ -188,45 +241,35 @@ __device__ inline void finish_row(const Sums &a, uint32_t key, uint32_t c, uint3
     }
 }
 
-// The first workgroups sum pieces of sorted tokens, 256 * V columns each; the rest writes zeros where a row has no token.
-template <typename T>
+// A workgroup sums a piece of sorted tokens, 256 * V columns of them.  Bound by the bytes of dy, of the rows that are finished and of the partial sums: 16384
+// tokens of 4096 in bfloat16, added to what is there, 55 us, 4.5 TB/s.
+template <typename T, uint32_t PIECE, bool WHOLE>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
 {
     constexpr uint32_t V = 16 / sizeof(T);
     const uint32_t span = blockIdx.x % a.spans, c = (span * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
     const uint32_t piece = blockIdx.x / a.spans;
-    if (piece >= a.pieces) {
-        const uint32_t first = (piece - a.pieces) * kZeroRows;
-        __shared__ uint32_t found[kZeroRows];
-        if (threadIdx.x < kZeroRows) {
-            const uint32_t v = first + threadIdx.x, at = under(a.sorted.keys, a.rows, v);
-            found[threadIdx.x] = at < a.rows && a.sorted.keys[at] == v;
-        }
-        __syncthreads();
-        if (!have) return;
-        const float zeros[V] = {};
-        for (uint32_t r = 0; r < kZeroRows && first + r < a.vocab; ++r) {
-            if (found[r]) continue;
-            T *to = static_cast<T *>(a.dtable) + (first + r) * a.ldt + c;
-            if (have == V) {
-                store_n<T, V>(to, zeros);
-            } else {
-                for (uint32_t j = 0; j < have; ++j) to[j] = T(0);
-            }
-        }
-        return;
-    }
-    const uint32_t begin = piece * kPiece, end = min(begin + kPiece, a.rows);
-    const uint32_t before = begin ? a.sorted.keys[begin - 1] : 0xFFFFFFFFu, behind = end < a.rows ? a.sorted.keys[end] : 0xFFFFFFFFu;
+    const uint32_t begin = piece * PIECE, n = min(PIECE, a.rows - begin);
+    // a lane has a token's id and row, the piece's neighbours' ids behind them; all rows are asked for before the first is needed
+    const uint32_t lane = threadIdx.x % 64, at = lane < n ? begin + lane : lane == PIECE ? begin - 1 : begin + n;
+    const bool there = lane < n || (lane == PIECE && begin) || (lane == PIECE + 1 && begin + n < a.rows);
+    const uint32_t mine = there ? a.sorted.keys[at] : 0xFFFFFFFFu, row = a.sorted.order[lane < n ? at : begin];
+    // (taken from the lanes before lanes part: behind that, those that are done with a register may write to it)
+    uint32_t rows[PIECE], keys[PIECE + 2];
+#pragma unroll
+    for (uint32_t k = 0; k < PIECE; ++k) rows[k] = __builtin_amdgcn_readlane(row, k);
+#pragma unroll
+    for (uint32_t k = 0; k < PIECE + 2; ++k) keys[k] = __builtin_amdgcn_readlane(mine, k);
+    const uint32_t before = keys[PIECE], behind = keys[PIECE + 1];
     float sum[V] = {};
-    uint32_t now = a.sorted.keys[begin];
+    uint32_t now = keys[0];
     bool began = now == before;
     auto flush = [&](bool goes_on) {
         if (now >= a.vocab || !have) return;
-        if (!began && !goes_on) return finish_row<T>(a, now, c, have, sum);
+        if (!began && !goes_on) return finish_row<T, WHOLE>(a, now, c, have, sum);
         // (a run that fills its piece and goes on both ways has the first place)
         float *to = a.partial + (uint64_t(piece) * 2 + (began ? 0 : 1)) * a.width + c;
-        if (have == V) {
+        if (WHOLE || have == V) {
             store_n<float, V>(to, sum);
         } else {
 #pragma unroll
@@ -234,72 +277,91 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
                 if (j < have) to[j] = sum[j];
         }
     };
-    // tokens' rows come four at a time
+    // rows come four at a time, the next ones while these are added (two, eight: 1 % slower, the same; all at once, which leaves fewer workgroups
+    // room, half as long again)
     constexpr uint32_t kAhead = 4;
-    for (uint32_t i = begin; i < end; i += kAhead) {
-        uint32_t key[kAhead];
-        float x[kAhead][V];
+    Lane<T, V> x[2][kAhead];
+    auto fetch = [&](uint32_t first, Lane<T, V>(&to)[kAhead]) __attribute__((always_inline)) {
 #pragma unroll
         for (uint32_t k = 0; k < kAhead; ++k) {
-            const uint32_t at = min(i + k, end - 1);
-            key[k] = a.sorted.keys[at];
-            const T *row = static_cast<const T *>(a.dy) + a.sorted.order[at] * a.lddy + c;
-            if (have == V) {
-                load_n<T, V>(row, x[k]);
+            const T *from = static_cast<const T *>(a.dy) + rows[first + k] * a.lddy + c;
+            if (WHOLE || have == V) {
+                if (have) to[k].load(from);
             } else {
 #pragma unroll
-                for (uint32_t j = 0; j < V; ++j) x[k][j] = j < have ? widen(row[j]) : 0.0f;
+                for (uint32_t j = 0; j < V; ++j) to[k].v[j] = j < have ? from[j] : T(0);
             }
         }
+    };
+    fetch(0, x[0]);
+#pragma unroll
+    for (uint32_t g = 0; g < PIECE; g += kAhead) {
+        if (g + kAhead < PIECE) fetch(g + kAhead, x[g / kAhead + 1 & 1]);
 #pragma unroll
         for (uint32_t k = 0; k < kAhead; ++k) {
-            if (i + k >= end) break;
-            if (key[k] != now) {
+            if (g + k >= n) break;
+            if (keys[g + k] != now) {
                 flush(false);
-                now = key[k];
+                now = keys[g + k];
                 began = false;
 #pragma unroll
-                for (uint32_t j = 0; j < V; ++j) sum[j] = x[k][j];
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < V; ++j) sum[j] += x[k][j];
+                for (uint32_t j = 0; j < V; ++j) sum[j] = 0;
             }
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) sum[j] += x[g / kAhead & 1][k][j];
         }
     }
     flush(now == behind);
 }
 
-// Runs that go on behind the piece that they begin in: their partial sums in order.
-template <typename T>
+// Runs that go on behind the piece that they begin in: their partial sums in order, a quarter to each of the four waves that share 64 * V
+// columns, eight on their way at once.  (A token's share of text can be a tenth: 50 pieces of 16384 tokens, 10 us; one
+// part after the other, four on their way, 31.)
+template <typename T, uint32_t PIECE>
 __global__ __launch_bounds__(kSumThreads) void run_kernel(Sums a)
 {
-    constexpr uint32_t V = 16 / sizeof(T);
-    const uint32_t piece = blockIdx.x / a.spans, c = (blockIdx.x % a.spans * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
-    const uint32_t begin = piece * kPiece, next = begin + kPiece;
+    constexpr uint32_t V = 16 / sizeof(T), kAhead = 8;
+    __shared__ float parts[kRunSlices][V][64];
+    const uint32_t spans = (a.width + 64 * V - 1) / (64 * V), piece = blockIdx.x / spans, lane = threadIdx.x % 64, slice = threadIdx.x / 64;
+    const uint32_t c = (blockIdx.x % spans * 64 + lane) * V, have = c < a.width ? min(V, a.width - c) : 0;
+    const uint32_t begin = piece * PIECE, next = begin + PIECE;
     if (next >= a.rows) return;
     const uint32_t key = a.sorted.keys[next];
     if (key >= a.vocab || a.sorted.keys[next - 1] != key || (begin && a.sorted.keys[begin - 1] == key)) return;
-    if (!have) return;
-    const uint32_t end = under(a.sorted.keys, a.rows, key + 1), last = (end - 1) / kPiece;
-    float sum[V];
-    auto part = [&](uint32_t p, uint32_t which, float (&x)[V]) {
-        const float *from = a.partial + (uint64_t(p) * 2 + which) * a.width + c;
-        if (have == V) {
-            load_n<float, V>(from, x);
-        } else {
+    const uint32_t end = under(a.sorted.keys, a.rows, key + 1), count = (end - 1) / PIECE - piece + 1;
+    // (the first part is its piece's second sum, the others are their pieces' first)
+    const uint32_t each = (count + kRunSlices - 1) / kRunSlices, from = slice * each, to = min(from + each, count);
+    float sum[V] = {};
+    for (uint32_t p = from; p < to; p += kAhead) {
+        float x[kAhead][V];
 #pragma unroll
-            for (uint32_t j = 0; j < V; ++j) x[j] = j < have ? from[j] : 0.0f;
+        for (uint32_t k = 0; k < kAhead; ++k) {
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) x[k][j] = 0;
+            if (p + k >= to) continue;
+            const float *at = a.partial + (uint64_t(piece + p + k) * 2 + (p + k == 0)) * a.width + c;
+            if (have == V) {
+                load_n<float, V>(at, x[k]);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j)
+                    if (j < have) x[k][j] = at[j];
+            }
         }
-    };
-    part(piece, 1, sum);
-#pragma unroll 4
-    for (uint32_t p = piece + 1; p <= last; ++p) {
-        float x[V];
-        part(p, 0, x);
 #pragma unroll
-        for (uint32_t j = 0; j < V; ++j) sum[j] += x[j];
+        for (uint32_t k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) sum[j] += x[k][j];
     }
-    finish_row<T>(a, key, c, have, sum);
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) parts[slice][j][lane] = sum[j];
+    __syncthreads();
+    if (slice || !have) return;
+#pragma unroll
+    for (uint32_t s = 1; s < kRunSlices; ++s)
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) sum[j] += parts[s][j][lane];
+    finish_row<T, false>(a, key, c, have, sum);
 }
 
 // ------------------------------------------------------------------ host
@@ -308,8 +370,8 @@ int check(uint64_t rows, uint64_t width, uint64_t vocab, uint32_t dtype, uint32_
 {
     if (dtype > TAGC_BF16 || id_type > TAGC_ID_I64 || !isfinite(scale) || !isfinite(float(scale))) return TAGC_EINVAL;
     if (rows >= kMaxSide || width >= kMaxSide || vocab >= kMaxSide) return TAGC_ESIZE;
-    // a launch has fewer than 2^32 threads: a workgroup of 256 to 16 rows and 1024 columns at least
-    if ((up(rows, 16) / 16 + up(vocab, 16) / 16 + 1) * (up(width, 1024) / 1024) >= (1ull << 24) || up(rows, 4) * (up(width, 1024) / 1024) >= (1ull << 25)) return TAGC_ESIZE;
+    // a launch has fewer than 2^32 threads: a workgroup of 256 to eight rows and 256 columns at least
+    if ((up(rows, 8) / 8 + 1) * (up(width, 256) / 256) >= (1ull << 24)) return TAGC_ESIZE;
     return TAGC_OK;
 }
 
@@ -355,14 +417,13 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
 {
     const uint64_t M = l->rows;
     if (!l->vocab || !l->width || (!M && l->accumulate)) return TAGC_OK;
-    const uint32_t chunks = uint32_t((M + kChunk - 1) / kChunk), pieces = uint32_t((M + kPiece - 1) / kPiece);
+    const uint32_t piece = M <= kShort ? kShortPiece : kLongPiece, pieces = uint32_t((M + piece - 1) / piece);
     constexpr uint32_t V = 16 / sizeof(T);
-    Sorted sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)};
-    const Sorted first = chunks > 1 ? Sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)} : sorted;
+    Sorted sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)}, other = sorted;
+    if (M > kChunk) other = Sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)};
     Sums a{};
     a.partial = w.take<float>(uint64_t(pieces) * 2 * l->width);
     if (!enqueue) return TAGC_OK;
-    a.sorted = sorted;
     a.dy = l->dy;
     a.dtable = l->dtable;
     a.lddy = l->lddy;
@@ -374,15 +435,33 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
     a.spans = uint32_t((l->width + kSumThreads * V - 1) / (kSumThreads * V));
     a.accumulate = l->accumulate;
     a.scale = float(l->scale);
-    if (M) {
+    {
+        // (rows to a workgroup so that there are two workgroups to a compute unit)
+        Tokens t{l->ids, sorted, l->dtable, l->ldt, a.rows, a.width, a.vocab, l->id_type, uint32_t((M + 63) / 64), 1};
+        while (t.zero_rows < kZeroRows && l->vocab / t.zero_rows > 2 * uint64_t(device_cu_count())) t.zero_rows *= 2;
+        const uint32_t zeros = l->accumulate ? 0 : (a.vocab + t.zero_rows - 1) / t.zero_rows;
         ProfileScope prof("embed_sort", s);
-        rank_kernel<<<uint32_t((M + 63) / 64), kRankThreads, 0, s>>>(l->ids, l->id_type, a.rows, a.vocab, first);
-        if (chunks > 1) merge_kernel<<<uint32_t((M + 255) / 256), 256, 0, s>>>(first, a.rows, sorted);
+        rank_kernel<T><<<t.groups + zeros, kRankThreads, 0, s>>>(t);
+        for (uint64_t run = kChunk; run < M; run *= kMerge) {
+            merge_kernel<<<uint32_t((M + 255) / 256), 256, 0, s>>>(sorted, a.rows, uint32_t(run), other);
+            const Sorted was = sorted;
+            sorted = other;
+            other = was;
+        }
     }
-    ProfileScope prof("embed_sum", s);
-    const uint32_t zeros = l->accumulate ? 0 : uint32_t((l->vocab + kZeroRows - 1) / kZeroRows);
-    sum_kernel<T><<<(pieces + zeros) * a.spans, kSumThreads, 0, s>>>(a);
-    if (pieces > 1) run_kernel<T><<<(pieces - 1) * a.spans, kSumThreads, 0, s>>>(a);
+    if (pieces) {
+        a.sorted = sorted;
+        ProfileScope prof("embed_sum", s);
+        const uint32_t runs = (pieces - 1) * uint32_t((l->width + 64 * V - 1) / (64 * V));
+        const auto go = [&](auto size) {
+            constexpr uint32_t P = decltype(size)::value;
+            if (l->width % V) sum_kernel<T, P, false><<<pieces * a.spans, kSumThreads, 0, s>>>(a);
+            else sum_kernel<T, P, true><<<pieces * a.spans, kSumThreads, 0, s>>>(a);
+            if (runs) run_kernel<T, P><<<runs, kSumThreads, 0, s>>>(a);
+        };
+        if (piece == kShortPiece) go(std::integral_constant<uint32_t, kShortPiece>());
+        else go(std::integral_constant<uint32_t, kLongPiece>());
+    }
     return hip_ok(hipGetLastError());
 }
 

@@ -214,13 +214,25 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void norm_grad_kernel(NormGrad
     if constexpr (kNarrow)
 #pragma unroll
         for (int i = 0; i < (LAYER ? 2 : 1) * P::N; ++i) held[i * LANES + threadIdx.x] = 0.0f;
-    for (uint64_t row = uint64_t(blockIdx.x) * kRows + threadIdx.x / LANES; row < a.rows; row += uint64_t(gridDim.x) * kRows) {
-        P px, py, pr;
-        px.load(x + row * a.ldx, a.width);
-        py.load(dy + row * a.lddy, a.width);
-        pr.fill(0);
-        if (res) pr.load(res + row * a.ldr, a.width);
-        const float2 stats = *reinterpret_cast<const float2 *>(a.stats + 2 * row);
+    // (the next row comes while this one's sums meet, where there are registers for it: 3 % at 8192 by 4096)
+    constexpr bool kAhead = P::N <= 16 && !kNarrow;
+    P ax, ay, ar;
+    float2 next_stats = make_float2(0, 0);
+    ar.fill(0);
+    auto fetch = [&](uint64_t row) __attribute__((always_inline)) {
+        ax.load(x + row * a.ldx, a.width);
+        ay.load(dy + row * a.lddy, a.width);
+        if (res) ar.load(res + row * a.ldr, a.width);
+        next_stats = *reinterpret_cast<const float2 *>(a.stats + 2 * row);
+    };
+    const uint64_t step = uint64_t(gridDim.x) * kRows;
+    uint64_t row = uint64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
+    if (kAhead && row < a.rows) fetch(row);
+    for (; row < a.rows; row += step) {
+        if (!kAhead) fetch(row);
+        P px = ax, py = ay, pr = ar;
+        const float2 stats = next_stats;
+        if (kAhead && row + step < a.rows) fetch(row + step);
         float sum[2] = {0, 0};
 #pragma unroll
         for (int i = 0; i < P::N; ++i) {
@@ -284,29 +296,35 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void norm_grad_kernel(NormGrad
         }
 }
 
-// dw and db from the workgroups' sums: 32 columns to a workgroup, whose 32 groups of threads take every 32nd sum.
-constexpr uint32_t kJoinSlices = 32;
+// dw (the first workgroups) or db (the others) from the workgroups' sums: 16 columns to a workgroup, whose 64 groups of threads take
+// every 64th sum, eight of them on their way at once: they come from other XCDs' writes, a microsecond each.
+constexpr uint32_t kJoinSlices = 64, kJoinColumns = 16, kJoinAhead = 8;
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_join_kernel(const float *sums, uint32_t groups, uint32_t width, T *dw, T *db, uint32_t accumulate)
 {
-    __shared__ float parts[2][kJoinSlices][32];
-    const uint32_t c = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32;
-    float sum[2] = {0, 0};
+    __shared__ float parts[kJoinSlices][kJoinColumns];
+    const uint32_t across = (width + kJoinColumns - 1) / kJoinColumns;
+    const bool second = !dw || blockIdx.x >= across;
+    const uint32_t at = threadIdx.x % kJoinColumns, slice = threadIdx.x / kJoinColumns, c = blockIdx.x % across * kJoinColumns + at;
+    float sum = 0;
     if (c < width)
-#pragma unroll 4
-        for (uint32_t g = slice; g < groups; g += kJoinSlices) {
-            const float *from = sums + uint64_t(g) * 2 * width + c;
-            if (dw) sum[0] += from[0];
-            if (db) sum[1] += from[width];
+        for (uint32_t g = slice; g < groups; g += kJoinSlices * kJoinAhead) {
+            float x[kJoinAhead];
+#pragma unroll
+            for (uint32_t i = 0; i < kJoinAhead; ++i) {
+                const uint32_t which = g + i * kJoinSlices;
+                x[i] = which < groups ? sums[(uint64_t(which) * 2 + second) * width + c] : 0.0f;
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kJoinAhead; ++i) sum += x[i];
         }
-    parts[0][slice][threadIdx.x % 32] = sum[0];
-    parts[1][slice][threadIdx.x % 32] = sum[1];
+    parts[slice][at] = sum;
     __syncthreads();
-    T *to = slice == 0 ? dw : db;
-    if (slice > 1 || !to || c >= width) return;
+    if (slice || c >= width) return;
+    T *to = second ? db : dw;
     float s = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kJoinSlices; ++i) s += parts[slice][i][threadIdx.x % 32];
+    for (uint32_t i = 0; i < kJoinSlices; ++i) s += parts[i][at];
     to[c] = narrow<T>(accumulate ? s + widen(to[c]) : s);
 }
 
@@ -328,10 +346,13 @@ static_assert(TAGC_MAX_NORM_WIDTH == 1024 * 16, "the widest rows that registers 
 
 uint32_t rows_at_once(uint64_t width) { return width <= 64 * 16 ? 4 : 1; }
 
-// workgroups of the backward pass
+// Workgroups of the backward pass.  The fewer there are, the fewer sums are left to be joined, and a row on its way behind the one in work keeps
+// the memory busy.  (us, one / two / three / four to a compute unit: bfloat16 8192 by 4096 54 / 57 / 60 / 62, 4096 by 8192 66 / 66 / 76 / 80,
+// 16384 by 2048 64 / 55 / 57 / 61, 32768 by 512 36 / 30 / 32 / 33, 512 by 4096 14 / 20 / 20 / 20; float32 8192 by 768 32 / 27 / 32 / 32, 2048 by
+// 8192 67 / 77 / 87 / 99.)
 uint32_t grad_groups(uint64_t rows, uint64_t width)
 {
-    const uint64_t all = (rows + rows_at_once(width) - 1) / rows_at_once(width), most = 4 * uint64_t(device_cu_count());
+    const uint64_t all = (rows + rows_at_once(width) - 1) / rows_at_once(width), most = (width > 2048 ? 1 : 2) * uint64_t(device_cu_count());
     return uint32_t(all < most ? all : most);
 }
 
@@ -411,7 +432,7 @@ int backward(const tagc_norm_grad *n, Places &w, bool enqueue, hipStream_t s)
     }
     if (sums) {
         ProfileScope prof("norm_join", s);
-        norm_join_kernel<T><<<uint32_t((n->width + 31) / 32), 1024, 0, s>>>(room, groups, uint32_t(n->width), static_cast<T *>(n->dw), static_cast<T *>(n->db),
+        norm_join_kernel<T><<<uint32_t((n->width + kJoinColumns - 1) / kJoinColumns) * ((n->dw ? 1 : 0) + (n->db ? 1 : 0)), 1024, 0, s>>>(room, groups, uint32_t(n->width), static_cast<T *>(n->dw), static_cast<T *>(n->db),
                                                                           n->accumulate);
     }
     return hip_ok(hipGetLastError());

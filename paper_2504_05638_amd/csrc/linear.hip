@@ -19,10 +19,6 @@ namespace tagc {
 
 namespace {
 
-// rows up to which few_kernel goes; from there on tiles are faster (weights of 4096 by 11008, 17, 32, 64 rows, us: bfloat16
-// 32, 35, 48, as tiles 23, 24, 26; float32 76, 95, 164, as tiles 74, 75, 80)
-constexpr uint32_t kFewRows = 16;
-
 // ------------------------------------------------------------------ activations
 
 // (the hardware's exp2 and reciprocal: within 2 ulp each)
@@ -362,107 +358,11 @@ __global__ __launch_bounds__(256) void join_kernel(const float *partial, uint32_
 
 // ------------------------------------------------------------------ few rows
 
-struct FewArgs {
-    const void *x, *w;
-    uint64_t ldx, ldw;
-    uint32_t rows, in, out;
+template <typename T>
+struct FewWritten : FewArgs {
     Result result;
+    __device__ inline void put(uint32_t m, uint32_t n, uint32_t have, float (&z)[8]) const { finish<T>(result, m, n, have, z); }
 };
-
-// Sixteen k's of a row from `k` on as they lie in memory, zeros from `end` on.
-template <typename T>
-struct Piece {
-    T x[16];
-    __device__ inline void load(const T *row, uint32_t k, uint32_t end)
-    {
-        if (k + 16 <= end) {
-            typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
-#pragma unroll
-            for (uint32_t i = 0; i < sizeof(T); ++i) {
-                const vec v = *reinterpret_cast<const vec *>(row + k + i * (16 / sizeof(T)));
-#pragma unroll
-                for (uint32_t j = 0; j < 16 / sizeof(T); ++j) x[i * (16 / sizeof(T)) + j] = v[j];
-            }
-        } else {
-#pragma unroll
-            for (uint32_t j = 0; j < 16; ++j) x[j] = k + j < end ? row[k + j] : T(0);
-        }
-    }
-    // the first or the second eight as the matrix instruction takes them
-    __device__ inline void half(int h, bf16x8 (&to)[sizeof(T) == 2 ? 1 : 3]) const
-    {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if constexpr (sizeof(T) == 2) {
-                to[0][e] = __builtin_bit_cast(__bf16, x[8 * h + e]);
-            } else {
-                uint32_t s[kParts];
-                split(x[8 * h + e], s);
-#pragma unroll
-                for (uint32_t q = 0; q < kParts; ++q) to[q][e] = __builtin_bit_cast(__bf16, uint16_t(s[q] >> 16));
-            }
-        }
-    }
-};
-
-// Up to kFewRows rows: the weights are read once, straight into registers, in pieces of 64 k's of 16 features out; rows of x,
-// which all workgroups read, come from the caches.  kFewWaves waves share the k's of 16 features out and add up their
-// sums in local memory.  The matrix instruction's k's may be in any order that both operands share: a lane takes 16
-// neighbours, so that four lanes read a whole cache line.  float32 is taken apart in registers.
-//
-// Bound by the weights' bytes (one row of bfloat16 through 4096 by 11008, not in any cache: 17.5 us, 5.2 TB/s; 16 features
-// out to a workgroup, 32 take half as long again; four or sixteen waves a sixth and a twelfth more; eight pieces on their way instead
-// of four a tenth), at 16 rows also by x, which is as many bytes to a workgroup then (26.0).
-constexpr int kFewWaves = 8;
-template <typename T>
-__global__ __launch_bounds__(kFewWaves * 64, 2) void few_kernel(FewArgs a)
-{
-    constexpr int planes = sizeof(T) == 2 ? 1 : 3, D = sizeof(T) == 2 ? 4 : 2;  // pieces on their way
-    __shared__ f32x4 sums[kFewWaves][64];
-    const uint32_t lane = lane_id(), wave = threadIdx.x >> 6, at = lane & 15, k0 = (lane >> 4) * 16;
-    const uint32_t n0 = blockIdx.x * 16;
-    const T *w = static_cast<const T *>(a.w) + min(n0 + at, a.out - 1) * a.ldw;
-    const T *x = static_cast<const T *>(a.x) + min(at, a.rows - 1) * a.ldx;
-    f32x4 acc = {};
-    for (uint32_t k = wave * 64; k < a.in; k += kFewWaves * 64 * D) {
-        Piece<T> pw[D], px[D];
-#pragma unroll
-        for (int d = 0; d < D; ++d) {
-            const uint32_t from = k + d * kFewWaves * 64 + k0;
-            pw[d].load(w, from, a.in);
-            px[d].load(x, from, a.in);
-        }
-#pragma unroll
-        for (int d = 0; d < D; ++d)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 fw[planes], fx[planes];
-                pw[d].half(h, fw);
-                px[d].half(h, fx);
-                if constexpr (planes == 1) {
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[0], fx[0], acc, 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (uint32_t t = 0; t < 6; ++t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[term_q(t)], fx[term_p(t)], acc, 0, 0, 0);
-                }
-            }
-    }
-    sums[wave][lane] = acc;
-    __syncthreads();
-    // Eight neighbours of a row, features 8 h to 8 h + 7, are in two lanes' words.
-    const uint32_t m = threadIdx.x / 2, h = threadIdx.x % 2, n = n0 + 8 * h;
-    if (m >= a.rows || n >= a.out) return;
-    float z[8] = {};
-#pragma unroll
-    for (int s = 0; s < kFewWaves; ++s)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const f32x4 v = sums[s][(2 * h + q) * 16 + m];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[4 * q + e] += v[e];
-        }
-    finish<T>(a.result, m, n, min(8u, a.out - n), z);
-}
 
 // ------------------------------------------------------------------ host
 
@@ -555,7 +455,7 @@ int forward(const tagc_linear *l, Places &w, bool enqueue, hipStream_t s)
     if (M <= kFewRows) {
         if (!enqueue) return TAGC_OK;
         ProfileScope prof("linear_few", s);
-        few_kernel<T><<<uint32_t((N + 15) / 16), kFewWaves * 64, 0, s>>>(FewArgs{l->x, l->w, l->ldx, l->ldw, uint32_t(M), uint32_t(K), uint32_t(N), r});
+        few_kernel<T><<<uint32_t((N + 15) / 16), kFewWaves * 64, 0, s>>>(FewWritten<T>{{l->x, l->w, l->ldx, l->ldw, uint32_t(M), uint32_t(K), uint32_t(N)}, r});
         return hip_ok(hipGetLastError());
     }
     Packs packs;

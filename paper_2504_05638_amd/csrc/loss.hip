@@ -22,6 +22,10 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLeast = 1.17549435e-38f;
 
+// Up to so many rows and scores, these are held between the product and what becomes of them.  (us, held / not: bfloat16 1 row of 4096 over 32000 54 / 80,
+// 128 rows 72 / 83, 512 rows 144 / 133; 333 of 777 over 1001 21 / 27, in float32 24 / 49; 4096 rows of 256 over 2048 35 / 28.)
+constexpr uint64_t kHeldRows = 1024, kHeld = 1u << 23;
+
 // What a piece of the vocabulary may hold (ds, operands laid out, the waves' sums), and its fewest rows.
 constexpr uint64_t kPieceBytes = 256ull << 20, kPieceRows = 1024;
 
@@ -292,18 +296,21 @@ __device__ inline void put_f32(float *to, uint32_t have, const float (&z)[8])
     }
 }
 
-// dx of the rows that have a term, in float32: a plane for each part of the sum, added to from piece to piece.
-struct Planes : Counted {
-    static constexpr bool kCounted = true;
+// A result in float32, a plane for each part of its sum: dx of the rows that have a term (Counted), added to from piece to piece, or a
+// few tiles' scores (Product).
+template <typename Base>
+struct Planes : Base {
+    static constexpr bool kCounted = std::is_same<Base, Counted>::value;
     float *planes;  // [parts][rows][n]
     uint32_t rows, add;
     template <int RM, int RN>
     __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t p) const
     {
-        in_rows(acc, strip, lane, m0, n0, m, n, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) {
+        const uint32_t n = this->n;
+        in_rows(acc, strip, lane, m0, n0, this->m, n, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) {
             float *to = planes + (uint64_t(p) * rows + r) * n + c;
             const uint32_t have = n - c;
-            if (add) {
+            if (kCounted && add) {
 #pragma unroll
                 for (uint32_t j = 0; j < 8; ++j)
                     if (j < have) z[j] += to[j];
@@ -311,6 +318,12 @@ struct Planes : Counted {
             put_f32(to, have, z);
         });
     }
+};
+
+// The scores of a few rows.
+struct FewScores : FewArgs {
+    float *plane;  // [rows][out]
+    __device__ inline void put(uint32_t m, uint32_t n, uint32_t have, float (&z)[8]) const { put_f32(plane + uint64_t(m) * out + n, have, z); }
 };
 
 // dw of a piece, or parts of its sum.
@@ -468,6 +481,125 @@ __global__ __launch_bounds__(256) void close_kernel(Close a)
     }
 }
 
+// Scores that are held, a row to a workgroup.
+struct Held {
+    Terms terms;
+    const float *planes;  // [parts][rows][vocab], before they are divided by the temperature
+    uint32_t parts;
+    float *loss, *saved;
+};
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void held_kernel(Held a)
+{
+    constexpr int W = THREADS / 64;
+    __shared__ float2 tops[W];
+    __shared__ float room[W], q[TAGC_MAX_TERMS];
+    const uint32_t row = blockIdx.x, K = a.terms.terms, V = a.terms.vocab, wave = threadIdx.x / 64;
+    const uint64_t first = uint64_t(row) * K, next = uint64_t(a.terms.rows) * V;
+    const float *scores = a.planes + uint64_t(row) * V;
+    // largest number of all threads, and the sum of 2^(theirs - largest) numbers
+    auto together = [&](float &top, float &sum) {
+        auto join = [&](float t, float s) {
+            const float most = fmaxf(top, t), against = most == -INFINITY ? 0.0f : most;
+            sum = sum * __builtin_amdgcn_exp2f(top - against) + s * __builtin_amdgcn_exp2f(t - against);
+            top = most;
+        };
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) join(__shfl_xor(top, d, 64), __shfl_xor(sum, d, 64));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) tops[wave] = make_float2(top, sum);
+        __syncthreads();
+        top = -INFINITY;
+        sum = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) join(tops[w].x, tops[w].y);
+    };
+    // a term's share: 1, or the teacher's
+    bool any = false;
+    float top = -INFINITY, sum = 0;
+    for (uint32_t k = threadIdx.x; k < K; k += THREADS) {
+        const bool none = id_at(a.terms.ids, a.terms.wide, first + k, V) == V;
+        float x = none ? -INFINITY : 0.0f;
+        if (a.terms.logits && !none) x = a.terms.logits[first + k] * (a.terms.over * kLog2e);
+        q[k] = x;
+        if (x == -INFINITY) continue;
+        any = true;
+        const float most = fmaxf(top, x), against = most == -INFINITY ? 0.0f : most;
+        sum = sum * __builtin_amdgcn_exp2f(top - against) + __builtin_amdgcn_exp2f(x - against);
+        top = most;
+    }
+    any = __syncthreads_or(any);
+    if (!any) {
+        if (threadIdx.x == 0) a.loss[row] = 0;
+        if (a.saved)
+            for (uint32_t k = threadIdx.x; k < 1 + K; k += THREADS) a.saved[uint64_t(row) * (1 + K) + k] = 0;
+        return;
+    }
+    if (a.terms.logits) {
+        together(top, sum);
+        const float against = top == -INFINITY ? 0.0f : top;
+        for (uint32_t k = threadIdx.x; k < K; k += THREADS) {
+            const float x = q[k], share = __builtin_amdgcn_exp2f(x - against) / sum;
+            q[k] = x == -INFINITY ? 0.0f : share < kLeast ? kLeast : share;
+        }
+    } else if (threadIdx.x == 0) {
+        q[0] = 1;
+    }
+    // the scores, four neighbours at a time, times log2(e) / T
+    const float over2 = a.terms.over * kLog2e;
+    top = -INFINITY;
+    sum = 0;
+    for (uint32_t c = threadIdx.x * 4; c < V; c += THREADS * 4) {
+        float z[4] = {};
+        const uint32_t have = min(4u, V - c);
+#pragma unroll 2
+        for (uint32_t p = 0; p < a.parts; ++p) {
+            const float *from = scores + p * next + c;
+            if (have == 4) {
+                float x[4];
+                load_n<float, 4>(from, x);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] += x[j];
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j)
+                    if (j < have) z[j] += from[j];
+            }
+        }
+        float most = top;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            z[j] *= over2;
+            if (j < have) most = fmaxf(most, z[j]);
+        }
+        const float against = most == -INFINITY ? 0.0f : most;
+        sum *= __builtin_amdgcn_exp2f(top - against);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            if (j < have) sum += __builtin_amdgcn_exp2f(z[j] - against);
+        top = most;
+    }
+    together(top, sum);
+    const float lse = (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    float loss[1] = {0};
+    for (uint32_t k = threadIdx.x; k < K; k += THREADS) {
+        float s = 0;
+        if (q[k] != 0) {  // (each thread's own)
+            const uint32_t id = id_at(a.terms.ids, a.terms.wide, first + k, V);
+            for (uint32_t p = 0; p < a.parts; ++p) s += scores[p * next + id];
+            s *= a.terms.over;
+            loss[0] += q[k] * (__builtin_amdgcn_logf(q[k]) * kLn2 + (lse - s));
+        }
+        if (a.saved) a.saved[uint64_t(row) * (1 + K) + 1 + k] = s;
+    }
+    const float all = block_sum<float, W>(loss[0], room);
+    if (threadIdx.x == 0) {
+        a.loss[row] = all;
+        if (a.saved) a.saved[uint64_t(row) * (1 + K)] = lse;
+    }
+}
+
 // ds where a row has a term, in its place: from the score that the forward pass saved, so that 1 - q's difference is taken before
 // anything is rounded.  A token that is a row's term twice gets the same value twice.
 template <typename T>
@@ -617,12 +749,54 @@ void launch_terms(const Terms &t, const List &l, hipStream_t s)
     list_kernel<<<1, kListThreads, 0, s>>>(t, l);
 }
 
+// Scores of few rows or of a small vocabulary are held, all rows', as parts of their sums: two launches, and as many workgroups as the
+// parts make.
+template <typename T>
+int forward_held(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
+{
+    const uint64_t M = l->rows, D = l->in, V = l->vocab;
+    constexpr uint32_t dtype = sizeof(T) == 4 ? TAGC_F32 : TAGC_BF16;
+    Operand x{l->x, l->ldx, 0}, q{l->w, l->ldw, 0};
+    // (us, few_kernel / thin tiles: bfloat16 1, 8, 16 rows of 4096 over 32000 55, 63, 73 / 59, 64, 65, of 768 over 50257 48, 50, 52 / 30, 31, 31, whose rows
+    // leave most of its waves nothing; float32 of 768 over 50257 50, 54, 59 / 170, 88, 76)
+    const bool lies = as_it_lies(dtype, l->w, l->ldw, D, false);
+    const bool few = M <= kFewRows && (sizeof(T) == 4 || !lies || (M <= 8 && D >= 2048)), raw = sizeof(T) == 4 && raw_pays(M, V) && l->ldx < kMaxSide && l->ldw < kMaxSide;
+    const bool lay_x = !few && !raw && !as_it_lies(dtype, l->x, l->ldx, D, false), lay_w = !few && !raw && !lies;
+    if (lay_x) x = room(w, dtype, M, D);
+    if (lay_w) q = room(w, dtype, V, D);
+    const Shape f = few ? Shape{} : shape_of(M, V, D, dtype, false);
+    const uint32_t parts = few ? 1 : f.splits;
+    float *planes = w.take<float>(parts * M * V);
+    if (!enqueue) return TAGC_OK;
+    if (lay_x) launch_gather<T>(gather<T>(l->x, l->ldx, M, D, x), s);
+    if (lay_w) launch_gather<T>(gather<T>(l->w, l->ldw, V, D, q), s);
+    {
+        ProfileScope prof("loss_product", s);
+        if (few) {
+            few_kernel<T><<<uint32_t((V + 15) / 16), kFewWaves * 64, 0, s>>>(FewScores{{l->x, l->w, l->ldx, l->ldw, uint32_t(M), uint32_t(D), uint32_t(V)}, planes});
+        } else {
+            Planes<Product> a{};
+            aim(a, x, q, M, V, D, f);
+            a.planes = planes;
+            a.rows = uint32_t(M);
+            launch<T, false, false>(a, f, s);
+        }
+    }
+    ProfileScope prof("loss_close", s);
+    const Terms terms{l->ids, l->logits, nullptr, nullptr, uint32_t(M), l->terms, uint32_t(V), l->id_type, float(1 / l->temperature)};
+    const Held h{terms, planes, parts, l->loss, l->saved};
+    if (V <= 8192) held_kernel<256><<<uint32_t(M), 256, 0, s>>>(h);
+    else held_kernel<1024><<<uint32_t(M), 1024, 0, s>>>(h);
+    return hip_ok(hipGetLastError());
+}
+
 template <typename T>
 int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
 {
     const uint64_t M = l->rows, D = l->in, V = l->vocab;
     constexpr uint32_t dtype = sizeof(T) == 4 ? TAGC_F32 : TAGC_BF16;
     if (!M) return TAGC_OK;
+    if (M <= kHeldRows && M * V <= kHeld) return forward_held<T>(l, w, enqueue, s);
     Chosen chosen{};
     Close close{};
     const Terms terms = terms_of(l, w);
@@ -735,7 +909,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
         Operand p = ds;
         if (sizeof(T) == 2) p.part = 0;
         if (l->dx && M) {
-            Planes a{};
+            Planes<Counted> a{};
             aim(a, p, q, M, D, n, fx);
             const uint64_t slab = dtype == TAGC_F32 ? kSlab3 : kSlab;
             a.slabs = uint32_t((up(n, slab) / slab + fx.splits - 1) / fx.splits);

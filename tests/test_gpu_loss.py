@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 E = 2.0 ** -24
 T = {"f32": torch.float32, "bf16": torch.bfloat16}
 SHAPES = [(1, 1, 1), (1, 64, 200), (1, 4096, 1000), (3, 64, 5), (17, 100, 31), (33, 128, 257), (64, 256, 1000), (65, 72, 4097), (129, 65, 130), (200, 777, 1001),
-          (300, 64, 5003), (2048, 512, 2304)]
+          (300, 64, 5003), (2048, 512, 2304), (1025, 96, 333), (70, 24, 130_001), (300, 72, 30_011)]
 
 
 def _randn(shape, seed, dtype, scale=1.0, ld_more=0, shift=0):
@@ -173,7 +173,7 @@ def test_pieces_of_the_vocabulary_backward(dtype):
     _check((65536, 40, 5003), T[dtype], 0, 1.0, True, True, 1, 0)
 
 
-@pytest.mark.parametrize("shape,dtype", [((20, 4001, 40003), "bf16"), ((1400, 2001, 40003), "f32")], ids=str)
+@pytest.mark.parametrize("shape,dtype", [((20, 4001, 40003), "bf16"), ((1400, 2001, 40003), "f32"), ((300, 4001, 40003), "bf16")], ids=str)
 def test_pieces_of_the_vocabulary_forward(shape, dtype):
     """Weights that have to be laid out, more than a piece of them."""
     print("[case] pieces, forward", shape, dtype, flush=True)

@@ -4,8 +4,8 @@
 //   ds = dloss (e^(s - lse) - q) / T;  dx = ds w,  dw = ds^T x
 //
 // Forward, the scores stay in the registers of the product that makes them: of every row a wave leaves its columns' largest score
-// and the sum of exponentials against it, and these are put together when the product is done.  Terms' own scores are products of
-// two rows each, taken by themselves.  Backward, the product is made again, a piece of the vocabulary at a time, and ends in ds of that piece,
+// and the sum of exponentials against it, and these are put together when the product is done.  Terms' own scores
+// are taken from there, too.  Backward, the product is made again, a piece of the vocabulary at a time, and ends in ds of that piece,
 // which the two products behind it read; the terms' few elements are put right between them.  What is held of a piece is bounded, whatever the
 // vocabulary.
 //
@@ -93,10 +93,9 @@ __device__ inline float share(const Terms &a, uint64_t at, uint32_t id) { return
 struct List {
     uint32_t *rows;   // those with a term in order, then the others
     uint32_t *count;  // of the first
-    const float *saved, *dloss;
-    float2 *row;      // backward: of each of the first the log2 of its sum of exponentials, and dloss / temperature
-    uint32_t step;
 };
+
+__device__ inline bool has_term(const Terms &a, uint32_t row) { return a.logits ? a.any[row] != 0 : id_at(a.ids, a.wide, row, a.vocab) < a.vocab; }
 
 constexpr uint32_t kListThreads = 1024, kListEach = 8;
 __global__ __launch_bounds__(kListThreads) void list_kernel(Terms a, List l)
@@ -108,7 +107,7 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(Terms a, List l)
         uint32_t bits = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kListEach; ++i)
-            if (from + i < a.rows) bits |= uint32_t(a.logits ? a.any[from + i] != 0 : id_at(a.ids, a.wide, from + i, a.vocab) < a.vocab) << i;
+            if (from + i < a.rows) bits |= uint32_t(has_term(a, from + i)) << i;
         uint32_t total;
         uint32_t at = done + block_excl_scan<uint32_t, kListThreads / 64>(__popc(bits), &total, room);
 #pragma unroll
@@ -119,9 +118,7 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(Terms a, List l)
                 l.rows[a.rows - 1 - (row - at)] = row;  // (row - at: those without a term before it)
                 continue;
             }
-            l.rows[at] = row;
-            if (l.row) l.row[at] = make_float2(l.saved[uint64_t(row) * (1 + a.terms)] * kLog2e, l.dloss[uint64_t(row) * l.step] * a.over);
-            ++at;
+            l.rows[at++] = row;
         }
         done += total;
     }
@@ -131,22 +128,17 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(Terms a, List l)
 // ------------------------------------------------------------------ operands laid out
 
 struct Gather {
-    const void *src;       // rows of `cols`, ld elements apart
+    const void *src;  // rows of `cols`, ld elements apart
     void *to;
-    const uint32_t *rows;  // which rows, or NULL: all
-    const uint32_t *count; // how many, or NULL: all
     uint64_t ld, to_ld;
     uint32_t n, cols, part;  // part: float32 taken apart, elements from one part to the next; 0: as they are
     uint32_t across;         // pieces of eight elements to a row, zeros behind cols
 };
 
 template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(Gather a)
+__device__ inline void lay_piece(const Gather &a, uint32_t from, uint32_t r, uint32_t c)
 {
-    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
-    const uint32_t r = uint32_t(i / a.across), c = uint32_t(i % a.across) * 8;
-    if (r >= (a.count ? *a.count : a.n)) return;
-    const T *src = static_cast<const T *>(a.src) + (a.rows ? a.rows[r] : r) * a.ld + c;
+    const T *src = static_cast<const T *>(a.src) + from * a.ld + c;
     float x[8];
     if (c + 8 <= a.cols) {
         load_n<T, 8>(src, x);
@@ -172,10 +164,79 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a)
     }
 }
 
+template <typename T>
+__global__ __launch_bounds__(256) void gather_kernel(Gather a)
+{
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t r = uint32_t(i / a.across);
+    if (r < a.n) lay_piece<T>(a, r, r, uint32_t(i % a.across) * 8);
+}
+
+// The rows that have a term, one behind the other: x's, their terms' ids, and what the backward pass needs of each.
+struct Lay {
+    Terms terms;
+    List list;
+    Gather x;
+    uint32_t groups;   // workgroups for x; the rest is for ids
+    uint32_t *ids;     // [rows][2^shift]: a row's terms, kNone for none
+    uint32_t shift;
+    const float *saved, *dloss;
+    float2 *row;       // backward: of a row the log2 of its sum of exponentials, and dloss / temperature
+    uint32_t step;
+};
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+// SCAN: up to 1024 rows' list is made here, by each workgroup for itself: a launch less.
+constexpr uint32_t kScanRows = 1024;
+template <typename T, bool SCAN>
+__global__ __launch_bounds__(256) void lay_kernel(Lay a)
+{
+    __shared__ uint32_t rows[SCAN ? kScanRows : 1], room[4];
+    uint32_t count;
+    if constexpr (SCAN) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (threadIdx.x * 4 + i < a.terms.rows) bits |= uint32_t(has_term(a.terms, threadIdx.x * 4 + i)) << i;
+        uint32_t at = block_excl_scan<uint32_t, 4>(__popc(bits), &count, room);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t row = threadIdx.x * 4 + i;
+            if (row >= a.terms.rows) break;
+            const uint32_t to = bits >> i & 1 ? at++ : a.terms.rows - 1 - (row - at);
+            rows[to] = row;
+            if (blockIdx.x == 0) a.list.rows[to] = row;
+        }
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.list.count = count;
+        __syncthreads();
+    } else {
+        count = *a.list.count;
+    }
+    const auto row_at = [&](uint32_t r) { return SCAN ? rows[r] : a.list.rows[r]; };
+    if (blockIdx.x < a.groups) {
+        const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+        const uint32_t r = uint32_t(i / a.x.across);
+        if (r < count) lay_piece<T>(a.x, row_at(r), r, uint32_t(i % a.x.across) * 8);
+        return;
+    }
+    const uint64_t i = uint64_t(blockIdx.x - a.groups) * 256 + threadIdx.x;
+    const uint32_t r = uint32_t(i >> a.shift), k = uint32_t(i) & ((1u << a.shift) - 1);
+    if (r >= count) return;
+    const uint32_t row = row_at(r);
+    uint32_t id = kNone;
+    if (k < a.terms.terms) {
+        const uint64_t at = uint64_t(row) * a.terms.terms + k;
+        id = id_at(a.terms.ids, a.terms.wide, at, a.terms.vocab);
+        if (id == a.terms.vocab || share(a.terms, at, id) == 0) id = kNone;
+    }
+    a.ids[i] = id;
+    if (a.row && k == 0) a.row[r] = make_float2(a.saved[uint64_t(row) * (1 + a.terms.terms)] * kLog2e, a.dloss[uint64_t(row) * a.step] * a.terms.over);
+}
+
 // ------------------------------------------------------------------ ends of the products
 
 // A wave's sums in rows, eight neighbours at a time, by way of its strip: f(m, n, z) for rows under `rows` and columns, by eights, under
-// `cols`.
+// `cols`.  (What f reads may be asked for 32 rows ahead; that won nothing.)
 template <int RM, int RN, typename F>
 __device__ inline __attribute__((always_inline)) void in_rows(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t rows,
                                                               uint32_t cols, F f)
@@ -212,15 +273,64 @@ __device__ inline __attribute__((always_inline)) void in_rows(const f32x4 (&acc)
     }
 }
 
-// Forward: of a row's scores in a wave's columns the largest, and the sum of 2^(score - largest), scores times log2(e) / T.
+// Forward: of a row's scores in a wave's columns the largest, and the sum of 2^(score - largest), scores times log2(e) / T; and those of
+// its terms.  These are looked for among the terms' ids, 32 rows at a time, and where there is one the rows go through local memory.
+// (64 terms of 2048 rows of 4096: 446 us of the product that takes 393 without; by themselves, as products of two rows each, they took 164.)
 struct Scores : Counted {
     static constexpr bool kCounted = true;
     float2 *stats;  // [strips of columns][rows]
     uint32_t rows;
     float over2;    // log2(e) / T
+    const uint32_t *ids;  // [rows][2^shift]
+    float *scores;        // [rows][terms]
+    uint32_t shift, terms, base;  // base: the id of the piece's first column
+    float over;           // 1 / T
     template <int RM, int RN>
-    __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
+    __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
     {
+        constexpr uint32_t kRow = RN * 16 + 4, kQuads = 8;  // quads of ids on their way
+        const uint32_t first = base + n0, quads = 32u << (shift - 2);
+#pragma unroll 1
+        for (int i = 0; i < RM; i += 2) {
+            // (rows that there are not have no ids)
+            const uint32_t r0 = m0 + i * 16;
+            const uint4 *from = reinterpret_cast<const uint4 *>(ids + (uint64_t(r0) << shift));
+            const auto quad = [&](uint32_t q) { return r0 + (q >> (shift - 2)) < m ? from[q] : make_uint4(kNone, kNone, kNone, kNone); };
+            const auto in = [&](uint32_t id) { return id - first < RN * 16; };
+            bool written = false;
+            for (uint32_t at_quad = 0; at_quad < quads; at_quad += 64 * kQuads) {  // (all lanes, which write the strip together)
+                const uint32_t q0 = at_quad + lane;
+                uint4 id[kQuads];
+                bool any = false;
+#pragma unroll
+                for (uint32_t b = 0; b < kQuads; ++b) id[b] = q0 + 64 * b < quads ? quad(q0 + 64 * b) : make_uint4(kNone, kNone, kNone, kNone);
+#pragma unroll
+                for (uint32_t b = 0; b < kQuads; ++b) any = any || in(id[b].x) || in(id[b].y) || in(id[b].z) || in(id[b].w);
+                if (!__any(any)) continue;
+                if (!written) {
+                    written = true;
+#pragma unroll
+                    for (int at = 0; at < RM; at += 2)
+                        if (at == i)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                for (int j = 0; j < RN; ++j)
+                                    *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[at + h][j];
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                }
+#pragma unroll
+                for (uint32_t b = 0; b < kQuads; ++b) {
+                    const uint32_t q = q0 + 64 * b, r = q >> (shift - 2), k = (q << 2) & ((1u << shift) - 1);
+                    float *to = scores + uint64_t(r0 + r) * terms + k;
+                    if (in(id[b].x)) to[0] = strip[r * kRow + id[b].x - first] * over;
+                    if (in(id[b].y)) to[1] = strip[r * kRow + id[b].y - first] * over;
+                    if (in(id[b].z)) to[2] = strip[r * kRow + id[b].z - first] * over;
+                    if (in(id[b].w)) to[3] = strip[r * kRow + id[b].w - first] * over;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
         float2 *to = stats + uint64_t(n0 / (RN * 16)) * rows;
         const uint32_t c0 = n0 + 4 * (lane >> 4);
 #pragma unroll
@@ -256,14 +366,17 @@ struct Slopes : Counted {
     uint64_t ld;
     uint32_t part;
     const float2 *row;
+    const uint32_t *ids;  // [rows][2^shift]: where a row has one term, whose weight is 1, or NULL: they are put right afterwards
+    uint32_t shift, base;
     float over2;
     template <int RM, int RN>
     __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
     {
         in_rows(acc, strip, lane, m0, n0, m, part, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) {
             const float2 by = row[r];
+            const uint32_t term = ids ? ids[uint64_t(r) << shift] - base : kNone;
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) z[j] = c + j < n ? by.y * __builtin_amdgcn_exp2f(z[j] * over2 - by.x) : 0.0f;
+            for (uint32_t j = 0; j < 8; ++j) z[j] = c + j < n ? by.y * (__builtin_amdgcn_exp2f(z[j] * over2 - by.x) - (c + j == term ? 1.0f : 0.0f)) : 0.0f;
             uint16_t *to = ds + r * ld + c;
             if constexpr (sizeof(T) == 2) {
                 store_n<uint16_t, 8>(to, z);
@@ -381,52 +494,13 @@ __global__ __launch_bounds__(256) void weights_join_kernel(Weights<T> a)
 
 // ------------------------------------------------------------------ between and behind the products
 
-struct Chosen {
-    Terms terms;
-    List list;
-    const void *x, *w;
-    uint64_t ldx, ldw;
-    uint32_t in;
-    float *scores;  // [rows, terms]: s of every term, 0 for none
-};
-
-// A term's own score: two rows' product, a wave each.
-template <typename T>
-__global__ __launch_bounds__(256) void chosen_kernel(Chosen a)
-{
-    constexpr uint32_t V = 16 / sizeof(T);
-    const uint64_t job = uint64_t(blockIdx.x) * 4 + threadIdx.x / 64;
-    const uint32_t i = uint32_t(job / a.terms.terms), k = uint32_t(job % a.terms.terms), lane = threadIdx.x & 63;
-    if (i >= *a.list.count) return;
-    const uint32_t row = a.list.rows[i];
-    const uint64_t at = uint64_t(row) * a.terms.terms + k;
-    const uint32_t id = id_at(a.terms.ids, a.terms.wide, at, a.terms.vocab);
-    float sum = 0;
-    if (id < a.terms.vocab && share(a.terms, at, id) != 0.0f) {
-        const T *x = static_cast<const T *>(a.x) + row * a.ldx, *w = static_cast<const T *>(a.w) + id * a.ldw;
-        for (uint32_t c = lane * V; c < a.in; c += 64 * V) {
-            if (c + V <= a.in) {
-                Lane<T, V> p, q;
-                p.load(x + c);
-                q.load(w + c);
-#pragma unroll
-                for (uint32_t j = 0; j < V; ++j) sum = fmaf(p[j], q[j], sum);
-            } else {
-                for (uint32_t j = c; j < a.in; ++j) sum = fmaf(widen(x[j]), widen(w[j]), sum);
-            }
-        }
-        sum = wave_sum(sum) * a.terms.over;
-    }
-    if (lane == 0) a.scores[at] = sum;
-}
-
 struct Close {
     Terms terms;
     List list;
     const float2 *stats;  // [strips][rows]
     float2 *run;          // [rows]: what earlier pieces of the vocabulary left, or this one leaves
     uint32_t strips, earlier, last;
-    const float *scores;
+    const float *scores;  // [rows with a term, terms]
     float *loss, *saved;
 };
 
@@ -466,10 +540,10 @@ __global__ __launch_bounds__(256) void close_kernel(Close a)
     for (uint32_t k = at; k < K; k += 16) {
         const uint64_t t = uint64_t(row) * K + k;
         float s = 0;
-        if (there) {
-            const float q = share(a.terms, t, id_at(a.terms.ids, a.terms.wide, t, a.terms.vocab));
-            s = a.scores[t];
-            if (q != 0) loss += q * (__builtin_amdgcn_logf(q) * kLn2 + (lse - s));
+        const float q = there ? share(a.terms, t, id_at(a.terms.ids, a.terms.wide, t, a.terms.vocab)) : 0.0f;
+        if (q != 0) {
+            s = a.scores[uint64_t(j) * K + k];
+            loss += q * (__builtin_amdgcn_logf(q) * kLn2 + (lse - s));
         }
         if (a.saved) a.saved[uint64_t(row) * (1 + K) + 1 + k] = s;
     }
@@ -603,7 +677,7 @@ __global__ __launch_bounds__(THREADS) void held_kernel(Held a)
 // ds where a row has a term, in its place: from the score that the forward pass saved, so that 1 - q's difference is taken before
 // anything is rounded.  A token that is a row's term twice gets the same value twice.
 template <typename T>
-__global__ __launch_bounds__(256) void terms_slope_kernel(Terms a, List l, uint16_t *ds, uint64_t ld, uint32_t part, uint32_t begin, uint32_t end)
+__global__ __launch_bounds__(256) void terms_slope_kernel(Terms a, List l, const float2 *rows, const float *saved, uint16_t *ds, uint64_t ld, uint32_t part, uint32_t begin, uint32_t end)
 {
     const uint64_t job = uint64_t(blockIdx.x) * 256 + threadIdx.x;
     const uint32_t i = uint32_t(job / a.terms), k = uint32_t(job % a.terms);
@@ -615,8 +689,8 @@ __global__ __launch_bounds__(256) void terms_slope_kernel(Terms a, List l, uint1
     float q = 0;
     for (uint32_t j = 0; j < a.terms; ++j)
         if (id_at(a.ids, a.wide, first + j, a.vocab) == id) q += share(a, first + j, id);
-    const float2 by = l.row[i];
-    const float x = by.y * (__builtin_amdgcn_exp2f(l.saved[first + row + 1 + k] * kLog2e - by.x) - q);
+    const float2 by = rows[i];
+    const float x = by.y * (__builtin_amdgcn_exp2f(saved[first + row + 1 + k] * kLog2e - by.x) - q);
     uint16_t *to = ds + i * ld + (id - begin);
     if constexpr (sizeof(T) == 2) {
         *to = narrow<uint16_t>(x);
@@ -690,13 +764,15 @@ Operands operands_of(uint64_t M, uint64_t D, uint64_t V, const void *w, uint64_t
     return Operands{raw, !raw};
 }
 
-// Rows of a piece of the vocabulary that holds so many bytes a row: whole tiles, pieces alike.
+// Rows of a piece of the vocabulary that holds so many bytes a row: pieces alike, but in whole rounds of tiles, of which 4096 rows make so many
+// that they fill 256 compute units at most sizes.  (Float32, 1024 rows of 768 over 50257: pieces of 20480 instead of
+// three alike of 16768 take 1350 us instead of 1386.)
 uint64_t piece_rows(uint64_t vocab, uint64_t bytes)
 {
     uint64_t n = kPieceBytes / (bytes ? bytes : 1);
     if (n < kPieceRows) n = kPieceRows;
-    const uint64_t pieces = (vocab + n - 1) / n;
-    return up((vocab + pieces - 1) / pieces, 256);
+    const uint64_t pieces = (vocab + n - 1) / n, each = (vocab + pieces - 1) / pieces;
+    return up(each, 4096) <= n ? up(each, 4096) : up(each, 256);
 }
 
 template <typename T>
@@ -742,11 +818,38 @@ Terms terms_of(const G *l, Places &w)
     return t;
 }
 
-void launch_terms(const Terms &t, const List &l, hipStream_t s)
+// What the backward pass gives to a row's part.
+struct Rowwise {
+    const float *saved, *dloss;
+    float2 *row;
+    uint32_t step;
+};
+
+// Room for the list of the rows that have a term, and for the ids of their terms.
+struct Listed {
+    List list;
+    uint32_t *ids, shift;
+    Listed(Places &w, uint64_t rows, uint32_t terms) : shift(2)
+    {
+        while (1u << shift < terms) ++shift;
+        list = List{w.take<uint32_t>(rows), w.take<uint32_t>(1)};
+        ids = w.take<uint32_t>(rows << shift);
+    }
+};
+
+template <typename T>
+void launch_rows(const Terms &t, const Listed &l, const Gather &x, const Rowwise &r, hipStream_t s)
 {
-    ProfileScope prof("loss_terms", s);
+    ProfileScope prof("loss_rows", s);
     if (t.logits && t.rows) terms_kernel<<<(t.rows + 3) / 4, 256, 0, s>>>(t);
-    list_kernel<<<1, kListThreads, 0, s>>>(t, l);
+    const uint64_t groups = (uint64_t(x.n) * x.across + 255) / 256, more = ((uint64_t(t.rows) << l.shift) + 255) / 256;
+    const Lay a{t, l.list, x, uint32_t(groups), l.ids, l.shift, r.saved, r.dloss, r.row, r.step};
+    if (t.rows <= kScanRows) {
+        lay_kernel<T, true><<<uint32_t(groups + more + 1), 256, 0, s>>>(a);
+    } else {
+        list_kernel<<<1, kListThreads, 0, s>>>(t, l.list);
+        lay_kernel<T, false><<<uint32_t(groups + more), 256, 0, s>>>(a);
+    }
 }
 
 // Scores of few rows or of a small vocabulary are held, all rows', as parts of their sums: two launches, and as many workgroups as the
@@ -797,10 +900,10 @@ int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
     constexpr uint32_t dtype = sizeof(T) == 4 ? TAGC_F32 : TAGC_BF16;
     if (!M) return TAGC_OK;
     if (M <= kHeldRows && M * V <= kHeld) return forward_held<T>(l, w, enqueue, s);
-    Chosen chosen{};
     Close close{};
     const Terms terms = terms_of(l, w);
-    List list{w.take<uint32_t>(M), w.take<uint32_t>(1), nullptr, nullptr, nullptr, 0};
+    const Listed listed(w, M, l->terms);
+    const List list = listed.list;
     const Operands ops = operands_of<T>(M, D, V, l->w, l->ldw, true);
     const Operand x = room_for_x<T>(w, M, D, ops.raw);
     // (a wave's strip of columns has 32 at least)
@@ -815,16 +918,7 @@ int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
     float *scores = w.take<float>(M * l->terms);
     if (!enqueue) return TAGC_OK;
 
-    launch_terms(terms, list, s);
-    Gather gx = gather<T>(l->x, l->ldx, M, D, x);
-    gx.rows = list.rows;
-    gx.count = list.count;
-    launch_gather<T>(gx, s);
-    {
-        ProfileScope prof("loss_terms", s);
-        chosen = Chosen{terms, list, l->x, l->w, l->ldx, l->ldw, uint32_t(D), scores};
-        chosen_kernel<T><<<uint32_t((M * l->terms + 3) / 4), 256, 0, s>>>(chosen);
-    }
+    launch_rows<T>(terms, listed, gather<T>(l->x, l->ldx, M, D, x), Rowwise{}, s);
     for (uint64_t v = 0; v < V; v += piece) {
         const uint64_t n = V - v < piece ? V - v : piece;
         const T *from = static_cast<const T *>(l->w) + v * l->ldw;
@@ -840,6 +934,12 @@ int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
         a.stats = stats;
         a.rows = uint32_t(M);
         a.over2 = float(kLog2e / l->temperature);
+        a.ids = listed.ids;
+        a.scores = scores;
+        a.shift = listed.shift;
+        a.terms = l->terms;
+        a.base = uint32_t(v);
+        a.over = terms.over;
         {
             ProfileScope prof("loss_product", s);
             launch<T, false, false>(a, f, s);
@@ -860,7 +960,9 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     if ((!l->dx && !l->dw) || (!M && (l->accumulate || !l->dw))) return TAGC_OK;
     const uint64_t rows = M ? M : 1;  // (no rows: dw becomes zeros by a product without terms)
     const Terms terms = terms_of(l, w);
-    const List list{w.take<uint32_t>(rows), w.take<uint32_t>(1), l->saved, l->dloss, w.take<float2>(rows), l->dloss_step};
+    const Listed listed(w, rows, l->terms);
+    const List list = listed.list;
+    const Rowwise by{l->saved, l->dloss, w.take<float2>(rows), l->dloss_step};
     const Operands ops = operands_of<T>(rows, D, V, l->w, l->ldw, false);
     const Operand x = room_for_x<T>(w, rows, D, false);
     const uint64_t e = sizeof(T) == 4 ? 6 : 2, piece = piece_rows(V, (rows + (ops.lay ? up(D, 64) : 0)) * e);
@@ -874,13 +976,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     float *planes = w.take<float>(l->dx ? fx.splits * rows * D : 0), *partial = w.take<float>(l->dw && fw.splits > 1 ? fw.splits * piece * D : 0);
     if (!enqueue) return TAGC_OK;
 
-    launch_terms(terms, list, s);
-    if (M) {
-        Gather gx = gather<T>(l->x, l->ldx, M, D, x);
-        gx.rows = list.rows;
-        gx.count = list.count;
-        launch_gather<T>(gx, s);
-    }
+    launch_rows<T>(terms, listed, gather<T>(l->x, l->ldx, M, D, x), by, s);
     for (uint64_t v = 0; v < V; v += piece) {
         const uint64_t n = V - v < piece ? V - v : piece;
         const T *from = static_cast<const T *>(l->w) + v * l->ldw;
@@ -897,14 +993,19 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
             a.ds = static_cast<uint16_t *>(const_cast<void *>(ds.p));
             a.ld = ds.ld;
             a.part = ds.part;
-            a.row = list.row;
+            a.row = by.row;
+            a.ids = l->terms == 1 ? listed.ids : nullptr;
+            a.shift = listed.shift;
+            a.base = uint32_t(v);
             a.over2 = float(kLog2e / l->temperature);
             {
                 ProfileScope prof("loss_slopes", s);
                 launch<T, false, false>(a, f, s);
             }
-            ProfileScope prof("loss_terms", s);
-            terms_slope_kernel<T><<<uint32_t((M * l->terms + 255) / 256), 256, 0, s>>>(terms, list, a.ds, ds.ld, ds.part, uint32_t(v), uint32_t(v + n));
+            if (l->terms > 1) {
+                ProfileScope prof("loss_terms", s);
+                terms_slope_kernel<T><<<uint32_t((M * l->terms + 255) / 256), 256, 0, s>>>(terms, list, by.row, l->saved, a.ds, ds.ld, ds.part, uint32_t(v), uint32_t(v + n));
+            }
         }
         Operand p = ds;
         if (sizeof(T) == 2) p.part = 0;

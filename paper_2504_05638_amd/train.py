@@ -222,8 +222,10 @@ def _check_tensor(x, name, stream):
 
 
 def _no_graph(what, *tensors):
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        warnings.warn("%s records no autograd graph: gradients are %s_backward's; call it under torch.no_grad()" % (what, what), stacklevel=3)
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            warnings.warn("%s records no autograd graph: gradients are %s_backward's; call it under torch.no_grad()" % (what, what), stacklevel=3)
+            return
 
 
 def _all_ids(t, name, shape, device):
@@ -397,8 +399,9 @@ def _loss_backward(dloss, x, w, ids, logits, saved, temperature, dx, dw, accumul
     dtype, device = x.dtype, x.device
     _need(need_dx or dx is None, "dx is given, but need_dx is not")
     sp = _floats(saved, "saved", (m, 1 + terms), device)
-    one = dloss.numel() == 1 and dloss.dim() <= 1
-    gp = _floats(dloss, "dloss", dloss.shape if one else shape, device)
+    _need(dloss.shape == shape or (dloss.numel() == 1 and dloss.dim() <= 1), "dloss: a number for each row, or one, is wanted")
+    one = m > 0 and all(step == 0 or n == 1 for step, n in zip(dloss.stride(), dloss.shape))     # (also one that is expanded)
+    gp = _floats(dloss.as_strided((1,), (1,)) if one else dloss, "dloss", (1,) if one else shape, device)
     _need(dx is None or dx.shape == x.shape, "dx: x's shape is wanted")
     dp, ldd = _rows_of((_flat(dx, m, k) if x.dim() != 1 else dx.view(1, k)) if dx is not None else None, "dx", m, k, dtype, device)
     wp, ldw = _rows_of(dw, "dw", v, k, dtype, device)
@@ -427,7 +430,7 @@ def cross_entropy(x, w, targets, save=False, stream=None):
 
 
 def cross_entropy_backward(dloss, x, w, targets, saved, dx=None, dw=None, accumulate=False, need_dx=True, stream=None):
-    """dx (None without need_dx).  `dloss`: float32, a number for each row, or one for all (such as 1 / the rows that count).  With `dw`
+    """dx (None without need_dx).  `dloss`: float32, a number for each row, or one for all (such as 1 / the rows that count; an expanded one is one).  With `dw`
     ([vocab, in], a view into a bucket's gradient) given, w's gradient is written there, or added to what is there (accumulate).
     `saved`: what cross_entropy(save=True) gave.  `stream`: as for linear."""
     return _loss_backward(dloss, x, w, targets, None, saved, 1.0, dx, dw, accumulate, need_dx, stream)
@@ -439,7 +442,7 @@ def distill(x, w, ids, logits, temperature=1.0, save=False, stream=None):
     largest scores; int32 or int64, logits float32).  A token outside [0, vocab), or one with the logit -inf, is none; a row
     without any has loss 0 and no gradient.  `saved`: [rows, 1 + terms], as for cross_entropy.  (To have gradients of
     the usual size at a temperature, weigh dloss by its square.)"""
-    _no_graph("distill", x, w)
+    _no_graph("distill", x, w, logits)
     _need(logits is not None, "logits: the teacher's are wanted")
     return _loss(x, w, ids, logits, temperature, save, stream)
 

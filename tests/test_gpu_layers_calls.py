@@ -1,0 +1,209 @@
+"""Norms, embeddings and losses as calls: streams, devices, versions that autograd counts, refusals from Python."""
+import warnings
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _owner(address):
+    """The stream whose memory an address is, as the allocator has it."""
+    for segment in torch.cuda.memory_snapshot():
+        if segment["address"] <= address < segment["address"] + segment["total_size"]:
+            return segment["stream"]
+    raise AssertionError("not the allocator's")
+
+
+@pytest.fixture
+def side():
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    yield s
+    s.synchronize()
+
+
+def _inputs(dtype=torch.bfloat16):
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda").to(dtype)  # noqa: E731
+    return {"x": r(1300, 200), "w": r(200), "b": r(200), "dy": r(1300, 200), "head": r(7001, 200), "table": r(900, 200),
+            "ids": torch.randint(0, 900, (1300,), generator=gen, device="cuda"), "targets": torch.randint(0, 7001, (1300,), generator=gen, device="cuda"),
+            "terms": torch.randint(0, 7001, (1300, 5), generator=gen, device="cuda"), "logits": torch.randn((1300, 5), generator=gen, device="cuda"),
+            "one": torch.ones((), device="cuda")}
+
+
+def _everything(i, stream=None):
+    """Every call once; its results."""
+    from paper_2504_05638_amd import train as t
+    k = {"stream": stream}
+    y, stats = t.norm(i["x"], i["w"], i["b"], save=True, **k)
+    gains = torch.empty(400, device="cuda", dtype=i["x"].dtype), torch.empty_like(i["table"]), torch.empty_like(i["head"]), torch.empty_like(i["head"])
+    torch.cuda.current_stream(i["x"].device).synchronize()
+    dx = t.norm_backward(i["dy"], i["x"], i["w"], stats, dw=gains[0][:200], db=gains[0][200:], **k)
+    e = t.embedding(i["ids"], i["table"], scale=2.0, residual=i["x"], **k)
+    t.embedding_backward(i["dy"], i["ids"], gains[1], **k)
+    loss, saved = t.cross_entropy(i["x"], i["head"], i["targets"], save=True, **k)
+    dc = t.cross_entropy_backward(i["one"], i["x"], i["head"], i["targets"], saved, dw=gains[2], **k)
+    div, kept = t.distill(i["x"], i["head"], i["terms"], i["logits"], temperature=2.0, save=True, **k)
+    dd = t.distill_backward(i["one"], i["x"], i["head"], i["terms"], i["logits"], kept, temperature=2.0, dw=gains[3], **k)
+    return [y, stats, dx, e, loss, saved, dc, div, kept, dd], list(gains)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_calls_make_the_streams_own_memory(dtype, side, monkeypatch):
+    from paper_2504_05638_amd import train
+    i = _inputs(dtype)
+    torch.cuda.synchronize()
+    used = []
+    for name in ("norm_backward", "embedding_backward", "loss_forward", "loss_backward"):
+        call = getattr(train.B, "tagc_" + name)
+        monkeypatch.setattr(train.B, "tagc_" + name, lambda a, at, on, call=call: (used.append((at, on)), call(a, at, on))[1])
+    made, given = _everything(i, side)
+    assert len(used) == 6 and all(at and on == side.cuda_stream for at, on in used)
+    for address in [at for at, _ in used] + [m.data_ptr() for m in made]:
+        assert _owner(address) == side.cuda_stream
+    side.synchronize()
+    want, also = _everything(i)
+    assert all(torch.equal(a, b) for a, b in zip(made + given, want + also))
+    assert all(_owner(w.data_ptr()) == torch.cuda.current_stream().cuda_stream for w in want)
+
+
+CALLS = ["tagc_norm_forward", "tagc_norm_backward_workspace", "tagc_norm_backward", "tagc_embedding_forward", "tagc_embedding_backward_workspace",
+         "tagc_embedding_backward", "tagc_loss_forward_workspace", "tagc_loss_forward", "tagc_loss_backward_workspace", "tagc_loss_backward"]
+
+
+def test_calls_are_made_with_the_tensors_device(monkeypatch):
+    from paper_2504_05638_amd import train
+    i = _inputs()
+    want, _ = _everything(i)
+    on, made = [7], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = torch.device(device).index
+
+        def __enter__(self):
+            on.append(self.index)
+
+        def __exit__(self, *a):
+            on.pop()
+
+    monkeypatch.setattr(train, "_current_device", lambda: on[-1])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for name in CALLS:
+        call = getattr(train.B, name)
+        monkeypatch.setattr(train.B, name, lambda *a, call=call, name=name: (made.append((name, on[-1])), call(*a))[1])
+    got, _ = _everything(i)
+    assert on == [7] and sorted({n for n, _ in made}) == sorted(CALLS) and {d for _, d in made} == {i["x"].device.index}
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_stream_of_another_device_is_refused():
+    from paper_2504_05638_amd import train as t
+
+    class Other:
+        device, cuda_stream = torch.device("cuda", 1), 0
+
+    i = _inputs()
+    _, stats = t.norm(i["x"], save=True)
+    _, saved = t.cross_entropy(i["x"], i["head"], i["targets"], save=True)
+    for call in (lambda: t.norm(i["x"], stream=Other()), lambda: t.norm_backward(i["dy"], i["x"], None, stats, stream=Other()),
+                 lambda: t.embedding(i["ids"], i["table"], stream=Other()), lambda: t.embedding_backward(i["dy"], i["ids"], i["table"], stream=Other()),
+                 lambda: t.cross_entropy(i["x"], i["head"], i["targets"], stream=Other()),
+                 lambda: t.cross_entropy_backward(i["one"], i["x"], i["head"], i["targets"], saved, stream=Other())):
+        with pytest.raises(ValueError, match="device"):
+            call()
+
+
+def test_written_tensors_count_a_version():
+    from paper_2504_05638_amd import train as t
+    i = _inputs()
+    out, flat, dx = torch.empty_like(i["x"]), torch.zeros(400, dtype=torch.bfloat16, device="cuda"), torch.empty_like(i["x"])
+    _, stats = t.norm(i["x"], i["w"], save=True)
+    _, saved = t.cross_entropy(i["x"], i["head"], i["targets"], save=True)
+    head, table = torch.empty_like(i["head"]), torch.empty_like(i["table"])
+    for call, written in ((lambda: t.norm(i["x"], i["w"], out=out), [out]), (lambda: t.embedding(i["ids"], i["table"], out=out), [out]),
+                          (lambda: t.norm_backward(i["dy"], i["x"], i["w"], stats, dx=dx, dw=flat[:200]), [dx, flat]),
+                          (lambda: t.embedding_backward(i["dy"], i["ids"], table), [table]),
+                          (lambda: t.cross_entropy_backward(i["one"], i["x"], i["head"], i["targets"], saved, dx=dx, dw=head), [dx, head])):
+        every = [*i.values(), out, flat, dx, head, table, stats, saved]
+        was = [v._version for v in every]
+        call()
+        assert all((v._version > w) == any(v is x for x in written) for v, w in zip(every, was))
+
+
+def test_a_graph_that_is_not_recorded_is_told():
+    from paper_2504_05638_amd import train as t
+    i = _inputs()
+    calls = {"norm": (lambda a: t.norm(a["x"], a["w"], a["b"]), ["x", "w", "b"]), "embedding": (lambda a: t.embedding(a["ids"], a["table"], residual=a["x"]), ["table", "x"]),
+             "cross_entropy": (lambda a: t.cross_entropy(a["x"], a["head"], a["targets"]), ["x", "head"]),
+             "distill": (lambda a: t.distill(a["x"], a["head"], a["terms"], a["logits"]), ["x", "head", "logits"])}
+    for name, (call, which) in calls.items():
+        for w in which:
+            a = {k: v.detach() for k, v in i.items()}
+            a[w] = a[w].clone().requires_grad_()
+            with pytest.warns(UserWarning, match=name + " records no autograd"):
+                call(a)
+            with warnings.catch_warnings():
+                warnings.simplefilter("error")
+                with torch.no_grad():
+                    call(a)
+
+
+def _refused(call, match=None):
+    with pytest.raises((ValueError, RuntimeError), match=match):
+        call()
+
+
+def test_refusals():
+    from paper_2504_05638_amd import train as t
+    i = _inputs()
+    x, w, head, table, ids, targets, dy = (i[k] for k in ("x", "w", "head", "table", "ids", "targets", "dy"))
+    _, stats = t.norm(x, save=True)
+    _refused(lambda: t.norm(x.cpu()), "CUDA")
+    _refused(lambda: t.norm(x.half()), "float32")
+    _refused(lambda: t.norm(x, w.float()), "w")
+    _refused(lambda: t.norm(x, w[:-1]), "w")
+    _refused(lambda: t.norm(x, kind="batch"), "kind")
+    _refused(lambda: t.norm(x, b=w, kind="rms"))
+    _refused(lambda: t.norm(x, eps=-1.0))
+    _refused(lambda: t.norm(x.t()), "neighbours")
+    _refused(lambda: t.norm(x, out=torch.empty(1300, 201, device="cuda", dtype=x.dtype)), "out")
+    _refused(lambda: t.norm(torch.empty(2, 16385, device="cuda")))
+    _refused(lambda: t.norm_backward(dy, x, w, stats[:-1]), "stats")
+    _refused(lambda: t.norm_backward(dy, x, w, stats, residual=x, need_dx=False), "need_dx")
+    _refused(lambda: t.norm_backward(dy, x, w, stats, kind="rms", db=w))
+    _refused(lambda: t.norm_backward(dy, x, w, stats, dw=dy[0], dx=dy[:, :]))      # dw lies in dx
+    _refused(lambda: t.embedding(ids.float(), table), "ids")
+    _refused(lambda: t.embedding(ids[::2], table), "ids")
+    _refused(lambda: t.embedding(ids.cpu(), table), "ids")
+    _refused(lambda: t.embedding(ids, table[0]), "table")
+    _refused(lambda: t.embedding(ids, table, scale=float("inf")))
+    _refused(lambda: t.embedding(ids[:900], table, out=table))
+    _refused(lambda: t.embedding_backward(dy[:-1], ids, table), "dy")
+    _refused(lambda: t.embedding_backward(table, torch.arange(900, device="cuda"), table))
+    _refused(lambda: t.cross_entropy(x, head.t(), targets))
+    _refused(lambda: t.cross_entropy(x, head.float(), targets), "w")
+    _refused(lambda: t.cross_entropy(x, head, targets[:-1]), "targets")
+    _refused(lambda: t.cross_entropy(x[:, :0], head[:, :0], targets))
+    _refused(lambda: t.distill(x, head, i["terms"], i["logits"].bfloat16()), "logits")
+    _refused(lambda: t.distill(x, head, i["terms"], i["logits"][:, :-1]), "logits")
+    _refused(lambda: t.distill(x, head, i["terms"], None), "logits")
+    _refused(lambda: t.distill(x, head, i["terms"], i["logits"], temperature=0.0), "temperature")
+    _refused(lambda: t.distill(x, head, i["terms"][:, :0], i["logits"][:, :0]))
+    _, saved = t.cross_entropy(x, head, targets, save=True)
+    _refused(lambda: t.cross_entropy_backward(torch.ones(5, device="cuda"), x, head, targets, saved), "dloss")
+    _refused(lambda: t.cross_entropy_backward(i["one"], x, head, targets, saved[:, :1]), "saved")
+    _refused(lambda: t.cross_entropy_backward(i["one"], x, head, targets, saved, dw=head))
+    _refused(lambda: t.cross_entropy_backward(i["one"], x, head, targets, saved, dx=x))
+    _refused(lambda: t.cross_entropy_backward(i["one"], x, head, targets, saved, dx=x, need_dx=False), "need_dx")
+
+
+def test_an_expanded_gradient_is_one_number():
+    from paper_2504_05638_amd import train as t
+    i = _inputs(torch.float32)
+    _, saved = t.cross_entropy(i["x"], i["head"], i["targets"], save=True)
+    each = torch.full((1300,), 0.25, device="cuda")
+    want = t.cross_entropy_backward(each, i["x"], i["head"], i["targets"], saved)
+    for d in (torch.tensor(0.25, device="cuda"), torch.tensor([0.25], device="cuda"), torch.tensor(0.25, device="cuda").expand(1300)):
+        assert torch.equal(t.cross_entropy_backward(d, i["x"], i["head"], i["targets"], saved), want)

@@ -8,6 +8,8 @@
 // others, kMerge of them at a time.  Pieces of sorted tokens are summed side by side; a run of one id that goes on into the next piece
 // leaves a partial sum there, and these are joined in order.  No atomics on sums, nothing to clear.
 //
+// Batches of up to kDirect tokens are not sorted: the first token of an id finds the others, and all is one launch.
+//
 // Bound by bytes: the rows looked up, or dy and the table's gradient, most of which is zeros; these are written while the tokens are
 // sorted.
 #include <math.h>
@@ -32,6 +34,10 @@ constexpr uint32_t kRankThreads = 512, kRankSlices = kRankThreads / 64;
 constexpr uint32_t kShortPiece = 8, kLongPiece = 32, kShort = 8192;
 constexpr uint32_t kSumThreads = 256, kRunSlices = kSumThreads / 64;
 constexpr uint32_t kZeroRows = 64;     // most table rows that a workgroup looks after for want of tokens
+
+// Tokens up to which there is one launch.  (us, with it / with the sort: 128 tokens into 1000 by 512 7 / 12; 512 there 18 / 13, and 512 of one id into
+// 32000 by 4096 116 / 62, for which a workgroup adds them all.)
+constexpr uint32_t kDirect = 128;
 
 // An id, or `vocab` for what is no token.
 __device__ inline uint32_t id_at(const void *ids, uint32_t wide, uint64_t t, uint32_t vocab)
@@ -108,9 +114,36 @@ struct Tokens {
     uint32_t zero_rows;  // table rows of a workgroup
 };
 
+// Looks for tokens of some rows of the table, and writes zeros where there are none.  `found`: local memory for kZeroRows words.
+template <typename T, uint32_t THREADS>
+__device__ inline void zero_rows(const Tokens &a, uint32_t which, uint32_t *found)
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    const uint32_t first = which * a.zero_rows;
+    if (threadIdx.x < a.zero_rows) found[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (uint32_t t = threadIdx.x; t < a.rows; t += THREADS) {
+        const uint32_t v = id_at(a.ids, a.wide, t, a.vocab) - first;
+        if (v < a.zero_rows) found[v] = 1;
+    }
+    __syncthreads();
+    const float zeros[V] = {};
+    for (uint32_t r = 0; r < a.zero_rows && first + r < a.vocab; ++r) {
+        if (found[r]) continue;
+        T *to = static_cast<T *>(a.dtable) + (first + r) * a.ldt;
+        for (uint32_t c = threadIdx.x * V; c < a.width; c += THREADS * V) {
+            if (c + V <= a.width) {
+                store_n<T, V>(to + c, zeros);
+            } else {
+                for (uint32_t j = c; j < a.width; ++j) to[j] = T(0);
+            }
+        }
+    }
+}
+
 // The first workgroups rank 64 tokens each among their chunk's: a lane has a token, a wave an eighth of the chunk.  Ids that are as
-// large count if they stand before it.  The others look for tokens of some rows of the table, and write zeros where there
-// are none: bytes that keep the memory busy meanwhile (16384 tokens into 32000 by 4096 in bfloat16: 222 MB beside
+// large count if they stand before it.  The others write zeros: bytes that keep the memory busy meanwhile (16384 tokens into 32000 by 4096 in bfloat16: 222 MB beside
 // ranking take 40 us, 5.5 TB/s; ranking alone 13).
 template <typename T>
 __global__ __launch_bounds__(kRankThreads) void rank_kernel(Tokens a)
@@ -118,32 +151,7 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(Tokens a)
     __shared__ __attribute__((aligned(16))) uint32_t keys[kChunk];
     __shared__ uint32_t counts[kRankSlices][64];
     const uint32_t group = blockIdx.x;
-    if (group >= a.groups) {
-        constexpr uint32_t V = 16 / sizeof(T);
-        const uint32_t first = (group - a.groups) * a.zero_rows;
-        uint32_t *found = keys;
-        if (threadIdx.x < a.zero_rows) found[threadIdx.x] = 0;
-        __syncthreads();
-#pragma unroll 4
-        for (uint32_t t = threadIdx.x; t < a.rows; t += kRankThreads) {
-            const uint32_t v = id_at(a.ids, a.wide, t, a.vocab) - first;
-            if (v < a.zero_rows) found[v] = 1;
-        }
-        __syncthreads();
-        const float zeros[V] = {};
-        for (uint32_t r = 0; r < a.zero_rows && first + r < a.vocab; ++r) {
-            if (found[r]) continue;
-            T *to = static_cast<T *>(a.dtable) + (first + r) * a.ldt;
-            for (uint32_t c = threadIdx.x * V; c < a.width; c += kRankThreads * V) {
-                if (c + V <= a.width) {
-                    store_n<T, V>(to + c, zeros);
-                } else {
-                    for (uint32_t j = c; j < a.width; ++j) to[j] = T(0);
-                }
-            }
-        }
-        return;
-    }
+    if (group >= a.groups) return zero_rows<T, kRankThreads>(a, group - a.groups, keys);
     const uint32_t chunk = group * 64 / kChunk * kChunk, have = min(kChunk, a.rows - chunk), whole = (have + 63) / 64 * 64;
 #pragma unroll 4
     for (uint32_t i = threadIdx.x; i < whole; i += kRankThreads) keys[i] = i < have ? id_at(a.ids, a.wide, chunk + i, a.vocab) : 0xFFFFFFFFu;
@@ -239,6 +247,52 @@ __device__ inline void finish_row(const Sums &a, uint32_t key, uint32_t c, uint3
         for (uint32_t j = 0; j < V; ++j)
             if (j < have) to[j] = narrow<T>(a.accumulate ? a.scale * sum[j] + widen(to[j]) : a.scale * sum[j]);
     }
+}
+
+// Up to kDirect tokens: a workgroup to a token and 256 * V columns, if it is the first of its id, and the zeros beside them.
+template <typename T>
+__global__ __launch_bounds__(kSumThreads) void direct_kernel(Tokens a, Sums b)
+{
+    constexpr uint32_t V = 16 / sizeof(T), kAhead = 16;
+    __shared__ uint32_t keys[kDirect], list[kDirect + kAhead];
+    if (blockIdx.x >= a.groups) return zero_rows<T, kSumThreads>(a, blockIdx.x - a.groups, keys);
+    const uint32_t t = blockIdx.x / b.spans, c = (blockIdx.x % b.spans * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
+    for (uint32_t i = threadIdx.x; i < a.rows; i += kSumThreads) keys[i] = id_at(a.ids, a.wide, i, a.vocab);
+    __syncthreads();
+    const uint32_t key = keys[t];
+    if (key == a.vocab) return;
+    bool earlier = false;
+    for (uint32_t i = threadIdx.x; i < t; i += kSumThreads) earlier |= keys[i] == key;
+    if (__syncthreads_or(earlier)) return;
+    // each wave finds its tokens, 64 at a time, and one of them writes the list
+    uint32_t n = 0;
+    for (uint32_t i = t / 64 * 64; i < a.rows; i += 64) {
+        const uint32_t at = i + (threadIdx.x & 63);
+        const bool mine = at < a.rows && keys[at] == key;
+        const uint64_t mask = __ballot(mine);
+        if (threadIdx.x < 64 && mine) list[n + __popcll(mask & ((1ull << threadIdx.x) - 1))] = at;
+        n += uint32_t(__popcll(mask));
+    }
+    __syncthreads();
+    float sum[V] = {};
+    for (uint32_t k = 0; k < n; k += kAhead) {
+        Lane<T, V> x[kAhead];
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) {
+            const T *from = static_cast<const T *>(b.dy) + list[min(k + i, n - 1)] * b.lddy + c;
+            if (have == V) {
+                x[i].load(from);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j) x[i].v[j] = j < have ? from[j] : T(0);
+            }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) sum[j] += k + i < n ? x[i][j] : 0.0f;
+    }
+    if (have) finish_row<T, false>(b, key, c, have, sum);
 }
 
 // A workgroup sums a piece of sorted tokens, 256 * V columns of them.  Bound by the bytes of dy, of the rows that are finished and of the partial sums: 16384
@@ -417,12 +471,14 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
 {
     const uint64_t M = l->rows;
     if (!l->vocab || !l->width || (!M && l->accumulate)) return TAGC_OK;
+    const bool direct = M <= kDirect;
     const uint32_t piece = M <= kShort ? kShortPiece : kLongPiece, pieces = uint32_t((M + piece - 1) / piece);
     constexpr uint32_t V = 16 / sizeof(T);
-    Sorted sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)}, other = sorted;
+    Sorted sorted{}, other{};
+    if (!direct) sorted = Sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)};
     if (M > kChunk) other = Sorted{w.take<uint32_t>(M), w.take<uint32_t>(M)};
     Sums a{};
-    a.partial = w.take<float>(uint64_t(pieces) * 2 * l->width);
+    a.partial = w.take<float>(direct ? 0 : uint64_t(pieces) * 2 * l->width);
     if (!enqueue) return TAGC_OK;
     a.dy = l->dy;
     a.dtable = l->dtable;
@@ -440,6 +496,12 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
         Tokens t{l->ids, sorted, l->dtable, l->ldt, a.rows, a.width, a.vocab, l->id_type, uint32_t((M + 63) / 64), 1};
         while (t.zero_rows < kZeroRows && l->vocab / t.zero_rows > 2 * uint64_t(device_cu_count())) t.zero_rows *= 2;
         const uint32_t zeros = l->accumulate ? 0 : (a.vocab + t.zero_rows - 1) / t.zero_rows;
+        if (direct) {
+            t.groups = a.rows * a.spans;
+            ProfileScope prof("embed_sum", s);
+            direct_kernel<T><<<t.groups + zeros, kSumThreads, 0, s>>>(t, a);
+            return hip_ok(hipGetLastError());
+        }
         ProfileScope prof("embed_sort", s);
         rank_kernel<T><<<t.groups + zeros, kRankThreads, 0, s>>>(t);
         for (uint64_t run = kChunk; run < M; run *= kMerge) {

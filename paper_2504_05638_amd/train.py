@@ -88,7 +88,7 @@ def _rows_of(t, name, rows, cols, dtype, device):
 def _vector(t, name, n, dtype, device):
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+    if t.dtype != dtype or t.device != device or t.shape != (n,) or not (t.is_contiguous() or n <= 1):
         raise ValueError("%s: a contiguous vector of %d, %s on %s, is wanted" % (name, n, dtype, device))
     return t.data_ptr() or None
 
@@ -243,6 +243,19 @@ def _floats(t, name, shape, device):
     return t.data_ptr() or None
 
 
+def _matrix(t, name, rows, cols, dtype, device):
+    """_rows_of of a tensor [..., cols]; of one that lies one row behind the other nothing else is asked."""
+    if t is None:
+        return None, 0
+    if t.is_contiguous() and t.dtype == dtype and t.device == device and t.numel() == rows * cols and t.dim() and t.shape[-1] == cols:
+        return t.data_ptr() or None, cols
+    return _rows_of(_flat(t, rows, cols), name, rows, cols, dtype, device)
+
+
+def _like(x):
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
 def norm(x, w=None, b=None, kind="layer", eps=1e-5, save=False, out=None, stream=None):
     """(y, stats): y = (x - mean) / sqrt(variance + eps) * w + b over the last dimension, or, kind "rms", without mean
     and b.  `save`: stats, float32 [rows, 2], for norm_backward (else None).  `out` may be given, and be x.  No autograd graph is
@@ -253,15 +266,16 @@ def norm(x, w=None, b=None, kind="layer", eps=1e-5, save=False, out=None, stream
     _no_graph("norm", x, w, b)
     shape, dtype, device = x.shape, x.dtype, x.device
     n = shape[-1]
-    m = math.prod(shape[:-1])
-    xp, ldx = _rows_of(_flat(x, m, n), "x", m, n, dtype, device)
+    m = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
+    xp, ldx = _matrix(x, "x", m, n, dtype, device)
     wp, bp = _vector(w, "w", n, dtype, device), _vector(b, "b", n, dtype, device)
-    _need(out is None or out.shape == shape, "out: x's shape is wanted")
-    yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
-    given, stats, sp, user = out, None, None, torch.cuda.current_stream(device) if stream is not None else None
+    given, stats, sp, user = out, None, None, None if stream is None else torch.cuda.current_stream(device)
+    if out is not None:
+        _need(out.shape == shape, "out: x's shape is wanted")
+        yp, ldy = _matrix(out, "out", m, n, dtype, device)
     with _at(device, stream):
         if out is None:
-            out = x.new_empty(shape)
+            out = _like(x)
             yp, ldy = out.data_ptr() or None, n
         if save:
             stats = torch.empty((m, 2), dtype=torch.float32, device=device)
@@ -285,16 +299,16 @@ def norm_backward(dy, x, w, stats, kind="layer", residual=None, dx=None, dw=None
     shape, dtype, device = x.shape, x.dtype, x.device
     n = shape[-1]
     m = math.prod(shape[:-1])
-    xp, ldx = _rows_of(_flat(x, m, n), "x", m, n, dtype, device)
-    yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
-    rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
-    dp, ldd = _rows_of(_flat(dx, m, n), "dx", m, n, dtype, device)
+    xp, ldx = _matrix(x, "x", m, n, dtype, device)
+    yp, ldy = _matrix(dy, "dy", m, n, dtype, device)
+    rp, ldr = _matrix(residual, "residual", m, n, dtype, device)
+    dp, ldd = _matrix(dx, "dx", m, n, dtype, device)
     wp, gp, bp = (_vector(t, name, n, dtype, device) for t, name in ((w, "w"), (dw, "dw"), (db, "db")))
     sp = _floats(stats, "stats", (m, 2), device)
-    given, user = (dx, dw, db), torch.cuda.current_stream(device) if stream is not None else None
+    given, user = (dx, dw, db), None if stream is None else torch.cuda.current_stream(device)
     with _at(device, stream):
         if need_dx and dx is None:
-            dx = x.new_empty(shape)
+            dx = _like(x)
             dp, ldd = dx.data_ptr() or None, n
         a = B.tagc_norm_grad(m, n, _TYPES[dtype], _KINDS[kind], xp, ldx, wp, sp, yp, ldy, rp, ldr, dp, ldd, gp, bp, 1 if accumulate else 0, 0)
         ws, at = _work(B.tagc_norm_backward_workspace(a), x)
@@ -316,12 +330,12 @@ def embedding(ids, table, scale=1.0, residual=None, out=None, stream=None):
     dtype, device = table.dtype, table.device
     m, shape = ids.numel(), (*ids.shape, n)
     ip, wide = _all_ids(ids, "ids", ids.shape, device)
-    tp, ldt = _rows_of(table, "table", v, n, dtype, device)
+    tp, ldt = _matrix(table, "table", v, n, dtype, device)
     for t, name in ((residual, "residual"), (out, "out")):
         _need(t is None or t.shape == shape, "%s: the shape %s is wanted" % (name, shape))
-    rp, ldr = _rows_of(_flat(residual, m, n), "residual", m, n, dtype, device)
-    yp, ldy = _rows_of(_flat(out, m, n), "out", m, n, dtype, device)
-    given, user = out, torch.cuda.current_stream(device) if stream is not None else None
+    rp, ldr = _matrix(residual, "residual", m, n, dtype, device)
+    yp, ldy = _matrix(out, "out", m, n, dtype, device)
+    given, user = out, None if stream is None else torch.cuda.current_stream(device)
     with _at(device, stream):
         if out is None:
             out = table.new_empty(shape)
@@ -345,8 +359,8 @@ def embedding_backward(dy, ids, dtable, scale=1.0, accumulate=False, stream=None
     m = ids.numel()
     ip, wide = _all_ids(ids, "ids", ids.shape, device)
     _need(dy.shape == (*ids.shape, n), "dy: the shape %s is wanted" % ((*ids.shape, n),))
-    yp, ldy = _rows_of(_flat(dy, m, n), "dy", m, n, dtype, device)
-    tp, ldt = _rows_of(dtable, "dtable", v, n, dtype, device)
+    yp, ldy = _matrix(dy, "dy", m, n, dtype, device)
+    tp, ldt = _matrix(dtable, "dtable", v, n, dtype, device)
     with _at(device, stream):
         a = B.tagc_embedding_grad(m, n, v, _TYPES[dtype], wide, scale, ip, yp, ldy, tp, ldt, 1 if accumulate else 0, 0)
         ws, at = _work(B.tagc_embedding_backward_workspace(a), dtable)
@@ -372,14 +386,14 @@ def _loss_operands(x, w, ids, logits, temperature, stream):
         terms = ids.shape[-1]
         ip, wide = _all_ids(ids, "ids", ids.shape, device)
         ap = _floats(logits, "logits", ids.shape, device)
-    xp, ldx = _rows_of(_flat(x, m, k) if x.dim() != 1 else x.view(1, k), "x", m, k, dtype, device)
-    wp, ldw = _rows_of(w, "w", v, k, dtype, device)
+    xp, ldx = _matrix(x, "x", m, k, dtype, device)
+    wp, ldw = _matrix(w, "w", v, k, dtype, device)
     return (m, k, v, terms), wide, (xp, ldx, wp, ldw, ip, ap), shape
 
 
 def _loss(x, w, ids, logits, temperature, save, stream):
     size, wide, operands, shape = _loss_operands(x, w, ids, logits, temperature, stream)
-    device, saved, sp, user = x.device, None, None, torch.cuda.current_stream(x.device) if stream is not None else None
+    device, saved, sp, user = x.device, None, None, None if stream is None else torch.cuda.current_stream(x.device)
     with _at(device, stream):
         loss = torch.empty(shape, dtype=torch.float32, device=device)
         if save:
@@ -403,12 +417,12 @@ def _loss_backward(dloss, x, w, ids, logits, saved, temperature, dx, dw, accumul
     one = m > 0 and all(step == 0 or n == 1 for step, n in zip(dloss.stride(), dloss.shape))     # (also one that is expanded)
     gp = _floats(dloss.as_strided((1,), (1,)) if one else dloss, "dloss", (1,) if one else shape, device)
     _need(dx is None or dx.shape == x.shape, "dx: x's shape is wanted")
-    dp, ldd = _rows_of((_flat(dx, m, k) if x.dim() != 1 else dx.view(1, k)) if dx is not None else None, "dx", m, k, dtype, device)
-    wp, ldw = _rows_of(dw, "dw", v, k, dtype, device)
-    given, user = (dx, dw), torch.cuda.current_stream(device) if stream is not None else None
+    dp, ldd = _matrix(dx, "dx", m, k, dtype, device)
+    wp, ldw = _matrix(dw, "dw", v, k, dtype, device)
+    given, user = (dx, dw), None if stream is None else torch.cuda.current_stream(device)
     with _at(device, stream):
         if need_dx and dx is None:
-            dx = x.new_empty(x.shape)
+            dx = _like(x)
             dp, ldd = dx.data_ptr() or None, k
         a = B.tagc_loss_grad(*size, _TYPES[dtype], wide, 1 if accumulate else 0, temperature, *operands, sp, gp, 0 if one else 1, 0, dp, ldd, wp, ldw)
         ws, at = _work(B.tagc_loss_backward_workspace(a), x)

@@ -1,5 +1,5 @@
-"""Token embeddings against float64: lookups, and the table's gradient with its sorting, at sizes around a chunk of sorted tokens (4096)
-and a piece of summed ones (16).
+"""Token embeddings against float64: lookups, and the table's gradient with its sorting, at sizes around what is not sorted
+(128 tokens), a chunk of what is (4096) and a piece of summed tokens (8 or 32).
 
 Bounds, with E = 2^-24: a lookup is one multiplication and one addition, a gradient's row of n tokens n additions, and half a step of
 the result's type."""
@@ -121,7 +121,7 @@ def _gradient(n, vocab, width, dtype, kind, add, seed, odd):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("kind", KINDS)
 def test_gradient(kind, dtype):
-    for i, (n, vocab, width) in enumerate([(1, 1, 1), (1, 40, 64), (15, 7, 33), (16, 100, 8), (17, 3, 130), (64, 64, 64), (65, 1000, 5), (333, 50, 777),
+    for i, (n, vocab, width) in enumerate([(1, 1, 1), (1, 40, 64), (15, 7, 33), (16, 100, 8), (17, 3, 130), (64, 64, 64), (65, 1000, 5), (333, 50, 777), (128, 40, 2049), (129, 40, 33),
                                            (1023, 5000, 256), (4095, 300, 40), (4096, 301, 64), (4097, 302, 72), (9000, 20000, 32), (13000, 9, 2050)]):
         print("[case] embedding gradient", kind, dtype, n, vocab, width, flush=True)
         _gradient(n, vocab, width, T[dtype], kind, i % 3 == 1, 3 * i, i % 2)

@@ -981,7 +981,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
         const uint64_t n = V - v < piece ? V - v : piece;
         const T *from = static_cast<const T *>(l->w) + v * l->ldw;
         Operand q{from, l->ldw, 0};
-        if (ops.lay) {
+        if (ops.lay && M) {  // (without rows there need be no w)
             launch_gather<T>(gather<T>(from, l->ldw, n, D, wq), s);
             q = wq;
         }

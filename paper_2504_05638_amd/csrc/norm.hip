@@ -399,16 +399,23 @@ int check(const tagc_norm_grad *n)
     return TAGC_OK;
 }
 
+// (a launch has fewer than 2^32 threads, and a row up to 1024 of them)
+constexpr uint64_t kLaunchRows = 1u << 21;
+
 template <typename T>
 int forward(const tagc_norm *n, hipStream_t s)
 {
-    if (!n->rows || !n->width) return TAGC_OK;
-    const Norm a{n->x, n->w, n->b, n->y, n->stats, n->ldx, n->ldy, uint32_t(n->rows), uint32_t(n->width), n->kind, float(n->eps)};
+    if (!n->width) return TAGC_OK;
     ProfileScope prof("norm", s);
-    by_width<T>(n->width, [&](auto lanes, auto steps) {
-        constexpr int L = decltype(lanes)::value, threads = kNormThreads<L>;
-        norm_kernel<T, L, decltype(steps)::value><<<uint32_t((n->rows + threads / L - 1) / (threads / L)), threads, 0, s>>>(a);
-    });
+    for (uint64_t first = 0; first < n->rows; first += kLaunchRows) {
+        const uint64_t rows = n->rows - first < kLaunchRows ? n->rows - first : kLaunchRows;
+        const Norm a{static_cast<const T *>(n->x) + first * n->ldx, n->w, n->b, static_cast<T *>(n->y) + first * n->ldy, n->stats ? n->stats + 2 * first : nullptr,
+                     n->ldx, n->ldy, uint32_t(rows), uint32_t(n->width), n->kind, float(n->eps)};
+        by_width<T>(n->width, [&](auto lanes, auto steps) {
+            constexpr int L = decltype(lanes)::value, threads = kNormThreads<L>;
+            norm_kernel<T, L, decltype(steps)::value><<<uint32_t((rows + threads / L - 1) / (threads / L)), threads, 0, s>>>(a);
+        });
+    }
     return hip_ok(hipGetLastError());
 }
 

@@ -213,6 +213,13 @@ def test_no_rows_and_shapes():
     assert float(dw.sum()) == dw.numel()
     cross_entropy_backward(torch.empty(0, device="cuda"), x, w, t, saved, dw=dw)
     assert not dw.any()
+    from paper_2504_05638_amd import binding as B
+    for dtype, width in ((torch.float32, 16), (torch.bfloat16, 15)):     # nothing but a result: zeros
+        dw = torch.ones((50, width), device="cuda", dtype=dtype)
+        a = B.tagc_loss_grad(rows=0, in_=width, vocab=50, terms=1, dtype=int(dtype == torch.bfloat16), temperature=1.0, dw=dw.data_ptr(), lddw=width)
+        ws = torch.empty(B.tagc_loss_backward_workspace(a), dtype=torch.uint8, device="cuda")
+        B.tagc_loss_backward(a, ws.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        assert not dw.any()
     x, t = _randn((6, 16), 2, torch.float32), torch.arange(6, device="cuda")
     want, _ = cross_entropy(x, w, t)
     got, _ = cross_entropy(x.view(2, 3, 16), w, t.view(2, 3))

@@ -137,6 +137,16 @@ def test_many_rows(kind, dtype):
         _backward((M, D), T[dtype], kind, True, True, True, 6, 1)
 
 
+def test_more_rows_than_a_launch_takes():
+    from paper_2504_05638_amd.train import norm
+    M = (1 << 21) + 3
+    x = torch.randn(M, 2, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    y, stats = norm(x, save=True)
+    for part in (slice(0, 9), slice((1 << 21) - 4, M)):
+        few, also = norm(x[part].contiguous(), save=True)
+        assert torch.equal(y[part], few) and torch.equal(stats[part], also)
+
+
 def test_rows_far_from_zero():
     """A mean a thousand times the spread: the variance is that of what is left, not a difference of sums."""
     from paper_2504_05638_amd.train import norm

@@ -290,20 +290,28 @@ struct Scores : Counted {
     {
         constexpr uint32_t kRow = RN * 16 + 4, kQuads = 8;  // quads of ids on their way
         const uint32_t first = base + n0, quads = 32u << (shift - 2);
+        // (rows that there are not have no ids)
+        const uint4 *from = reinterpret_cast<const uint4 *>(ids + (uint64_t(m0) << shift));
+        const auto quad = [&](uint32_t q) { return m0 + (q >> (shift - 2)) < m ? from[q] : make_uint4(kNone, kNone, kNone, kNone); };
+        const auto in = [&](uint32_t id) { return id - first < RN * 16; };
+        // (up to four terms a row: three of four waves have none)
+        bool search = shift > 2;
+        if (!search) {
+            for (uint32_t q = lane; q < RM * 16; q += 64) {
+                const uint4 id = quad(q);
+                search = search || in(id.x) || in(id.y) || in(id.z) || in(id.w);
+            }
+            search = __any(search);
+        }
 #pragma unroll 1
-        for (int i = 0; i < RM; i += 2) {
-            // (rows that there are not have no ids)
-            const uint32_t r0 = m0 + i * 16;
-            const uint4 *from = reinterpret_cast<const uint4 *>(ids + (uint64_t(r0) << shift));
-            const auto quad = [&](uint32_t q) { return r0 + (q >> (shift - 2)) < m ? from[q] : make_uint4(kNone, kNone, kNone, kNone); };
-            const auto in = [&](uint32_t id) { return id - first < RN * 16; };
+        for (int i = search ? 0 : RM; i < RM; i += 2) {
             bool written = false;
             for (uint32_t at_quad = 0; at_quad < quads; at_quad += 64 * kQuads) {  // (all lanes, which write the strip together)
                 const uint32_t q0 = at_quad + lane;
                 uint4 id[kQuads];
                 bool any = false;
 #pragma unroll
-                for (uint32_t b = 0; b < kQuads; ++b) id[b] = q0 + 64 * b < quads ? quad(q0 + 64 * b) : make_uint4(kNone, kNone, kNone, kNone);
+                for (uint32_t b = 0; b < kQuads; ++b) id[b] = q0 + 64 * b < quads ? quad(q0 + 64 * b + i / 2 * quads) : make_uint4(kNone, kNone, kNone, kNone);
 #pragma unroll
                 for (uint32_t b = 0; b < kQuads; ++b) any = any || in(id[b].x) || in(id[b].y) || in(id[b].z) || in(id[b].w);
                 if (!__any(any)) continue;
@@ -322,7 +330,7 @@ struct Scores : Counted {
 #pragma unroll
                 for (uint32_t b = 0; b < kQuads; ++b) {
                     const uint32_t q = q0 + 64 * b, r = q >> (shift - 2), k = (q << 2) & ((1u << shift) - 1);
-                    float *to = scores + uint64_t(r0 + r) * terms + k;
+                    float *to = scores + uint64_t(m0 + i * 16 + r) * terms + k;
                     if (in(id[b].x)) to[0] = strip[r * kRow + id[b].x - first] * over;
                     if (in(id[b].y)) to[1] = strip[r * kRow + id[b].y - first] * over;
                     if (in(id[b].z)) to[2] = strip[r * kRow + id[b].z - first] * over;
@@ -333,28 +341,36 @@ struct Scores : Counted {
         }
         float2 *to = stats + uint64_t(n0 / (RN * 16)) * rows;
         const uint32_t c0 = n0 + 4 * (lane >> 4);
+        const bool whole = n0 + RN * 16 <= n;
 #pragma unroll
         for (int i = 0; i < RM; ++i) {
             const uint32_t row = m0 + i * 16 + (lane & 15);
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < RN; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c0 + 16 * j + e < n) top = fmaxf(top, acc[i][j][e] * over2);
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float against = top == -INFINITY ? 0.0f : top;  // (no column, or nothing but -infinity and NaN)
-            float sum = 0;
-#pragma unroll
-            for (int j = 0; j < RN; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c0 + 16 * j + e < n) sum += __builtin_amdgcn_exp2f(acc[i][j][e] * over2 - against);
-            sum += __shfl_xor(sum, 16, 64);
-            sum += __shfl_xor(sum, 32, 64);
-            if (lane < 16 && row < m) to[row] = make_float2(top, sum);
+            const float2 of = whole ? summed<true>(acc[i], c0) : summed<false>(acc[i], c0);
+            if (lane < 16 && row < m) to[row] = of;
         }
+    }
+    // of a row's scores in columns c0 + 16 j + (0 .. 3) of four lanes; WHOLE: all these columns are there
+    template <bool WHOLE, int RN>
+    __device__ inline float2 summed(const f32x4 (&row)[RN], uint32_t c0) const
+    {
+        float top = -INFINITY, sum = 0;
+#pragma unroll
+        for (int j = 0; j < RN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (WHOLE || c0 + 16 * j + e < n) top = fmaxf(top, row[j][e]);
+        top *= over2;
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float against = top == -INFINITY ? 0.0f : top;  // (no column, or nothing but -infinity and NaN)
+#pragma unroll
+        for (int j = 0; j < RN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (WHOLE || c0 + 16 * j + e < n) sum += __builtin_amdgcn_exp2f(row[j][e] * over2 - against);
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        return make_float2(top, sum);
     }
 };
 

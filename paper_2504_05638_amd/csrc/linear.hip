@@ -255,7 +255,7 @@ __device__ inline void finish(const Result &r, uint32_t m, uint32_t n, uint32_t 
 // A product whose sums go through finish(), or as parts of them to be joined.
 template <typename T>
 struct Written : Product {
-    static constexpr bool kCounted = false;
+    static constexpr bool kCounted = false, kPartByPart = true;
     float *partial;                 // [splits][m][n]
     Result result;
     template <int RM, int RN>

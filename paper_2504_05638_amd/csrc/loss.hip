@@ -429,7 +429,7 @@ __device__ inline void put_f32(float *to, uint32_t have, const float (&z)[8])
 // few tiles' scores (Product).
 template <typename Base>
 struct Planes : Base {
-    static constexpr bool kCounted = std::is_same<Base, Counted>::value;
+    static constexpr bool kCounted = std::is_same<Base, Counted>::value, kPartByPart = false;
     float *planes;  // [parts][rows][n]
     uint32_t rows, add;
     template <int RM, int RN>

@@ -143,8 +143,8 @@ __device__ inline void zero_rows(const Tokens &a, uint32_t which, uint32_t *foun
 }
 
 // The first workgroups rank 64 tokens each among their chunk's: a lane has a token, a wave an eighth of the chunk.  Ids that are as
-// large count if they stand before it.  The others write zeros: bytes that keep the memory busy meanwhile (16384 tokens into 32000 by 4096 in bfloat16: 222 MB beside
-// ranking take 40 us, 5.5 TB/s; ranking alone 13).
+// large count if they stand before it.  The others write zeros: bytes that keep the memory busy meanwhile (16384 tokens into 32000 by 4096 in bfloat16: 218 MB beside
+// ranking take 40 to 51 us, by what the caches have to write back; ranking alone 13).
 template <typename T>
 __global__ __launch_bounds__(kRankThreads) void rank_kernel(Tokens a)
 {
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kSumThreads) void direct_kernel(Tokens a, Sums b)
 }
 
 // A workgroup sums a piece of sorted tokens, 256 * V columns of them.  Bound by the bytes of dy, of the rows that are finished and of the partial sums: 16384
-// tokens of 4096 in bfloat16, added to what is there, 55 us, 4.5 TB/s.
+// tokens of 4096 in bfloat16 40 us, 4.9 TB/s.
 template <typename T, uint32_t PIECE, bool WHOLE>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
 {
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
                 if (j < have) to[j] = sum[j];
         }
     };
-    // rows come four at a time, the next ones while these are added (two, eight: 1 % slower, the same; all at once, which leaves fewer workgroups
+    // rows come four at a time, past the caches' order, which the table's rows are left to (61 -> 40 us), the next ones while these are added (two, eight: 1 % slower, the same; all at once, which leaves fewer workgroups
     // room, half as long again)
     constexpr uint32_t kAhead = 4;
     Lane<T, V> x[2][kAhead];
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
         for (uint32_t k = 0; k < kAhead; ++k) {
             const T *from = static_cast<const T *>(a.dy) + rows[first + k] * a.lddy + c;
             if (WHOLE || have == V) {
-                if (have) to[k].load(from);
+                if (have) to[k].v = __builtin_nontemporal_load(reinterpret_cast<const typename Lane<T, V>::vec *>(from));
             } else {
 #pragma unroll
                 for (uint32_t j = 0; j < V; ++j) to[k].v[j] = j < have ? from[j] : T(0);

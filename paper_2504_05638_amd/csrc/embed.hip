@@ -3,9 +3,8 @@
 //   y[t] = scale * table[ids[t]] + residual[t]            dtable[v] (+)= scale * sum over t with ids[t] = v of dy[t]
 //
 // The gradient's sums have an order of their own: tokens are sorted by id, and by place where ids are equal, so that
-// a row's terms lie one behind the other.  Sorting is counting: a token's place among kChunk tokens is the number of those
-// before it, which all compute units count at once; chunks are then merged by searching each one for every token of the
-// others, kMerge of them at a time.  Pieces of sorted tokens are summed side by side; a run of one id that goes on into the next piece
+// a row's terms lie one behind the other.  A workgroup sorts kChunk tokens, four bits of their ids at a time; sorted chunks are merged by searching
+// each one for every token of the others, kMerge of them at a time.  Pieces of sorted tokens are summed side by side; a run of one id that goes on into the next piece
 // leaves a partial sum there, and these are joined in order.  No atomics on sums, nothing to clear.
 //
 // Batches of up to kDirect tokens are not sorted: the first token of an id finds the others, and all is one launch.
@@ -25,15 +24,17 @@ namespace tagc {
 
 namespace {
 
-// Tokens sorted together: ranking costs each of them a pass over the chunk, merging a launch.  (us of sorting 16384: 13 + 9, as one chunk 41.)
-constexpr uint32_t kChunk = 4096;
+// Tokens sorted together, in local memory.
+constexpr uint32_t kChunk = 4096, kSortThreads = 1024, kSlots = kChunk / kSortThreads, kSortWaves = kSortThreads / 64;
 constexpr uint32_t kMerge = 16;        // sorted lists merged at once
-constexpr uint32_t kRankThreads = 512, kRankSlices = kRankThreads / 64;
 // Sorted tokens summed by a workgroup: many leave fewer partial sums behind, few make more workgroups of a short batch.  (us, eight / 16 /
 // 32: 16384 tokens into 32000 by 4096 in bfloat16 133 / 126 / 123, 1023 into 50257 by 768 in float32 38 / 41 / 45.)
 constexpr uint32_t kShortPiece = 8, kLongPiece = 32, kShort = 8192;
 constexpr uint32_t kSumThreads = 256, kRunSlices = kSumThreads / 64;
 constexpr uint32_t kZeroRows = 64;     // most table rows that a workgroup looks after for want of tokens
+// Tokens up to which it looks at all of them, while they are sorted; at more it searches the sorted ones, while these are summed.  (us, 65536 tokens into 50257
+// by 768 in bfloat16: 139 / 90.)
+constexpr uint32_t kZerosFirst = 16384;
 
 // Tokens up to which there is one launch.  (us, with it / with the sort: 128 tokens into 1000 by 512 7 / 12; 512 there 18 / 13, and 512 of one id into
 // 32000 by 4096 116 / 62, for which a workgroup adds them all.)
@@ -112,13 +113,33 @@ struct Tokens {
     uint64_t ldt;
     uint32_t rows, width, vocab, wide, groups;
     uint32_t zero_rows;  // table rows of a workgroup
+    uint32_t bits;       // of the largest id, which is `vocab`
 };
 
-// Looks for tokens of some rows of the table, and writes zeros where there are none.  `found`: local memory for kZeroRows words.
+// Zeros in those of a workgroup's rows, from `first` on, that no token has been found for.
+template <typename T, uint32_t THREADS>
+__device__ inline void write_zeros(T *dtable, uint64_t ld, uint32_t width, uint32_t first, uint32_t rows, const uint32_t *found)
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    const uint32_t across = (width + V - 1) / V;
+    const float zeros[V] = {};
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < rows * across; i += THREADS) {
+        const uint32_t r = i / across, c = (i - r * across) * V;
+        if (found[r]) continue;
+        T *to = dtable + (first + r) * ld + c;
+        if (c + V <= width) {
+            store_n<T, V>(to, zeros);
+        } else {
+            for (uint32_t j = 0; c + j < width; ++j) to[j] = T(0);
+        }
+    }
+}
+
+// The same for some rows of the table, whose tokens are looked for among all.  `found`: local memory for kZeroRows words.
 template <typename T, uint32_t THREADS>
 __device__ inline void zero_rows(const Tokens &a, uint32_t which, uint32_t *found)
 {
-    constexpr uint32_t V = 16 / sizeof(T);
     const uint32_t first = which * a.zero_rows;
     if (threadIdx.x < a.zero_rows) found[threadIdx.x] = 0;
     __syncthreads();
@@ -128,64 +149,73 @@ __device__ inline void zero_rows(const Tokens &a, uint32_t which, uint32_t *foun
         if (v < a.zero_rows) found[v] = 1;
     }
     __syncthreads();
-    const float zeros[V] = {};
-    for (uint32_t r = 0; r < a.zero_rows && first + r < a.vocab; ++r) {
-        if (found[r]) continue;
-        T *to = static_cast<T *>(a.dtable) + (first + r) * a.ldt;
-        for (uint32_t c = threadIdx.x * V; c < a.width; c += THREADS * V) {
-            if (c + V <= a.width) {
-                store_n<T, V>(to + c, zeros);
-            } else {
-                for (uint32_t j = c; j < a.width; ++j) to[j] = T(0);
-            }
-        }
-    }
+    write_zeros<T, THREADS>(static_cast<T *>(a.dtable), a.ldt, a.width, first, min(a.zero_rows, a.vocab - first), found);
 }
 
-// The first workgroups rank 64 tokens each among their chunk's: a lane has a token, a wave an eighth of the chunk.  Ids that are as
-// large count if they stand before it.  The others write zeros: bytes that keep the memory busy meanwhile (16384 tokens into 32000 by 4096 in bfloat16: 218 MB beside
-// ranking take 40 to 51 us, by what the caches have to write back; ranking alone 13).
+// The first workgroups sort a chunk each: by four bits at a time, lowest first, each time in the order that there was, so that equal ids stay in the
+// tokens' order.  A token's new place is the number of smaller digits, of the same digit in the waves before and, by ballots, in the lanes
+// before it.  The others write zeros: bytes that keep the memory busy meanwhile (16384 tokens into 32000 by 4096 in bfloat16: 218 MB, 40 to 51 us by what
+// the caches have to write back; sorting alone takes 15 at 65536 tokens).
 template <typename T>
-__global__ __launch_bounds__(kRankThreads) void rank_kernel(Tokens a)
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(Tokens a)
 {
-    __shared__ __attribute__((aligned(16))) uint32_t keys[kChunk];
-    __shared__ uint32_t counts[kRankSlices][64];
-    const uint32_t group = blockIdx.x;
-    if (group >= a.groups) return zero_rows<T, kRankThreads>(a, group - a.groups, keys);
-    const uint32_t chunk = group * 64 / kChunk * kChunk, have = min(kChunk, a.rows - chunk), whole = (have + 63) / 64 * 64;
-#pragma unroll 4
-    for (uint32_t i = threadIdx.x; i < whole; i += kRankThreads) keys[i] = i < have ? id_at(a.ids, a.wide, chunk + i, a.vocab) : 0xFFFFFFFFu;
-    __syncthreads();
-    const uint32_t lane = threadIdx.x % 64, slice = threadIdx.x / 64, at = group * 64 - chunk + lane;
-    const uint32_t key = keys[at];
-    const uint32_t each = (whole / 64 + kRankSlices - 1) / kRankSlices * 64;
-    const uint32_t begin = slice * each, end = min(begin + each, whole), own = at / 64 * 64;
-    uint32_t count = 0;
-    // (a wave's tokens are 64 neighbours: what lies before them counts if it is at most the key, what lies behind if it is under it)
-    for (uint32_t i = begin; i < end; i += 64) {
-        if (i == own) {
-#pragma unroll 8
-            for (uint32_t j = 0; j < 64; ++j) {
-                const uint32_t k = keys[i + j];
-                count += k < key || (k == key && i + j < at);
-            }
-        } else {
-            const uint32_t under = key + (i < own);
+    __shared__ uint32_t keys[kChunk], counts[16 * kSlots * kSortWaves], room[kSortWaves];
+    __shared__ uint16_t order[kChunk];
+    static_assert(16 * kSlots * kSortWaves == kSortThreads, "a count to a thread");
+    if (blockIdx.x >= a.groups) return zero_rows<T, kSortThreads>(a, blockIdx.x - a.groups, keys);
+    const uint32_t chunk = blockIdx.x * kChunk, have = min(kChunk, a.rows - chunk), slots = (have + kSortThreads - 1) / kSortThreads;
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint64_t before = (1ull << lane) - 1;
+    uint32_t key[kSlots], at[kSlots];
 #pragma unroll
-            for (uint32_t j = 0; j < 64; j += 4) {
-                const uint4 k = *reinterpret_cast<const uint4 *>(&keys[i + j]);
-                count += (k.x < under) + (k.y < under) + (k.z < under) + (k.w < under);
+    for (uint32_t s = 0; s < kSlots; ++s) {
+        at[s] = s * kSortThreads + threadIdx.x;
+        key[s] = at[s] < have ? id_at(a.ids, a.wide, chunk + at[s], a.vocab) : 0xFFFFFFFFu;  // (behind all others)
+    }
+    for (uint32_t shift = 0; shift < a.bits; shift += 4) {
+        counts[threadIdx.x] = 0;
+        __syncthreads();
+        uint32_t place[kSlots];
+#pragma unroll
+        for (uint32_t s = 0; s < kSlots; ++s) {
+            if (s >= slots) break;
+            const uint32_t digit = key[s] >> shift & 15;
+            uint64_t same = ~0ull;
+#pragma unroll
+            for (uint32_t b = 0; b < 4; ++b) {
+                const uint64_t set = __ballot(digit >> b & 1);
+                same &= digit >> b & 1 ? set : ~set;
             }
+            place[s] = uint32_t(__popcll(same & before));
+            if (!place[s]) counts[(digit * kSlots + s) * kSortWaves + wave] = uint32_t(__popcll(same));
+        }
+        __syncthreads();
+        uint32_t all;
+        const uint32_t first = block_excl_scan<uint32_t, kSortWaves>(counts[threadIdx.x], &all, room);
+        counts[threadIdx.x] = first;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t s = 0; s < kSlots; ++s) {
+            if (s >= slots) break;
+            const uint32_t to = counts[((key[s] >> shift & 15) * kSlots + s) * kSortWaves + wave] + place[s];
+            keys[to] = key[s];
+            order[to] = uint16_t(at[s]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t s = 0; s < kSlots; ++s) {
+            if (s >= slots) break;
+            key[s] = keys[s * kSortThreads + threadIdx.x];
+            at[s] = order[s * kSortThreads + threadIdx.x];
         }
     }
-    counts[slice][lane] = count;
-    __syncthreads();
-    if (slice || at >= have) return;
-    count = 0;
 #pragma unroll
-    for (uint32_t s = 0; s < kRankSlices; ++s) count += counts[s][lane];
-    a.to.keys[chunk + count] = key;
-    a.to.order[chunk + count] = chunk + at;
+    for (uint32_t s = 0; s < kSlots; ++s) {
+        const uint32_t i = s * kSortThreads + threadIdx.x;
+        if (i >= have) break;
+        a.to.keys[chunk + i] = key[s];
+        a.to.order[chunk + i] = chunk + at[s];
+    }
 }
 
 // How many of `n` sorted keys are under `key`.
@@ -201,21 +231,35 @@ __device__ inline uint32_t under(const uint32_t *keys, uint32_t n, uint32_t key)
     return lo;
 }
 
-// Sorted lists of `run` tokens, kMerge of them to one: a token's place is its own list's, and what the others have before it.
+// Sorted lists of `run` tokens, kMerge of them to one: a token's place is its own list's, and what the others have before it.  The first half
+// of each search is among 64 of a list's ids in local memory.  (65536 tokens: 29 us without, 23 with.)
+constexpr uint32_t kSamples = 64;
 __global__ __launch_bounds__(256) void merge_kernel(Sorted from, uint32_t rows, uint32_t run, Sorted to)
 {
-    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+    __shared__ uint32_t samples[kMerge][kSamples];
+    static_assert(kChunk % 256 == 0, "a workgroup's tokens are of one list");
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x, own = blockIdx.x * 256 / run, first = own / kMerge * kMerge, step = run / kSamples;
+#pragma unroll
+    for (uint32_t s = threadIdx.x; s < kMerge * kSamples; s += 256) {
+        const uint64_t at = uint64_t(first + s / kSamples) * run + s % kSamples * step;
+        samples[s / kSamples][s % kSamples] = at < rows ? from.keys[at] : 0xFFFFFFFFu;
+    }
+    __syncthreads();
     if (i >= rows) return;
-    const uint32_t own = i / run, first = own / kMerge * kMerge, key = from.keys[i];
-    uint32_t at = i % run;
+    const uint32_t key = from.keys[i];
+    uint32_t place = i % run;
 #pragma unroll 4
     for (uint32_t k = 0; k < kMerge; ++k) {
         const uint32_t c = first + k;
         if (c == own || uint64_t(c) * run >= rows) continue;
-        at += under(from.keys + c * run, min(run, rows - c * run), key + (c < own));
+        const uint32_t want = key + (c < own), some = under(samples[k], kSamples, want);
+        if (!some) continue;
+        // (the last sample under it is, and the next one is not)
+        const uint32_t begin = (some - 1) * step + 1, length = min(run, rows - c * run);
+        place += begin + under(from.keys + c * run + begin, min(step - 1, length - begin), want);
     }
-    to.keys[first * run + at] = key;
-    to.order[first * run + at] = from.order[i];
+    to.keys[first * run + place] = key;
+    to.order[first * run + place] = from.order[i];
 }
 
 // ------------------------------------------------------------------ sums
@@ -227,6 +271,7 @@ struct Sums {
     float *partial;  // [pieces][2][width]: of a piece the sum of its first run, if that began before it, and of the run that goes on behind it
     uint64_t lddy, ldt;
     uint32_t rows, width, vocab, pieces, spans, accumulate;
+    uint32_t zero_rows;  // as Tokens has them, where this launch writes the zeros
     float scale;
 };
 
@@ -295,7 +340,7 @@ __global__ __launch_bounds__(kSumThreads) void direct_kernel(Tokens a, Sums b)
     if (have) finish_row<T, false>(b, key, c, have, sum);
 }
 
-// A workgroup sums a piece of sorted tokens, 256 * V columns of them.  Bound by the bytes of dy, of the rows that are finished and of the partial sums: 16384
+// A workgroup sums a piece of sorted tokens, 256 * V columns of them; workgroups behind those write zeros.  Bound by the bytes of dy, of the rows that are finished and of the partial sums: 16384
 // tokens of 4096 in bfloat16 40 us, 4.9 TB/s.
 template <typename T, uint32_t PIECE, bool WHOLE>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
@@ -303,6 +348,16 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
     constexpr uint32_t V = 16 / sizeof(T);
     const uint32_t span = blockIdx.x % a.spans, c = (span * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
     const uint32_t piece = blockIdx.x / a.spans;
+    if (piece >= a.pieces) {
+        __shared__ uint32_t found[kZeroRows];
+        const uint32_t first = (blockIdx.x - a.pieces * a.spans) * a.zero_rows, rows = min(a.zero_rows, a.vocab - first);
+        if (threadIdx.x < rows) {
+            const uint32_t v = first + threadIdx.x, at = under(a.sorted.keys, a.rows, v);
+            found[threadIdx.x] = at < a.rows && a.sorted.keys[at] == v;
+        }
+        __syncthreads();
+        return write_zeros<T, kSumThreads>(static_cast<T *>(a.dtable), a.ldt, a.width, first, rows, found);
+    }
     const uint32_t begin = piece * PIECE, n = min(PIECE, a.rows - begin);
     // a lane has a token's id and row, the piece's neighbours' ids behind them; all rows are asked for before the first is needed
     const uint32_t lane = threadIdx.x % 64, at = lane < n ? begin + lane : lane == PIECE ? begin - 1 : begin + n;
@@ -491,11 +546,14 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
     a.spans = uint32_t((l->width + kSumThreads * V - 1) / (kSumThreads * V));
     a.accumulate = l->accumulate;
     a.scale = float(l->scale);
+    uint32_t zeros = 0;
     {
         // (rows to a workgroup so that there are two workgroups to a compute unit)
-        Tokens t{l->ids, sorted, l->dtable, l->ldt, a.rows, a.width, a.vocab, l->id_type, uint32_t((M + 63) / 64), 1};
+        Tokens t{l->ids, sorted, l->dtable, l->ldt, a.rows, a.width, a.vocab, l->id_type, uint32_t((M + kChunk - 1) / kChunk), 1, 0};
+        while (l->vocab >> t.bits) ++t.bits;
         while (t.zero_rows < kZeroRows && l->vocab / t.zero_rows > 2 * uint64_t(device_cu_count())) t.zero_rows *= 2;
-        const uint32_t zeros = l->accumulate ? 0 : (a.vocab + t.zero_rows - 1) / t.zero_rows;
+        if (!l->accumulate) zeros = (a.vocab + t.zero_rows - 1) / t.zero_rows;
+        a.zero_rows = t.zero_rows;
         if (direct) {
             t.groups = a.rows * a.spans;
             ProfileScope prof("embed_sum", s);
@@ -503,7 +561,8 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
             return hip_ok(hipGetLastError());
         }
         ProfileScope prof("embed_sort", s);
-        rank_kernel<T><<<t.groups + zeros, kRankThreads, 0, s>>>(t);
+        sort_kernel<T><<<t.groups + (M <= kZerosFirst ? zeros : 0), kSortThreads, 0, s>>>(t);
+        if (M <= kZerosFirst) zeros = 0;
         for (uint64_t run = kChunk; run < M; run *= kMerge) {
             merge_kernel<<<uint32_t((M + 255) / 256), 256, 0, s>>>(sorted, a.rows, uint32_t(run), other);
             const Sorted was = sorted;
@@ -517,8 +576,8 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
         const uint32_t runs = (pieces - 1) * uint32_t((l->width + 64 * V - 1) / (64 * V));
         const auto go = [&](auto size) {
             constexpr uint32_t P = decltype(size)::value;
-            if (l->width % V) sum_kernel<T, P, false><<<pieces * a.spans, kSumThreads, 0, s>>>(a);
-            else sum_kernel<T, P, true><<<pieces * a.spans, kSumThreads, 0, s>>>(a);
+            if (l->width % V) sum_kernel<T, P, false><<<pieces * a.spans + zeros, kSumThreads, 0, s>>>(a);
+            else sum_kernel<T, P, true><<<pieces * a.spans + zeros, kSumThreads, 0, s>>>(a);
             if (runs) run_kernel<T, P><<<runs, kSumThreads, 0, s>>>(a);
         };
         if (piece == kShortPiece) go(std::integral_constant<uint32_t, kShortPiece>());

@@ -28,7 +28,8 @@ constexpr uint64_t kHeldRows = 1024, kHeld = 1u << 23;
 
 // What a piece of the vocabulary may hold (ds, operands laid out, the waves' sums), and its fewest rows.  (us, a quarter / a half / one GiB, backward in
 // bfloat16: 8192 rows of 768 over 50257 2613 / 2317 / 2170, of 4096 over 32000 5314 / 5251 / 5256, over 128256 21161 / 20707 / 20662: dx of narrow
-// rows has few tiles, and more parts the longer its sums are.)
+// rows has few tiles, and more parts the longer its sums are; float32, a quarter / a half: 1024 of 768 over 50257 1202 / 1235, 2048 of 4096 over 32000
+// 7575 / 7215.)
 constexpr uint64_t kPieceBytes = 512ull << 20, kPieceRows = 1024;
 
 // ------------------------------------------------------------------ terms and rows
@@ -55,33 +56,35 @@ __device__ inline float wave_max(float x)
     return x;
 }
 
-// A teacher's shares, a row to a wave.
+// A teacher's shares, a row to a wave.  (Logits are divided by the temperature once the largest is taken from them: a row whose
+// logits are all the type's lowest value, some masks' mark, has shares alike.)
 __global__ __launch_bounds__(256) void terms_kernel(Terms a)
 {
     const uint64_t row = uint64_t(blockIdx.x) * 4 + threadIdx.x / 64;
     if (row >= a.rows) return;
     const uint32_t lane = threadIdx.x & 63;
     const float *logits = a.logits + row * a.terms;
+    const float over2 = a.over * kLog2e;
     float top = -INFINITY, sum = 0;
     bool any = false;
     for (uint32_t k = lane; k < a.terms; k += 64) {
         const float x = logits[k];
         if (id_at(a.ids, a.wide, row * a.terms + k, a.vocab) == a.vocab || x == -INFINITY) continue;
         any = true;
-        top = fmaxf(top, x * a.over);
+        top = fmaxf(top, x);
     }
     top = wave_max(top);
     if (top == -INFINITY) top = 0;  // (all there is is NaN)
     for (uint32_t k = lane; k < a.terms; k += 64) {
         const float x = logits[k];
         if (id_at(a.ids, a.wide, row * a.terms + k, a.vocab) == a.vocab || x == -INFINITY) continue;
-        sum += __builtin_amdgcn_exp2f((x * a.over - top) * kLog2e);
+        sum += __builtin_amdgcn_exp2f((x - top) * over2);
     }
     sum = wave_sum(sum);
     for (uint32_t k = lane; k < a.terms; k += 64) {
         const float x = logits[k];
         const bool none = id_at(a.ids, a.wide, row * a.terms + k, a.vocab) == a.vocab || x == -INFINITY;
-        float q = __builtin_amdgcn_exp2f((x * a.over - top) * kLog2e) / sum;
+        float q = __builtin_amdgcn_exp2f((x - top) * over2) / sum;
         if (q < kLeast) q = kLeast;  // (a term, if one that does not count: its score is saved)
         a.q[row * a.terms + k] = none ? 0.0f : q;
     }
@@ -613,13 +616,10 @@ __global__ __launch_bounds__(THREADS) void held_kernel(Held a)
     for (uint32_t k = threadIdx.x; k < K; k += THREADS) {
         const bool none = id_at(a.terms.ids, a.terms.wide, first + k, V) == V;
         float x = none ? -INFINITY : 0.0f;
-        if (a.terms.logits && !none) x = a.terms.logits[first + k] * (a.terms.over * kLog2e);
+        if (a.terms.logits && !none) x = a.terms.logits[first + k];
         q[k] = x;
-        if (x == -INFINITY) continue;
-        any = true;
-        const float most = fmaxf(top, x), against = most == -INFINITY ? 0.0f : most;
-        sum = sum * __builtin_amdgcn_exp2f(top - against) + __builtin_amdgcn_exp2f(x - against);
-        top = most;
+        any = any || x != -INFINITY;
+        top = fmaxf(top, x);
     }
     any = __syncthreads_or(any);
     if (!any) {
@@ -628,18 +628,21 @@ __global__ __launch_bounds__(THREADS) void held_kernel(Held a)
             for (uint32_t k = threadIdx.x; k < 1 + K; k += THREADS) a.saved[uint64_t(row) * (1 + K) + k] = 0;
         return;
     }
+    const float over2 = a.terms.over * kLog2e;
     if (a.terms.logits) {
         together(top, sum);
         const float against = top == -INFINITY ? 0.0f : top;
+        sum = 0;
+        for (uint32_t k = threadIdx.x; k < K; k += THREADS) sum += __builtin_amdgcn_exp2f((q[k] - against) * over2);
+        sum = block_sum<float, W>(sum, room);
         for (uint32_t k = threadIdx.x; k < K; k += THREADS) {
-            const float x = q[k], share = __builtin_amdgcn_exp2f(x - against) / sum;
+            const float x = q[k], share = __builtin_amdgcn_exp2f((x - against) * over2) / sum;
             q[k] = x == -INFINITY ? 0.0f : share < kLeast ? kLeast : share;
         }
     } else if (threadIdx.x == 0) {
         q[0] = 1;
     }
     // the scores, four neighbours at a time, times log2(e) / T
-    const float over2 = a.terms.over * kLog2e;
     top = -INFINITY;
     sum = 0;
     for (uint32_t c = threadIdx.x * 4; c < V; c += THREADS * 4) {
@@ -783,8 +786,8 @@ Operands operands_of(uint64_t M, uint64_t D, uint64_t V, const void *w, uint64_t
 }
 
 // Rows of a piece of the vocabulary that holds so many bytes a row: pieces alike, but in whole rounds of tiles, of which 4096 rows make so many
-// that they fill 256 compute units at most sizes.  (Float32, 1024 rows of 768 over 50257: pieces of 20480 instead of
-// three alike of 16768 take 1350 us instead of 1386.)
+// that they fill 256 compute units at most sizes.  (Float32, 1024 rows of 768 over 50257, three pieces: of 20480
+// rows 1350 us, alike, of 16768, 1386.)
 uint64_t piece_rows(uint64_t vocab, uint64_t bytes)
 {
     uint64_t n = kPieceBytes / (bytes ? bytes : 1);

@@ -207,3 +207,48 @@ def test_an_expanded_gradient_is_one_number():
     want = t.cross_entropy_backward(each, i["x"], i["head"], i["targets"], saved)
     for d in (torch.tensor(0.25, device="cuda"), torch.tensor([0.25], device="cuda"), torch.tensor(0.25, device="cuda").expand(1300)):
         assert torch.equal(t.cross_entropy_backward(d, i["x"], i["head"], i["targets"], saved), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [5, 700, 5000])
+def test_what_a_workspace_holds_does_not_matter(dtype, rows, monkeypatch):
+    """The same bits from workspaces of zeros, of NaN and of whatever is there."""
+    from paper_2504_05638_amd import train
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda").to(dtype)  # noqa: E731
+    D, V, K = 77, 5001, 6
+    x, w, dy, gain = rand(rows, D), rand(V, D), rand(rows, D), rand(D)
+    ids = torch.randint(-400, V, (rows, K), generator=gen, device="cuda")
+    ids[::5] = -1
+    logits, dloss = torch.randn(rows, K, generator=gen, device="cuda"), torch.randn(rows, generator=gen, device="cuda")
+    first, made = ids[:, 0].contiguous(), []
+
+    def run(fill):
+        def work(nbytes, like):
+            if not nbytes:
+                return None, None
+            ws = torch.full((nbytes,), fill, dtype=torch.uint8, device=like.device)
+            made.append(nbytes)
+            return ws, ws.data_ptr()
+
+        monkeypatch.setattr(train, "_work", work)
+        out = []
+        for a, b in ((None, None), (logits, 2.0)):
+            t = first if a is None else ids
+            more = () if a is None else (a,)
+            named = {} if a is None else {"temperature": b}
+            forward, backward = (train.cross_entropy, train.cross_entropy_backward) if a is None else (train.distill, train.distill_backward)
+            loss, saved = forward(x, w, t, *more, save=True, **named)
+            dw = torch.zeros_like(w)
+            out += [loss, saved, dw, backward(dloss, x, w, t, *more, saved, dw=dw, **named)]
+        table = torch.zeros_like(w)
+        train.embedding_backward(dy, first, table)
+        _, stats = train.norm(x, gain, save=True)
+        dgain, dshift = torch.empty_like(gain), torch.empty_like(gain)
+        return out + [table, train.norm_backward(dy, x, gain, stats, dw=dgain, db=dshift), dgain, dshift]
+
+    want = run(0)
+    assert len(made) >= 5 and all(torch.isfinite(t).all() for t in want)
+    for fill in (255, 127):
+        for k, (a, b) in enumerate(zip(run(fill), want)):
+            assert torch.equal(a, b), k

@@ -245,6 +245,30 @@ def test_scores_far_apart(dtype):
     assert sure.any() and float(dx[sure].abs().max()) <= 2 * 70 * float(w.abs().max()) * float(ref.lse_err.max() + ref.s_err.max())
 
 
+@pytest.mark.parametrize("temperature", [1.0, 0.5, 30.0])
+@pytest.mark.parametrize("shape", [(50, 64, 300), (1100, 64, 300), (1100, 64, 7700)], ids=str)
+def test_a_teachers_mask_of_the_lowest_value(shape, temperature):
+    """Where all of a row's logits are float32's lowest value their shares are alike, as of any other equal ones; beside others they
+    have none.  (What is added for such a term is less than 10^-34, which no sum of float32 here takes notice of: equal results.)"""
+    from paper_2504_05638_amd.train import distill, distill_backward
+    M, D, V = shape
+    x, w = _randn((M, D), 1, torch.bfloat16), _randn((V, D), 2, torch.bfloat16, D ** -0.5)
+    ids, logits = _terms(M, V, 9, 3, True)
+    least = torch.finfo(torch.float32).min
+    some = torch.rand(logits.shape, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda") < 0.4
+    some[:, 0] = False
+    ids[:, 0] = ids[:, 0].clamp(0, V - 1)           # (each row has a term that is not masked so)
+    logits[:, 0] = logits[:, 0].clamp(min=-9.0)
+    masked, plain = logits.masked_fill(some, least), logits.masked_fill(some, -math.inf)
+    masked[::7], plain[::7] = least, 0.0
+    (got, saved), (want, other) = (distill(x, w, ids, t, temperature=temperature, save=True) for t in (masked, plain))
+    assert torch.isfinite(want).all() and torch.equal(got, want) and torch.equal(saved[:, 0], other[:, 0])
+    one = torch.ones((), device="cuda")
+    dw, dwant = torch.empty_like(w), torch.empty_like(w)
+    dx = distill_backward(one, x, w, ids, masked, saved, temperature=temperature, dw=dw)
+    assert torch.equal(dx, distill_backward(one, x, w, ids, plain, other, temperature=temperature, dw=dwant)) and torch.equal(dw, dwant)
+
+
 def test_not_finite_rows_stay_where_they_are():
     from paper_2504_05638_amd.train import cross_entropy
     x, w, t = _randn((40, 96), 1, torch.float32), _randn((200, 96), 2, torch.float32), torch.arange(40, device="cuda")

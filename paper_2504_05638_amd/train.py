@@ -414,7 +414,7 @@ def _loss_backward(dloss, x, w, ids, logits, saved, temperature, dx, dw, accumul
     _need(need_dx or dx is None, "dx is given, but need_dx is not")
     sp = _floats(saved, "saved", (m, 1 + terms), device)
     _need(dloss.shape == shape or (dloss.numel() == 1 and dloss.dim() <= 1), "dloss: a number for each row, or one, is wanted")
-    one = m > 0 and all(step == 0 or n == 1 for step, n in zip(dloss.stride(), dloss.shape))     # (also one that is expanded)
+    one = dloss.numel() > 0 and all(step == 0 or n == 1 for step, n in zip(dloss.stride(), dloss.shape))     # (also one that is expanded)
     gp = _floats(dloss.as_strided((1,), (1,)) if one else dloss, "dloss", (1,) if one else shape, device)
     _need(dx is None or dx.shape == x.shape, "dx: x's shape is wanted")
     dp, ldd = _matrix(dx, "dx", m, k, dtype, device)

@@ -252,3 +252,16 @@ def test_what_a_workspace_holds_does_not_matter(dtype, rows, monkeypatch):
     for fill in (255, 127):
         for k, (a, b) in enumerate(zip(run(fill), want)):
             assert torch.equal(a, b), k
+
+
+@pytest.mark.parametrize("shape", [(0,), (2, 0)], ids=str)
+def test_an_empty_batch_takes_one_number(shape):
+    from paper_2504_05638_amd.train import cross_entropy, cross_entropy_backward
+    x, w = torch.empty(*shape, 16, device="cuda"), torch.randn(50, 16, device="cuda")
+    t = torch.empty(shape, dtype=torch.int64, device="cuda")
+    loss, saved = cross_entropy(x, w, t, save=True)
+    assert loss.shape == shape
+    for dloss in (torch.ones((), device="cuda"), torch.ones(1, device="cuda"), torch.empty(shape, device="cuda")):
+        dw = torch.full_like(w, float("nan"))
+        assert cross_entropy_backward(dloss, x, w, t, saved, dw=dw).shape == x.shape
+        assert not dw.any()

@@ -57,6 +57,12 @@ struct Lookup {
     float scale;
 };
 
+// Where a lane whose piece begins at column c loads from: the piece, or, of a row's last one that is not whole, the row's last 16 bytes, of which
+// its own elements are the last ones.  Rows shorter than that are not loaded so.  (us, so / such a piece one element after the other, bfloat16:
+// lookup of 8192 rows of 4095 with a residual 36 / 40; gradient of 16384 tokens into 32000 by 4095 103 / 132, added to a table 84 / 136.)
+template <uint32_t V>
+__device__ inline uint32_t load_at(uint32_t c, uint32_t width) { return min(c, width - V); }
+
 // A wave takes kSteps pieces of 16 bytes to a lane of one row.
 constexpr uint32_t kSteps = 4;
 template <typename T>
@@ -75,27 +81,33 @@ __global__ __launch_bounds__(256) void lookup_kernel(Lookup a)
 #pragma unroll
     for (uint32_t s = 0; s < kSteps; ++s) {
         const uint32_t c = from + s * 64 * V;
-        if (c + V > a.width) continue;
-        if (token) in[s].load(row + c);
-        if (a.residual) add[s].load(res + c);
+        if (c >= a.width || a.width < V) continue;
+        if (token) in[s].load(row + load_at<V>(c, a.width));
+        if (a.residual) add[s].load(res + load_at<V>(c, a.width));
     }
 #pragma unroll
     for (uint32_t s = 0; s < kSteps; ++s) {
         const uint32_t c = from + s * 64 * V;
         if (c >= a.width) break;
-        if (c + V <= a.width) {
-            float z[V];
-#pragma unroll
-            for (uint32_t j = 0; j < V; ++j) z[j] = a.residual ? a.scale * in[s][j] + add[s][j] : a.scale * in[s][j];
-            if (!token)
-#pragma unroll
-                for (uint32_t j = 0; j < V; ++j) z[j] = add[s][j];
-            store_n<T, V>(y + c, z);
-        } else {
-            for (uint32_t j = c; j < a.width; ++j) {
+        if (a.width < V) {
+            for (uint32_t j = 0; j < a.width; ++j) {
                 const float z = token ? a.scale * widen(row[j]) : 0.0f;
                 y[j] = narrow<T>(a.residual ? z + widen(res[j]) : z);
             }
+            break;
+        }
+        float z[V];
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) z[j] = a.residual ? a.scale * in[s][j] + add[s][j] : a.scale * in[s][j];
+        if (!token)
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) z[j] = add[s][j];
+        if (c + V <= a.width) {
+            store_n<T, V>(y + c, z);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j)
+                if (a.width - V + j >= c) y[a.width - V + j] = narrow<T>(z[j]);
         }
     }
 }
@@ -127,11 +139,11 @@ __device__ inline void write_zeros(T *dtable, uint64_t ld, uint32_t width, uint3
     for (uint32_t i = threadIdx.x; i < rows * across; i += THREADS) {
         const uint32_t r = i / across, c = (i - r * across) * V;
         if (found[r]) continue;
-        T *to = dtable + (first + r) * ld + c;
-        if (c + V <= width) {
-            store_n<T, V>(to, zeros);
+        T *row = dtable + (first + r) * ld;
+        if (width >= V) {
+            store_n<T, V>(row + load_at<V>(c, width), zeros);
         } else {
-            for (uint32_t j = 0; c + j < width; ++j) to[j] = T(0);
+            for (uint32_t j = 0; j < width; ++j) row[j] = T(0);
         }
     }
 }
@@ -275,33 +287,57 @@ struct Sums {
     float scale;
 };
 
-// WHOLE: rows are whole pieces of V elements.
-template <typename T, bool WHOLE>
-__device__ inline void finish_row(const Sums &a, uint32_t key, uint32_t c, uint32_t have, const float (&sum)[16 / sizeof(T)])
+// By width: rows of whole pieces of V elements, of V at least, of less.
+enum { kWhole, kTail, kThin };
+
+// Of the piece that begins at column c; `sum` as load_piece has it.  A row's last piece that is not whole overlaps the one before it, whose sums are
+// the same: without what is there to be added to, both may write them.
+template <typename T, int ROWS>
+__device__ inline void finish_row(const Sums &a, uint32_t key, uint32_t c, const float (&sum)[16 / sizeof(T)])
 {
     constexpr uint32_t V = 16 / sizeof(T);
-    T *to = static_cast<T *>(a.dtable) + key * a.ldt + c;
-    if (WHOLE || have == V) {
+    T *row = static_cast<T *>(a.dtable) + key * a.ldt;
+    if constexpr (ROWS != kThin) {
+        const uint32_t at = ROWS == kWhole ? c : load_at<V>(c, a.width);
         float z[V], was[V];
-        if (a.accumulate) load_n<T, V>(to, was);
+        if (a.accumulate) load_n<T, V>(row + at, was);
 #pragma unroll
         for (uint32_t j = 0; j < V; ++j) z[j] = a.accumulate ? a.scale * sum[j] + was[j] : a.scale * sum[j];
-        store_n<T, V>(to, z);
+        if (ROWS == kWhole || !a.accumulate || at == c) return store_n<T, V>(row + at, z);
+#pragma unroll
+        for (uint32_t j = 1; j < V; ++j)
+            if (at + j >= c) row[at + j] = narrow<T>(z[j]);
     } else {
 #pragma unroll
         for (uint32_t j = 0; j < V; ++j)
-            if (j < have) to[j] = narrow<T>(a.accumulate ? a.scale * sum[j] + widen(to[j]) : a.scale * sum[j]);
+            if (j < a.width) row[j] = narrow<T>(a.accumulate ? a.scale * sum[j] + widen(row[j]) : a.scale * sum[j]);
+    }
+}
+
+// A lane's piece of a row of dy, for finish_row.  (Lanes behind the row's end have its last piece as well, and no use for it: loads without
+// branches go out together.)
+template <typename T, int ROWS, bool PAST>
+__device__ inline void load_piece(const T *row, uint32_t c, uint32_t width, Lane<T, 16 / sizeof(T)> &to)
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    if constexpr (ROWS != kThin) {
+        const T *from = row + load_at<V>(c, width);
+        if constexpr (PAST) to.v = __builtin_nontemporal_load(reinterpret_cast<const typename Lane<T, V>::vec *>(from));
+        else to.load(from);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) to.v[j] = c + j < width ? row[c + j] : T(0);
     }
 }
 
 // Up to kDirect tokens: a workgroup to a token and 256 * V columns, if it is the first of its id, and the zeros beside them.
-template <typename T>
+template <typename T, int ROWS>
 __global__ __launch_bounds__(kSumThreads) void direct_kernel(Tokens a, Sums b)
 {
     constexpr uint32_t V = 16 / sizeof(T), kAhead = 16;
     __shared__ uint32_t keys[kDirect], list[kDirect + kAhead];
     if (blockIdx.x >= a.groups) return zero_rows<T, kSumThreads>(a, blockIdx.x - a.groups, keys);
-    const uint32_t t = blockIdx.x / b.spans, c = (blockIdx.x % b.spans * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
+    const uint32_t t = blockIdx.x / b.spans, c = (blockIdx.x % b.spans * kSumThreads + threadIdx.x) * V;
     for (uint32_t i = threadIdx.x; i < a.rows; i += kSumThreads) keys[i] = id_at(a.ids, a.wide, i, a.vocab);
     __syncthreads();
     const uint32_t key = keys[t];
@@ -323,30 +359,22 @@ __global__ __launch_bounds__(kSumThreads) void direct_kernel(Tokens a, Sums b)
     for (uint32_t k = 0; k < n; k += kAhead) {
         Lane<T, V> x[kAhead];
 #pragma unroll
-        for (uint32_t i = 0; i < kAhead; ++i) {
-            const T *from = static_cast<const T *>(b.dy) + list[min(k + i, n - 1)] * b.lddy + c;
-            if (have == V) {
-                x[i].load(from);
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < V; ++j) x[i].v[j] = j < have ? from[j] : T(0);
-            }
-        }
+        for (uint32_t i = 0; i < kAhead; ++i) load_piece<T, ROWS, false>(static_cast<const T *>(b.dy) + list[min(k + i, n - 1)] * b.lddy, c, a.width, x[i]);
 #pragma unroll
         for (uint32_t i = 0; i < kAhead; ++i)
 #pragma unroll
             for (uint32_t j = 0; j < V; ++j) sum[j] += k + i < n ? x[i][j] : 0.0f;
     }
-    if (have) finish_row<T, false>(b, key, c, have, sum);
+    if (c < a.width) finish_row<T, ROWS>(b, key, c, sum);
 }
 
 // A workgroup sums a piece of sorted tokens, 256 * V columns of them; workgroups behind those write zeros.  Bound by the bytes of dy, of the rows that are finished and of the partial sums: 16384
 // tokens of 4096 in bfloat16 40 us, 4.9 TB/s.
-template <typename T, uint32_t PIECE, bool WHOLE>
+template <typename T, uint32_t PIECE, int ROWS>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
 {
     constexpr uint32_t V = 16 / sizeof(T);
-    const uint32_t span = blockIdx.x % a.spans, c = (span * kSumThreads + threadIdx.x) * V, have = c < a.width ? min(V, a.width - c) : 0;
+    const uint32_t span = blockIdx.x % a.spans, c = (span * kSumThreads + threadIdx.x) * V;
     const uint32_t piece = blockIdx.x / a.spans;
     if (piece >= a.pieces) {
         __shared__ uint32_t found[kZeroRows];
@@ -374,16 +402,16 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
     uint32_t now = keys[0];
     bool began = now == before;
     auto flush = [&](bool goes_on) {
-        if (now >= a.vocab || !have) return;
-        if (!began && !goes_on) return finish_row<T, WHOLE>(a, now, c, have, sum);
+        if (now >= a.vocab || c >= a.width) return;
+        if (!began && !goes_on) return finish_row<T, ROWS>(a, now, c, sum);
         // (a run that fills its piece and goes on both ways has the first place)
-        float *to = a.partial + (uint64_t(piece) * 2 + (began ? 0 : 1)) * a.width + c;
-        if (WHOLE || have == V) {
-            store_n<float, V>(to, sum);
+        float *to = a.partial + (uint64_t(piece) * 2 + (began ? 0 : 1)) * a.width;
+        if constexpr (ROWS != kThin) {
+            store_n<float, V>(to + load_at<V>(c, a.width), sum);
         } else {
 #pragma unroll
             for (uint32_t j = 0; j < V; ++j)
-                if (j < have) to[j] = sum[j];
+                if (j < a.width) to[j] = sum[j];
         }
     };
     // rows come four at a time, past the caches' order, which the table's rows are left to (61 -> 40 us), the next ones while these are added (two, eight: 1 % slower, the same; all at once, which leaves fewer workgroups
@@ -392,15 +420,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
     Lane<T, V> x[2][kAhead];
     auto fetch = [&](uint32_t first, Lane<T, V>(&to)[kAhead]) __attribute__((always_inline)) {
 #pragma unroll
-        for (uint32_t k = 0; k < kAhead; ++k) {
-            const T *from = static_cast<const T *>(a.dy) + rows[first + k] * a.lddy + c;
-            if (WHOLE || have == V) {
-                if (have) to[k].v = __builtin_nontemporal_load(reinterpret_cast<const typename Lane<T, V>::vec *>(from));
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < V; ++j) to[k].v[j] = j < have ? from[j] : T(0);
-            }
-        }
+        for (uint32_t k = 0; k < kAhead; ++k) load_piece<T, ROWS, true>(static_cast<const T *>(a.dy) + rows[first + k] * a.lddy, c, a.width, to[k]);
     };
     fetch(0, x[0]);
 #pragma unroll
@@ -426,13 +446,13 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
 // Runs that go on behind the piece that they begin in: their partial sums in order, a quarter to each of the four waves that share 64 * V
 // columns, eight on their way at once.  (A token's share of text can be a tenth: 50 pieces of 16384 tokens, 10 us; one
 // part after the other, four on their way, 31.)
-template <typename T, uint32_t PIECE>
+template <typename T, uint32_t PIECE, int ROWS>
 __global__ __launch_bounds__(kSumThreads) void run_kernel(Sums a)
 {
     constexpr uint32_t V = 16 / sizeof(T), kAhead = 8;
     __shared__ float parts[kRunSlices][V][64];
     const uint32_t spans = (a.width + 64 * V - 1) / (64 * V), piece = blockIdx.x / spans, lane = threadIdx.x % 64, slice = threadIdx.x / 64;
-    const uint32_t c = (blockIdx.x % spans * 64 + lane) * V, have = c < a.width ? min(V, a.width - c) : 0;
+    const uint32_t c = (blockIdx.x % spans * 64 + lane) * V;
     const uint32_t begin = piece * PIECE, next = begin + PIECE;
     if (next >= a.rows) return;
     const uint32_t key = a.sorted.keys[next];
@@ -448,13 +468,13 @@ __global__ __launch_bounds__(kSumThreads) void run_kernel(Sums a)
 #pragma unroll
             for (uint32_t j = 0; j < V; ++j) x[k][j] = 0;
             if (p + k >= to) continue;
-            const float *at = a.partial + (uint64_t(piece + p + k) * 2 + (p + k == 0)) * a.width + c;
-            if (have == V) {
-                load_n<float, V>(at, x[k]);
+            const float *part = a.partial + (uint64_t(piece + p + k) * 2 + (p + k == 0)) * a.width;
+            if constexpr (ROWS != kThin) {
+                load_n<float, V>(part + load_at<V>(c, a.width), x[k]);
             } else {
 #pragma unroll
                 for (uint32_t j = 0; j < V; ++j)
-                    if (j < have) x[k][j] = at[j];
+                    if (c + j < a.width) x[k][j] = part[c + j];
             }
         }
 #pragma unroll
@@ -465,12 +485,12 @@ __global__ __launch_bounds__(kSumThreads) void run_kernel(Sums a)
 #pragma unroll
     for (uint32_t j = 0; j < V; ++j) parts[slice][j][lane] = sum[j];
     __syncthreads();
-    if (slice || !have) return;
+    if (slice || c >= a.width) return;
 #pragma unroll
     for (uint32_t s = 1; s < kRunSlices; ++s)
 #pragma unroll
         for (uint32_t j = 0; j < V; ++j) sum[j] += parts[s][j][lane];
-    finish_row<T, false>(a, key, c, have, sum);
+    finish_row<T, ROWS>(a, key, c, sum);
 }
 
 // ------------------------------------------------------------------ host
@@ -521,6 +541,14 @@ int forward(const tagc_embedding *l, hipStream_t s)
     return hip_ok(hipGetLastError());
 }
 
+template <uint32_t V, typename F>
+void by_rows(uint64_t width, F f)
+{
+    if (width < V) f(std::integral_constant<int, kThin>());
+    else if (width % V) f(std::integral_constant<int, kTail>());
+    else f(std::integral_constant<int, kWhole>());
+}
+
 template <typename T>
 int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t s)
 {
@@ -557,7 +585,7 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
         if (direct) {
             t.groups = a.rows * a.spans;
             ProfileScope prof("embed_sum", s);
-            direct_kernel<T><<<t.groups + zeros, kSumThreads, 0, s>>>(t, a);
+            by_rows<V>(l->width, [&](auto rows) { direct_kernel<T, decltype(rows)::value><<<t.groups + zeros, kSumThreads, 0, s>>>(t, a); });
             return hip_ok(hipGetLastError());
         }
         ProfileScope prof("embed_sort", s);
@@ -575,10 +603,11 @@ int backward(const tagc_embedding_grad *l, Places &w, bool enqueue, hipStream_t 
         ProfileScope prof("embed_sum", s);
         const uint32_t runs = (pieces - 1) * uint32_t((l->width + 64 * V - 1) / (64 * V));
         const auto go = [&](auto size) {
-            constexpr uint32_t P = decltype(size)::value;
-            if (l->width % V) sum_kernel<T, P, false><<<pieces * a.spans + zeros, kSumThreads, 0, s>>>(a);
-            else sum_kernel<T, P, true><<<pieces * a.spans + zeros, kSumThreads, 0, s>>>(a);
-            if (runs) run_kernel<T, P><<<runs, kSumThreads, 0, s>>>(a);
+            by_rows<V>(l->width, [&](auto rows) {
+                constexpr uint32_t P = decltype(size)::value, R = decltype(rows)::value;
+                sum_kernel<T, P, R><<<pieces * a.spans + zeros, kSumThreads, 0, s>>>(a);
+                if (runs) run_kernel<T, P, R><<<runs, kSumThreads, 0, s>>>(a);
+            });
         };
         if (piece == kShortPiece) go(std::integral_constant<uint32_t, kShortPiece>());
         else go(std::integral_constant<uint32_t, kLongPiece>());

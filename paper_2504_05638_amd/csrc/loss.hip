@@ -393,28 +393,31 @@ struct Slopes : Counted {
     template <int RM, int RN>
     __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
     {
-        in_rows(acc, strip, lane, m0, n0, m, part, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) {
-            const float2 by = row[r];
-            const uint32_t term = ids ? ids[uint64_t(r) << shift] - base : kNone;
+        in_rows(acc, strip, lane, m0, n0, m, part, [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) { finish(r, c, z); });
+    }
+    // of eight products of a row
+    __device__ inline __attribute__((always_inline)) void finish(uint32_t r, uint32_t c, float (&z)[8]) const
+    {
+        const float2 by = row[r];
+        const uint32_t term = ids ? ids[uint64_t(r) << shift] - base : kNone;
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) z[j] = c + j < n ? by.y * (__builtin_amdgcn_exp2f(z[j] * over2 - by.x) - (c + j == term ? 1.0f : 0.0f)) : 0.0f;
-            uint16_t *to = ds + r * ld + c;
-            if constexpr (sizeof(T) == 2) {
-                store_n<uint16_t, 8>(to, z);
-            } else {
-                u32x4 out[kParts];
+        for (uint32_t j = 0; j < 8; ++j) z[j] = c + j < n ? by.y * (__builtin_amdgcn_exp2f(z[j] * over2 - by.x) - (c + j == term ? 1.0f : 0.0f)) : 0.0f;
+        uint16_t *to = ds + r * ld + c;
+        if constexpr (sizeof(T) == 2) {
+            store_n<uint16_t, 8>(to, z);
+        } else {
+            u32x4 out[kParts];
 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) {
-                    uint32_t s[2][kParts];
-                    split(z[2 * j], s[0]);
-                    split(z[2 * j + 1], s[1]);
+            for (uint32_t j = 0; j < 4; ++j) {
+                uint32_t s[2][kParts];
+                split(z[2 * j], s[0]);
+                split(z[2 * j + 1], s[1]);
 #pragma unroll
-                    for (uint32_t q = 0; q < kParts; ++q) out[q][j] = __builtin_amdgcn_perm(s[1][q], s[0][q], 0x07060302);
-                }
-#pragma unroll
-                for (uint32_t q = 0; q < kParts; ++q) *reinterpret_cast<u32x4 *>(to + q * part) = out[q];
+                for (uint32_t q = 0; q < kParts; ++q) out[q][j] = __builtin_amdgcn_perm(s[1][q], s[0][q], 0x07060302);
             }
-        });
+#pragma unroll
+            for (uint32_t q = 0; q < kParts; ++q) *reinterpret_cast<u32x4 *>(to + q * part) = out[q];
+        }
     }
 };
 
@@ -427,6 +430,32 @@ __device__ inline void put_f32(float *to, uint32_t have, const float (&z)[8])
 #pragma unroll
         for (uint32_t j = 0; j < 8; ++j)
             if (j < have) to[j] = z[j];
+    }
+}
+
+// The sum of N neighbours over planes `step` apart, of which `have` are there: in the planes' order, four on their way at once.  (us, so / one after
+// the other: 16 planes of 26 rows of 863 6 / 20.)
+template <int N>
+__device__ inline void sum_planes(const float *from, uint64_t step, uint32_t planes, uint32_t have, float (&z)[N])
+{
+    constexpr uint32_t kAhead = 4;
+#pragma unroll
+    for (int j = 0; j < N; ++j) z[j] = 0;
+    for (uint32_t p = 0; p < planes; p += kAhead) {
+        float x[kAhead][N];
+        if (have >= N) {
+#pragma unroll
+            for (uint32_t k = 0; k < kAhead; ++k) load_n<float, N>(from + min(p + k, planes - 1) * step, x[k]);
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < kAhead; ++k)
+#pragma unroll
+                for (uint32_t j = 0; j < N; ++j) x[k][j] = (from + min(p + k, planes - 1) * step)[min(j, have - 1)];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (uint32_t j = 0; j < N; ++j) z[j] += p + k < planes ? x[k][j] : 0.0f;
     }
 }
 
@@ -646,22 +675,9 @@ __global__ __launch_bounds__(THREADS) void held_kernel(Held a)
     top = -INFINITY;
     sum = 0;
     for (uint32_t c = threadIdx.x * 4; c < V; c += THREADS * 4) {
-        float z[4] = {};
+        float z[4];
         const uint32_t have = min(4u, V - c);
-#pragma unroll 2
-        for (uint32_t p = 0; p < a.parts; ++p) {
-            const float *from = scores + p * next + c;
-            if (have == 4) {
-                float x[4];
-                load_n<float, 4>(from, x);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) z[j] += x[j];
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < 4; ++j)
-                    if (j < have) z[j] += from[j];
-            }
-        }
+        sum_planes<4>(scores + c, next, a.parts, have, z);
         float most = top;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
@@ -693,6 +709,19 @@ __global__ __launch_bounds__(THREADS) void held_kernel(Held a)
         a.loss[row] = all;
         if (a.saved) a.saved[uint64_t(row) * (1 + K)] = lse;
     }
+}
+
+// ds from parts of the scores' sums, as the product's end makes it of whole ones.
+template <typename T>
+__global__ __launch_bounds__(256) void slopes_kernel(Slopes<T> a, const float *planes, uint32_t parts)
+{
+    const uint32_t across = (a.n + 63) / 64 * 8;  // (zeros up to a whole slab of the next product)
+    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t r = uint32_t(i / across), c = uint32_t(i % across) * 8;
+    if (r >= *a.there) return;
+    float z[8];
+    sum_planes<8>(planes + uint64_t(r) * a.n + min(c, a.n - 1), uint64_t(a.m) * a.n, parts, c < a.n ? a.n - c : 1, z);
+    a.finish(r, c, z);
 }
 
 // ds where a row has a term, in its place: from the score that the forward pass saved, so that 1 - q's difference is taken before
@@ -732,20 +761,7 @@ __global__ __launch_bounds__(256) void place_kernel(const float *planes, uint32_
     const uint32_t r = uint32_t(i / across), c = uint32_t(i % across) * 8, have = min(8u, cols - c);
     if (r >= rows) return;
     float z[8] = {};
-    if (r < count)
-        for (uint32_t p = 0; p < n_planes; ++p) {
-            const float *from = planes + (uint64_t(p) * rows + r) * cols + c;
-            if (have == 8) {
-                float x[8];
-                load_n<float, 8>(from, x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] += x[j];
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < 8; ++j)
-                    if (j < have) z[j] += from[j];
-            }
-        }
+    if (r < count) sum_planes<8>(planes + uint64_t(r) * cols + c, uint64_t(rows) * cols, n_planes, have, z);
     T *to = dx + l.rows[r] * ld + c;
     if (have == 8) {
         store_n<T, 8>(to, z);
@@ -994,6 +1010,13 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     }
     const Operand ds = room(w, dtype, rows, piece);
     const Shape fx = shape_of(rows, D, piece, dtype, false), fw = shape_of(piece, D, rows, dtype, true);
+    // Scores' sums in parts, as planes, where that pays a launch more: few rows, a small vocabulary.  (us, so / by tiles that hold whole sums: float32 26
+    // rows of 863 over 1977 49 / 59, 490 of 1152 over 980 66 / 83, bfloat16 64 of 2048 over 16000 81 / 87.)
+    const auto in_parts = [&](uint64_t n) { return M && M <= kHeldRows && M * n <= kHeld ? shape_of(M, n, D, dtype, false) : Shape{}; };
+    uint64_t held = 0;
+    for (const uint64_t n : {piece < V ? piece : V, V % piece})
+        if (const Shape f = in_parts(n); n && f.splits > 1 && f.splits * M * n > held) held = f.splits * M * n;
+    float *scores = w.take<float>(held);
     float *planes = w.take<float>(l->dx ? fx.splits * rows * D : 0), *partial = w.take<float>(l->dw && fw.splits > 1 ? fw.splits * piece * D : 0);
     if (!enqueue) return TAGC_OK;
 
@@ -1008,7 +1031,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
         }
         if (M) {
             Slopes<T> a{};
-            const Shape f = shape_of(M, n, D, dtype, false, 1);
+            const Shape parts = in_parts(n), f = parts.splits > 1 ? parts : shape_of(M, n, D, dtype, false, 1);
             aim(a, x, q, M, n, D, f);
             a.there = list.count;
             a.ds = static_cast<uint16_t *>(const_cast<void *>(ds.p));
@@ -1021,7 +1044,16 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
             a.over2 = float(kLog2e / l->temperature);
             {
                 ProfileScope prof("loss_slopes", s);
-                launch<T, false, false>(a, f, s);
+                if (f.splits > 1) {
+                    Planes<Counted> b{};
+                    static_cast<Counted &>(b) = a;
+                    b.planes = scores;
+                    b.rows = uint32_t(M);
+                    launch<T, false, false>(b, f, s);
+                    slopes_kernel<T><<<uint32_t((M * (up(n, 64) / 8) + 255) / 256), 256, 0, s>>>(a, scores, f.splits);
+                } else {
+                    launch<T, false, false>(a, f, s);
+                }
             }
             if (l->terms > 1) {
                 ProfileScope prof("loss_terms", s);

@@ -180,6 +180,11 @@ def test_pieces_of_the_vocabulary_forward(shape, dtype):
     _check(shape, T[dtype], 0, 1.0, True, False, 1, 0, backward=dtype == "bf16")
 
 
+def test_few_rows_over_pieces_of_the_vocabulary():
+    """Each piece's scores as parts of sums, those of the last piece cut in their own way."""
+    _check((60, 4096, 26000), torch.float32, 0, 1.0, True, True, 41, 0, repeat=True)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_large_tiles(dtype):
     print("[case] large tiles", dtype, flush=True)

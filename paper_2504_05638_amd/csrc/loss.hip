@@ -1009,7 +1009,8 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
         if (sizeof(T) == 2) wq.part = 0;
     }
     const Operand ds = room(w, dtype, rows, piece);
-    const Shape fx = shape_of(rows, D, piece, dtype, false), fw = shape_of(piece, D, rows, dtype, true);
+    // (us, dx of float32 64 rows of 768 over 50257 in up to 64 parts / 16: the whole call 264 / 295)
+    const Shape fx = shape_of(rows, D, piece, dtype, false, 64), fw = shape_of(piece, D, rows, dtype, true);
     // Scores' sums in parts, as planes, where that pays a launch more: few rows, a small vocabulary.  (us, so / by tiles that hold whole sums: float32 26
     // rows of 863 over 1977 49 / 59, 490 of 1152 over 980 66 / 83, bfloat16 64 of 2048 over 16000 81 / 87.)
     const auto in_parts = [&](uint64_t n) { return M && M <= kHeldRows && M * n <= kHeld ? shape_of(M, n, D, dtype, false) : Shape{}; };

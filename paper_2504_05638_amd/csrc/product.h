@@ -878,7 +878,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void few_kernel(E a)
 
 // ------------------------------------------------------------------ host
 
-// How a product is cut (into at most `most` parts of the sum, 16 or 1): tiles of `rows` by 256 (256 rows) or 128, and the parts of the sum that make up for few tiles.
+// How a product is cut (into at most `most` parts of the sum: 16, 1, or 64 of sums as long as a vocabulary): tiles of `rows` by 256 (256 rows) or 128, and the parts of the sum that make up for few tiles.
 struct Shape {
     uint32_t rows, tiles_m, tiles_n, slabs, splits;
     bool lone;  // bfloat16 tiles of 128 that each have a compute unit to themselves: lone_kernel

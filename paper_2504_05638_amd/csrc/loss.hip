@@ -1012,8 +1012,13 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     // (us, dx of float32 64 rows of 768 over 50257 in up to 64 parts / 16: the whole call 264 / 295)
     const Shape fx = shape_of(rows, D, piece, dtype, false, 64), fw = shape_of(piece, D, rows, dtype, true);
     // Scores' sums in parts, as planes, where that pays a launch more: few rows, a small vocabulary.  (us, so / by tiles that hold whole sums: float32 26
-    // rows of 863 over 1977 49 / 59, 490 of 1152 over 980 66 / 83, bfloat16 64 of 2048 over 16000 81 / 87.)
-    const auto in_parts = [&](uint64_t n) { return M && M <= kHeldRows && M * n <= kHeld ? shape_of(M, n, D, dtype, false) : Shape{}; };
+    // rows of 863 over 1977 49 / 59, 490 of 1152 over 980 66 / 83, bfloat16 64 of 2048 over 16000, 125 thin tiles, 81 / 87, 16 of 4096 over
+    // 32000, 250 of them, 220 / 214.)
+    const auto in_parts = [&](uint64_t n) {
+        if (!M || M > kHeldRows || M * n > kHeld) return Shape{};
+        const Shape f = shape_of(M, n, D, dtype, false);
+        return sizeof(T) == 2 && 2 * f.tiles_m * f.tiles_n > uint32_t(device_cu_count()) ? Shape{} : f;
+    };
     uint64_t held = 0;
     for (const uint64_t n : {piece < V ? piece : V, V % piece})
         if (const Shape f = in_parts(n); n && f.splits > 1 && f.splits * M * n > held) held = f.splits * M * n;

@@ -262,7 +262,7 @@ int tagc_norm_backward_workspace(const tagc_norm_grad *n, uint64_t *bytes);
 /*
  * h = (x - mean) r, u = dy w: dx = r (u - mean u - h mean(u h)) + residual (without mean u with TAGC_NORM_RMS);
  * dw (+)= the sum of dy h over the rows, db (+)= that of dy.  Sums in float32, in an order that depends on nothing but
- * the sizes and the number of compute units.
+ * the sizes, the number of compute units and whether dx is written over x or dy.
  */
 int tagc_norm_backward(const tagc_norm_grad *n, void *workspace, void *stream);
 

@@ -208,7 +208,77 @@ struct NormGrad {
     uint64_t ldx, lddy, ldr, lddx;
     uint32_t rows, width;
     float over;    // 1 / width
+    uint32_t groups;  // workgroups that take rows; those behind them take columns, for which `sums` is NULL
+    void *dw, *db;    // theirs
+    uint32_t accumulate;
 };
+
+// Few rows' dw and db without a launch to join them: a workgroup takes 8 * V columns of all rows, eight lanes to a row, and adds up what its
+// eighths of waves and its waves have, in their order.  It reads x and dy once more, from the caches.
+template <typename T, int THREADS>
+__device__ inline void norm_columns(const NormGrad &a)
+{
+    constexpr uint32_t V = 16 / sizeof(T), kSlices = THREADS / 8, kAhead = 4, W = THREADS / 64;
+    __shared__ float parts[2][W][8 * V];
+    const uint32_t lane = threadIdx.x % 8, slice = threadIdx.x / 8, c = (blockIdx.x - a.groups) * 8 * V + lane * V;
+    // (as Part: of a row's last piece that is not whole the row's last 16 bytes)
+    const bool thin = a.width < V;
+    const uint32_t at = thin ? 0 : min(c, a.width - V);
+    const T *x = static_cast<const T *>(a.x) + at, *dy = static_cast<const T *>(a.dy) + at;
+    float dw[V] = {}, db[V] = {};
+    for (uint32_t first = slice; first < a.rows; first += kSlices * kAhead) {
+        float px[kAhead][V], py[kAhead][V];
+        float2 stats[kAhead];
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k) {
+            const uint64_t row = min(first + k * kSlices, a.rows - 1);
+            stats[k] = *reinterpret_cast<const float2 *>(a.stats + 2 * row);
+            if (!thin) {
+                load_n<T, V>(x + row * a.ldx, px[k]);
+                load_n<T, V>(dy + row * a.lddy, py[k]);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < V; ++j) {
+                    px[k][j] = widen(x[row * a.ldx + min(j, a.width - 1)]);
+                    py[k][j] = widen(dy[row * a.lddy + min(j, a.width - 1)]);
+                }
+            }
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (uint32_t j = 0; j < V; ++j) {
+                const float g = first + k * kSlices < a.rows ? py[k][j] : 0.0f;
+                // (a row that is not there again, whose numbers may be infinite)
+                dw[j] += first + k * kSlices < a.rows ? g * ((px[k][j] - stats[k].x) * stats[k].y) : 0.0f;
+                db[j] += g;
+            }
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j)
+#pragma unroll
+        for (int d = 8; d < 64; d *= 2) {
+            dw[j] += __shfl_xor(dw[j], d, 64);
+            db[j] += __shfl_xor(db[j], d, 64);
+        }
+    if (threadIdx.x % 64 < 8)
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) {
+            parts[0][threadIdx.x / 64][lane * V + j] = dw[j];
+            parts[1][threadIdx.x / 64][lane * V + j] = db[j];
+        }
+    __syncthreads();
+    if (threadIdx.x >= 16 * V) return;
+    const uint32_t which = threadIdx.x / (8 * V), own = threadIdx.x % (8 * V);
+    float sum = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < W; ++w) sum += parts[which][w][own];
+    T *to = static_cast<T *>(which ? a.db : a.dw);
+    // (lanes behind the row's end, and elements of its last piece that are another lane's, are not stored)
+    const uint32_t begin = (blockIdx.x - a.groups) * 8 * V + own / V * V, place = (thin ? 0 : min(begin, a.width - V)) + own % V;
+    if (!to || begin >= a.width || place < begin || place >= a.width) return;
+    to[place] = narrow<T>(a.accumulate ? sum + widen(to[place]) : sum);
+}
 
 // A workgroup takes every gridDim.x-th row (group of rows), and keeps their part of dw and db in registers.  What lies between the sums
 // and dx is computed twice from the row as it lies: held, it would take as many registers as all the rest.
@@ -217,6 +287,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void norm_grad_kernel(NormGrad
 {
     typedef Part<T, LANES, STEPS> P;
     constexpr uint32_t kThreads = kNormThreads<LANES>, kRows = kThreads / LANES;
+    if (blockIdx.x >= a.groups) return norm_columns<T, kThreads>(a);
     __shared__ float room[2 * 2 * (LANES / 64)];
     uint32_t turn = 0;
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy), *res = static_cast<const T *>(a.residual);
@@ -243,7 +314,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void norm_grad_kernel(NormGrad
         if (res && !kNarrow) ar.load(res + row * a.ldr, a.width);
         next_stats = *reinterpret_cast<const float2 *>(a.stats + 2 * row);
     };
-    const uint64_t step = uint64_t(gridDim.x) * kRows;
+    const uint64_t step = uint64_t(a.groups) * kRows;
     uint64_t row = uint64_t(blockIdx.x) * kRows + threadIdx.x / LANES;
     if (kAhead && row < a.rows) fetch(row);
     for (; row < a.rows; row += step) {
@@ -387,6 +458,10 @@ uint32_t grad_groups(uint64_t rows, uint64_t width)
     return uint32_t(all < most ? all : most);
 }
 
+// Rows up to which dw and db are a part of the one launch.  (us, so / joined by a second one: bfloat16 64 rows of 4096 4.7 / 9.0, 256 8.5 / 12.9, 512
+// 13.0 / 13.7, 512 of 16384 24 / 34, of 512 8.2 / 7.0; float32 512 of 768 6.5 / 10.1, of 8192 23 / 31.)
+constexpr uint32_t kDirect = 512;
+
 int check(uint64_t rows, uint64_t width, uint32_t dtype, uint32_t kind)
 {
     if (dtype > TAGC_BF16 || kind > TAGC_NORM_RMS) return TAGC_EINVAL;
@@ -426,7 +501,8 @@ int check(const tagc_norm_grad *n)
     if ((!one(n->x, n->ldx) && meet(dx, x)) || (!one(n->dy, n->lddy) && meet(dx, dy)) || (!one(n->residual, n->ldr) && meet(dx, res)) || meet(dx, w) ||
         meet(dx, stats) || meet(dx, dw) || meet(dx, db) || meet(dw, db))
         return TAGC_EINVAL;
-    // (dw and db are written when the rows have been read; what they are added to is their own)
+    for (const Rows &in : {x, dy, res, w, stats})
+        if (meet(dw, in) || meet(db, in)) return TAGC_EINVAL;
     return TAGC_OK;
 }
 
@@ -454,18 +530,21 @@ template <typename T>
 int backward(const tagc_norm_grad *n, Places &w, bool enqueue, hipStream_t s)
 {
     if (!n->width) return TAGC_OK;
-    const bool sums = n->dw || n->db;
+    // (columns are read while rows' dx is written)
+    const bool direct = n->rows && n->rows <= kDirect && !(n->dx && (n->dx == n->x || n->dx == n->dy)), sums = (n->dw || n->db) && !direct, columns = (n->dw || n->db) && direct;
     const uint32_t groups = grad_groups(n->rows, n->width);
     float *room = sums ? w.take<float>(uint64_t(groups) * 2 * n->width) : nullptr;
     if (!enqueue) return TAGC_OK;
-    if (groups && (sums || n->dx)) {
+    if (groups && (sums || columns || n->dx)) {
+        constexpr uint32_t kColumns = 8 * 16 / sizeof(T);
         const NormGrad a{n->x, n->w, n->dy, n->residual, n->stats, n->dx, room, n->ldx, n->lddy, n->ldr, n->lddx, uint32_t(n->rows), uint32_t(n->width),
-                         float(1.0 / double(n->width))};
+                         float(1.0 / double(n->width)), sums || n->dx ? groups : 0, n->dw, n->db, n->accumulate};
+        const uint32_t grid = a.groups + (columns ? uint32_t((n->width + kColumns - 1) / kColumns) : 0);
         ProfileScope prof("norm_grad", s);
         by_width<T>(n->width, [&](auto lanes, auto steps) {
             constexpr int L = decltype(lanes)::value;
-            if (n->kind == TAGC_NORM_LAYER) norm_grad_kernel<T, L, decltype(steps)::value, true><<<groups, kNormThreads<L>, 0, s>>>(a);
-            else norm_grad_kernel<T, L, decltype(steps)::value, false><<<groups, kNormThreads<L>, 0, s>>>(a);
+            if (n->kind == TAGC_NORM_LAYER) norm_grad_kernel<T, L, decltype(steps)::value, true><<<grid, kNormThreads<L>, 0, s>>>(a);
+            else norm_grad_kernel<T, L, decltype(steps)::value, false><<<grid, kNormThreads<L>, 0, s>>>(a);
         });
     }
     if (sums) {

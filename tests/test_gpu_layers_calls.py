@@ -248,7 +248,7 @@ def test_what_a_workspace_holds_does_not_matter(dtype, rows, monkeypatch):
         return out + [table, train.norm_backward(dy, x, gain, stats, dw=dgain, db=dshift), dgain, dshift]
 
     want = run(0)
-    assert len(made) >= 5 and all(torch.isfinite(t).all() for t in want)
+    assert len(made) >= 4 and all(torch.isfinite(t).all() for t in want)
     for fill in (255, 127):
         for k, (a, b) in enumerate(zip(run(fill), want)):
             assert torch.equal(a, b), k

@@ -173,6 +173,32 @@ def test_not_finite_rows_stay_where_they_are():
         assert torch.isfinite(dx[keep]).all() and torch.isnan(dx[[2, 7]]).any(1).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_few_rows_and_more(kind, dtype):
+    """On both sides of the number of rows up to which dw and db are made beside dx."""
+    for i, (M, D) in enumerate([(511, 260), (512, 67), (513, 260), (512, 1031), (512, 5), (512, 8200), (200, 16384)]):
+        print("[case] few rows", kind, dtype, M, D, flush=True)
+        _backward((M, D), T[dtype], kind, i % 3 > 0, i % 2 == 0, i % 4 == 1, 10 * i, i % 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_rows_in_place(dtype):
+    """dx over dy or x, whose dw and db are made of what was there before."""
+    from paper_2504_05638_amd.train import norm, norm_backward
+    M, D = 300, 700
+    x, dy, w = _randn((M, D), 1, T[dtype], 2.0), _randn((M, D), 2, T[dtype]), _randn((1, D), 3, T[dtype])[0]
+    _, stats = norm(x, w, save=True)
+    want = norm_backward(dy, x, w, stats)
+    g, h = dy.double(), (x.double() - stats[:, :1].double()) * stats[:, 1:].double()
+    for place in (None, "dy", "x"):
+        a, b, dw, db = dy.clone(), x.clone(), torch.empty_like(w), torch.empty_like(w)
+        dx = norm_backward(a, b, w, stats, dw=dw, db=db, dx={"dy": a, "x": b}.get(place))
+        assert torch.equal(dx, want), place
+        _near(dw, (g * h).sum(0), (M + 43) * E * (g * h).abs().sum(0), T[dtype], ("dw", place))
+        _near(db, g.sum(0), (M + 40) * E * g.abs().sum(0), T[dtype], ("db", place))
+
+
 def test_in_place_and_shapes():
     from paper_2504_05638_amd.train import norm, norm_backward
     x, w = _randn((30, 700), 1, torch.bfloat16), _randn((1, 700), 2, torch.bfloat16)[0]

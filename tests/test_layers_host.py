@@ -56,14 +56,24 @@ def test_norm_backward_refuses(bad, code):
 
 
 def test_norm_workspace():
-    need = B.tagc_norm_backward_workspace(_norm_grad())
-    assert need >= 100 // 4 * 2 * 64 * 4
+    need = B.tagc_norm_backward_workspace(_norm_grad(rows=1000))
+    assert need >= 1000 // 4 * 2 * 64 * 4
     assert B.tagc_norm_backward_workspace(_norm_grad(dw=None, db=None)) == 0
     assert B.tagc_norm_backward_workspace(_norm_grad(rows=0)) == 0
     for place in (X, Y, Z):     # dx in the place of what it is made of
-        assert B.tagc_norm_backward_workspace(_norm_grad(dx=place)) == need
-    assert _code(B.tagc_norm_backward, _norm_grad(), None) == -1
-    assert _code(B.tagc_norm_backward, _norm_grad(), A + 16) == -1
+        assert B.tagc_norm_backward_workspace(_norm_grad(rows=1000, dx=place)) == need
+    assert _code(B.tagc_norm_backward, _norm_grad(rows=1000), None) == -1
+    assert _code(B.tagc_norm_backward, _norm_grad(rows=1000), A + 16) == -1
+    # few rows' dw and db are made beside dx, unless that is written over what they are made of
+    assert B.tagc_norm_backward_workspace(_norm_grad()) == B.tagc_norm_backward_workspace(_norm_grad(dx=Z)) == 0
+    assert B.tagc_norm_backward_workspace(_norm_grad(dx=X)) == B.tagc_norm_backward_workspace(_norm_grad(dx=Y)) > 0
+
+
+@pytest.mark.parametrize("of", ["dw", "db"])
+@pytest.mark.parametrize("place", [X, Y, Z, W, S])
+@pytest.mark.parametrize("rows", [100, 1000])
+def test_norm_gradients_over_operands_are_refused(of, place, rows):
+    assert _code(B.tagc_norm_backward_workspace, _norm_grad(rows=rows, **{of: place})) == -1
 
 
 def _embed(**kw):

@@ -26,6 +26,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLeas
 // 128 rows 72 / 83, 512 rows 144 / 133; 333 of 777 over 1001 21 / 27, in float32 24 / 49; 4096 rows of 256 over 2048 35 / 28.)
 constexpr uint64_t kHeldRows = 1024, kHeld = 1u << 23;
 
+// Elements up to which a vocabulary that is one piece is laid out in the launch that lays out x.  (us, backward, so / by a launch of its own: float32
+// 26 rows of 863 over 1977 49 / 52, bfloat16 1200 of 777 over 8001 91 / 95; float32 1024 of 1024 over 32000 1065 / 1068.)
+constexpr uint64_t kAtOnce = 1u << 26;
+
 // What a piece of the vocabulary may hold (ds, operands laid out, the waves' sums), and its fewest rows.  (us, a quarter / a half / one GiB, backward in
 // bfloat16: 8192 rows of 768 over 50257 2613 / 2317 / 2170, of 4096 over 32000 5314 / 5251 / 5256, over 128256 21161 / 20707 / 20662: dx of narrow
 // rows has few tiles, and more parts the longer its sums are; float32, a quarter / a half: 1024 of 768 over 50257 1202 / 1235, 2048 of 4096 over 32000
@@ -170,11 +174,16 @@ __device__ inline void lay_piece(const Gather &a, uint32_t from, uint32_t r, uin
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(Gather a)
+__device__ inline void lay_all(const Gather &a, uint32_t group)
 {
-    const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+    const uint64_t i = uint64_t(group) * 256 + threadIdx.x;
     const uint32_t r = uint32_t(i / a.across);
     if (r < a.n) lay_piece<T>(a, r, r, uint32_t(i % a.across) * 8);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void gather_kernel(Gather a)
+{
+    lay_all<T>(a, blockIdx.x);
 }
 
 // The rows that have a term, one behind the other: x's, their terms' ids, and what the backward pass needs of each.
@@ -182,7 +191,9 @@ struct Lay {
     Terms terms;
     List list;
     Gather x;
-    uint32_t groups;   // workgroups for x; the rest is for ids
+    uint32_t groups;   // workgroups for x; those behind them are for ids
+    Gather w;          // a vocabulary that is one piece
+    uint32_t w_from;   // workgroups from there on are its
     uint32_t *ids;     // [rows][2^shift]: a row's terms, kNone for none
     uint32_t shift;
     const float *saved, *dloss;
@@ -197,6 +208,7 @@ template <typename T, bool SCAN>
 __global__ __launch_bounds__(256) void lay_kernel(Lay a)
 {
     __shared__ uint32_t rows[SCAN ? kScanRows : 1], room[4];
+    if (blockIdx.x >= a.w_from) return lay_all<T>(a.w, blockIdx.x - a.w_from);
     uint32_t count;
     if constexpr (SCAN) {
         uint32_t bits = 0;
@@ -875,17 +887,19 @@ struct Listed {
 };
 
 template <typename T>
-void launch_rows(const Terms &t, const Listed &l, const Gather &x, const Rowwise &r, hipStream_t s)
+void launch_rows(const Terms &t, const Listed &l, const Gather &x, const Gather &w, const Rowwise &r, hipStream_t s)
 {
     ProfileScope prof("loss_rows", s);
     if (t.logits && t.rows) terms_kernel<<<(t.rows + 3) / 4, 256, 0, s>>>(t);
     const uint64_t groups = (uint64_t(x.n) * x.across + 255) / 256, more = ((uint64_t(t.rows) << l.shift) + 255) / 256;
-    const Lay a{t, l.list, x, uint32_t(groups), l.ids, l.shift, r.saved, r.dloss, r.row, r.step};
-    if (t.rows <= kScanRows) {
-        lay_kernel<T, true><<<uint32_t(groups + more + 1), 256, 0, s>>>(a);
+    const bool scan = t.rows <= kScanRows;
+    const uint32_t w_from = uint32_t(groups + more + scan), w_groups = w.n ? uint32_t((uint64_t(w.n) * w.across + 255) / 256) : 0;
+    const Lay a{t, l.list, x, uint32_t(groups), w, w_from, l.ids, l.shift, r.saved, r.dloss, r.row, r.step};
+    if (scan) {
+        lay_kernel<T, true><<<w_from + w_groups, 256, 0, s>>>(a);
     } else {
         list_kernel<<<1, kListThreads, 0, s>>>(t, l.list);
-        lay_kernel<T, false><<<uint32_t(groups + more), 256, 0, s>>>(a);
+        lay_kernel<T, false><<<w_from + w_groups, 256, 0, s>>>(a);
     }
 }
 
@@ -955,13 +969,14 @@ int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
     float *scores = w.take<float>(M * l->terms);
     if (!enqueue) return TAGC_OK;
 
-    launch_rows<T>(terms, listed, gather<T>(l->x, l->ldx, M, D, x), Rowwise{}, s);
+    const bool at_once = ops.lay && piece >= V && V * D < kAtOnce;
+    launch_rows<T>(terms, listed, gather<T>(l->x, l->ldx, M, D, x), at_once ? gather<T>(l->w, l->ldw, V, D, wq) : Gather{}, Rowwise{}, s);
     for (uint64_t v = 0; v < V; v += piece) {
         const uint64_t n = V - v < piece ? V - v : piece;
         const T *from = static_cast<const T *>(l->w) + v * l->ldw;
         Operand q{from, l->ldw, 0};
         if (ops.lay) {
-            launch_gather<T>(gather<T>(from, l->ldw, n, D, wq), s);
+            if (!at_once) launch_gather<T>(gather<T>(from, l->ldw, n, D, wq), s);
             q = wq;
         }
         Scores a{};
@@ -1026,13 +1041,14 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     float *planes = w.take<float>(l->dx ? fx.splits * rows * D : 0), *partial = w.take<float>(l->dw && fw.splits > 1 ? fw.splits * piece * D : 0);
     if (!enqueue) return TAGC_OK;
 
-    launch_rows<T>(terms, listed, gather<T>(l->x, l->ldx, M, D, x), by, s);
+    const bool at_once = ops.lay && M && piece >= V && V * D < kAtOnce;  // (without rows there need be no w)
+    launch_rows<T>(terms, listed, gather<T>(l->x, l->ldx, M, D, x), at_once ? gather<T>(l->w, l->ldw, V, D, wq) : Gather{}, by, s);
     for (uint64_t v = 0; v < V; v += piece) {
         const uint64_t n = V - v < piece ? V - v : piece;
         const T *from = static_cast<const T *>(l->w) + v * l->ldw;
         Operand q{from, l->ldw, 0};
-        if (ops.lay && M) {  // (without rows there need be no w)
-            launch_gather<T>(gather<T>(from, l->ldw, n, D, wq), s);
+        if (ops.lay && M) {
+            if (!at_once) launch_gather<T>(gather<T>(from, l->ldw, n, D, wq), s);
             q = wq;
         }
         if (M) {

@@ -28,7 +28,7 @@ namespace {
 constexpr uint32_t kChunk = 4096, kSortThreads = 1024, kSlots = kChunk / kSortThreads, kSortWaves = kSortThreads / 64;
 constexpr uint32_t kMerge = 16;        // sorted lists merged at once
 // Sorted tokens summed by a workgroup: many leave fewer partial sums behind, few make more workgroups of a short batch.  (us, eight / 16 /
-// 32: 16384 tokens into 32000 by 4096 in bfloat16 133 / 126 / 123, 1023 into 50257 by 768 in float32 38 / 41 / 45.)
+// 32: 16384 tokens into 32000 by 4096 in bfloat16 111 / 101 / 96, 65536 into 50257 by 768 101 / 93 / 88, 1023 there in float32 41 / 44 / 48.)
 constexpr uint32_t kShortPiece = 8, kLongPiece = 32, kShort = 8192;
 constexpr uint32_t kSumThreads = 256, kRunSlices = kSumThreads / 64;
 constexpr uint32_t kZeroRows = 64;     // most table rows that a workgroup looks after for want of tokens
@@ -368,8 +368,8 @@ __global__ __launch_bounds__(kSumThreads) void direct_kernel(Tokens a, Sums b)
     if (c < a.width) finish_row<T, ROWS>(b, key, c, sum);
 }
 
-// A workgroup sums a piece of sorted tokens, 256 * V columns of them; workgroups behind those write zeros.  Bound by the bytes of dy, of the rows that are finished and of the partial sums: 16384
-// tokens of 4096 in bfloat16 40 us, 4.9 TB/s.
+// A workgroup sums a piece of sorted tokens, 256 * V columns of them; workgroups behind those write zeros.  Bound by the bytes of dy, of the rows that
+// are finished and of the partial sums: 16384 tokens of 4096 in bfloat16 35 us, 5.1 TB/s.
 template <typename T, uint32_t PIECE, int ROWS>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
 {
@@ -414,8 +414,8 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
                 if (j < a.width) to[j] = sum[j];
         }
     };
-    // rows come four at a time, past the caches' order, which the table's rows are left to (61 -> 40 us), the next ones while these are added (two, eight: 1 % slower, the same; all at once, which leaves fewer workgroups
-    // room, half as long again)
+    // rows come four at a time, past the caches' order, which the table's rows are left to (16384 tokens of 4096: 40 us, 61 through the caches), the
+    // next ones while these are added (two, eight: 1 % slower, the same; all at once, which leaves fewer workgroups room, half as long again)
     constexpr uint32_t kAhead = 4;
     Lane<T, V> x[2][kAhead];
     auto fetch = [&](uint32_t first, Lane<T, V>(&to)[kAhead]) __attribute__((always_inline)) {

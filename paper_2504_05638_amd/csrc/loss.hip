@@ -537,6 +537,22 @@ struct Weights : Counted {
     }
 };
 
+// dx of a vocabulary that is one piece, whole sums: in the rows' own places at once.  (us, backward, so / by way of float32: bfloat16 4096 rows of
+// 4096 over 32000 2618 / 2638, 8192 of 2048 over 2000 231 / 250.)
+template <typename T>
+struct Placed : Counted {
+    static constexpr bool kCounted = true;
+    T *dx;
+    uint64_t ld;
+    const uint32_t *list;
+    template <int RM, int RN>
+    __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
+    {
+        in_rows(acc, strip, lane, m0, n0, m, n,
+                [&](uint32_t r, uint32_t c, float(&z)[8]) __attribute__((always_inline)) { put_dw<T>(dx + list[r] * ld + c, n - c, 0, z); });
+    }
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void weights_join_kernel(Weights<T> a)
 {
@@ -784,6 +800,19 @@ __global__ __launch_bounds__(256) void place_kernel(const float *planes, uint32_
     }
 }
 
+// Zeros in dx where a row has no term, a wave to a row.
+template <typename T>
+__global__ __launch_bounds__(256) void blank_kernel(List l, uint32_t rows, uint32_t cols, T *dx, uint64_t ld)
+{
+    const uint32_t r = blockIdx.x * 4 + threadIdx.x / 64;
+    if (r >= rows || r < *l.count) return;
+    T *to = dx + l.rows[r] * ld;
+    for (uint32_t c = threadIdx.x % 64 * 8; c < cols; c += 64 * 8) {
+        float z[8] = {};
+        put_dw<T>(to + c, cols - c, 0, z);
+    }
+}
+
 // ------------------------------------------------------------------ host
 
 int check_sizes(uint64_t rows, uint64_t in, uint64_t vocab, uint32_t terms, uint32_t dtype, uint32_t id_type, double temperature, const float *logits)
@@ -1026,6 +1055,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     const Operand ds = room(w, dtype, rows, piece);
     // (us, dx of float32 64 rows of 768 over 50257 in up to 64 parts / 16: the whole call 264 / 295)
     const Shape fx = shape_of(rows, D, piece, dtype, false, 64), fw = shape_of(piece, D, rows, dtype, true);
+    const bool placed = piece >= V && fx.splits == 1;
     // Scores' sums in parts, as planes, where that pays a launch more: few rows, a small vocabulary.  (us, so / by tiles that hold whole sums: float32 26
     // rows of 863 over 1977 49 / 59, 490 of 1152 over 980 66 / 83, bfloat16 64 of 2048 over 16000, 125 thin tiles, 81 / 87, 16 of 4096 over
     // 32000, 250 of them, 220 / 214.)
@@ -1038,7 +1068,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     for (const uint64_t n : {piece < V ? piece : V, V % piece})
         if (const Shape f = in_parts(n); n && f.splits > 1 && f.splits * M * n > held) held = f.splits * M * n;
     float *scores = w.take<float>(held);
-    float *planes = w.take<float>(l->dx ? fx.splits * rows * D : 0), *partial = w.take<float>(l->dw && fw.splits > 1 ? fw.splits * piece * D : 0);
+    float *planes = w.take<float>(l->dx && !placed ? fx.splits * rows * D : 0), *partial = w.take<float>(l->dw && fw.splits > 1 ? fw.splits * piece * D : 0);
     if (!enqueue) return TAGC_OK;
 
     const bool at_once = ops.lay && M && piece >= V && V * D < kAtOnce;  // (without rows there need be no w)
@@ -1084,7 +1114,16 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
         }
         Operand p = ds;
         if (sizeof(T) == 2) p.part = 0;
-        if (l->dx && M) {
+        if (l->dx && M && placed) {
+            Placed<T> a{};
+            aim(a, p, q, M, D, n, fx);
+            a.there = list.count;
+            a.dx = static_cast<T *>(l->dx);
+            a.ld = l->lddx;
+            a.list = list.rows;
+            ProfileScope prof("loss_dx", s);
+            launch<T, false, true>(a, fx, s);
+        } else if (l->dx && M) {
             Planes<Counted> a{};
             aim(a, p, q, M, D, n, fx);
             const uint64_t slab = dtype == TAGC_F32 ? kSlab3 : kSlab;
@@ -1120,7 +1159,8 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     }
     if (l->dx && M) {
         ProfileScope prof("loss_place", s);
-        place_kernel<T><<<uint32_t((M * ((D + 7) / 8) + 255) / 256), 256, 0, s>>>(planes, fx.splits, list, uint32_t(M), uint32_t(D), static_cast<T *>(l->dx), l->lddx);
+        if (placed) blank_kernel<T><<<uint32_t((M + 3) / 4), 256, 0, s>>>(list, uint32_t(M), uint32_t(D), static_cast<T *>(l->dx), l->lddx);
+        else place_kernel<T><<<uint32_t((M * ((D + 7) / 8) + 255) / 256), 256, 0, s>>>(planes, fx.splits, list, uint32_t(M), uint32_t(D), static_cast<T *>(l->dx), l->lddx);
     }
     return hip_ok(hipGetLastError());
 }

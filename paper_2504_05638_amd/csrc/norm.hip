@@ -450,7 +450,7 @@ uint32_t rows_at_once(uint64_t width) { return width <= 64 * 16 ? 4 : 1; }
 
 // Workgroups of the backward pass.  The fewer there are, the fewer sums are left to be joined, and a row on its way behind the one in work keeps
 // the memory busy.  (us, one / two / three / four to a compute unit: bfloat16 8192 by 4096 54 / 57 / 60 / 62, 4096 by 8192 66 / 66 / 76 / 80,
-// 16384 by 2048 64 / 55 / 57 / 61, 32768 by 512 36 / 30 / 32 / 33, 512 by 4096 14 / 20 / 20 / 20; float32 8192 by 768 32 / 27 / 32 / 32, 2048 by
+// 16384 by 2048 64 / 55 / 57 / 61, 32768 by 512 36 / 30 / 32 / 33; float32 8192 by 768 32 / 27 / 32 / 32, 2048 by
 // 8192 67 / 77 / 87 / 99.)
 uint32_t grad_groups(uint64_t rows, uint64_t width)
 {

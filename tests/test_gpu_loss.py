@@ -192,6 +192,22 @@ def test_large_tiles(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(3001, 1031, 901), (2100, 2056, 300), (70, 41, 300)], ids=str)
+def test_dx_of_a_small_vocabulary(shape, dtype):
+    """Whole sums of tiles, rows without terms among the others; into a view, whose surroundings stay."""
+    from paper_2504_05638_amd.train import cross_entropy, cross_entropy_backward
+    _check(shape, T[dtype], 0, 1.0, True, False, 51, 1)
+    M, D, V = shape
+    ids = _terms(M, V, 1, 52, True)[0][:, 0].contiguous()
+    x, w, one = _randn((M, D), 53, T[dtype]), _randn((V, D), 54, T[dtype], D ** -0.5), torch.ones((), device="cuda")
+    _, saved = cross_entropy(x, w, ids, save=True)
+    want = cross_entropy_backward(one, x, w, ids, saved)
+    room = torch.full((M, D + 9), 7.0, device="cuda", dtype=T[dtype])
+    cross_entropy_backward(one, x, w, ids, saved, dx=room[:, 5:5 + D])
+    assert torch.equal(room[:, 5:5 + D], want) and (room[:, :5] == 7).all() and (room[:, 5 + D:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_without_any_term(dtype):
     """No row counts: losses 0, dx 0, dw 0 or as it was."""
     from paper_2504_05638_amd.train import cross_entropy, cross_entropy_backward

@@ -1070,13 +1070,13 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
     // rows of 863 over 1977 49 / 59, 490 of 1152 over 980 66 / 83, bfloat16 64 of 2048 over 16000, 125 thin tiles, 81 / 87, 16 of 4096 over
     // 32000, 250 of them, 220 / 214.)
     const auto in_parts = [&](uint64_t n) {
-        if (!M || M > kHeldRows || M * n > kHeld) return Shape{};
+        if (!M || !n || M > kHeldRows || M * n > kHeld) return Shape{};
         const Shape f = shape_of(M, n, D, dtype, false);
         return sizeof(T) == 2 && 2 * f.tiles_m * f.tiles_n > uint32_t(device_cu_count()) ? Shape{} : f;
     };
     uint64_t held = 0;
     for (const uint64_t n : {piece < V ? piece : V, V % piece})
-        if (const Shape f = in_parts(n); n && f.splits > 1 && f.splits * M * n > held) held = f.splits * M * n;
+        if (const Shape f = in_parts(n); f.splits > 1 && f.splits * M * n > held) held = f.splits * M * n;
     float *scores = w.take<float>(held);
     float *planes = w.take<float>(l->dx && !placed ? fx.splits * rows * D : 0), *partial = w.take<float>(l->dw && fw.splits > 1 ? fw.splits * piece * D : 0);
     if (!enqueue) return TAGC_OK;

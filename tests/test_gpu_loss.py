@@ -192,6 +192,13 @@ def test_large_tiles(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(16, 64, 8192), (64, 200, 4096), (1000, 72, 4096)], ids=str)
+def test_a_vocabulary_of_whole_rounds(shape, dtype):
+    for K in (0, 7):
+        _check(shape, T[dtype], K, 1.0, True, False, 81, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("shape", [(3001, 1031, 901), (2100, 2056, 300), (70, 41, 300)], ids=str)
 def test_dx_of_a_small_vocabulary(shape, dtype):
     """Whole sums of tiles, rows without terms among the others; into a view, whose surroundings stay."""

@@ -150,6 +150,19 @@ def test_loss_backward_refuses(bad, code):
     assert _code(B.tagc_loss_backward, _loss_grad(**bad), A) == code
 
 
+@pytest.mark.parametrize("dtype", [B.TAGC_BF16, B.TAGC_F32])
+@pytest.mark.parametrize("terms", [1, 5, 1024])
+def test_loss_workspaces_of_any_size(dtype, terms):
+    """Whole pieces, single tiles, and what lies between."""
+    for rows in (1, 2, 16, 17, 64, 65, 128, 1000, 1024, 1025, 4096):
+        for vocab in (1, 31, 32, 64, 255, 256, 4095, 4096, 8192, 12288, 32000, 65536, 131072, 262144, 262145):
+            for width in (1, 8, 64, 777, 4096):
+                kw = dict(rows=rows, vocab=vocab, in_=width, ldx=width, ldw=width, terms=terms, dtype=dtype, logits=S if terms > 1 else None)
+                if rows * terms < 1 << 25:
+                    assert B.tagc_loss_forward_workspace(_loss(**kw)) > 0
+                    assert B.tagc_loss_backward_workspace(_loss_grad(lddx=width, lddw=width, **kw)) > 0
+
+
 def test_loss_workspaces():
     """What is held does not grow with the vocabulary, but for scores of few rows."""
     big = [B.tagc_loss_forward_workspace(_loss(rows=8192, in_=4096, ldx=4096, ldw=4096, vocab=v)) for v in (1 << 18, 1 << 19, 1 << 20)]

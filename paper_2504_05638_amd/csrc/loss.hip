@@ -26,6 +26,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLeas
 // 128 rows 72 / 83, 512 rows 144 / 133; 333 of 777 over 1001 21 / 27, in float32 24 / 49; 4096 rows of 256 over 2048 35 / 28.)
 constexpr uint64_t kHeldRows = 1024, kHeld = 1u << 23;
 
+// Terms of a row from which on they are listed by strips: few are found sooner than a launch makes lists.
+constexpr uint32_t kListTerms = 5;
+
 // Elements up to which a vocabulary that is one piece is laid out in the launch that lays out x.  (us, backward, so / by a launch of its own: float32
 // 26 rows of 863 over 1977 49 / 52, bfloat16 1200 of 777 over 8001 91 / 95; float32 1024 of 1024 over 32000 1065 / 1068.)
 constexpr uint64_t kAtOnce = 1u << 26;
@@ -250,6 +253,46 @@ __global__ __launch_bounds__(256) void lay_kernel(Lay a)
     if (a.row && k == 0) a.row[r] = make_float2(a.saved[uint64_t(row) * (1 + a.terms.terms)] * kLog2e, a.dloss[uint64_t(row) * a.step] * a.terms.over);
 }
 
+// Many terms, by strips of 32 of the vocabulary's tokens: a workgroup counts and places those of 32 rows.  (Their order within a strip does not
+// matter: each is copied to a place of its own.)
+constexpr uint32_t kStripsRows = 32, kStrip = 32, kMostStrips = 8192;
+struct Strips {
+    uint32_t *starts;   // [groups of rows][strips + 1]: where the terms of a strip begin, NULL: there are no lists
+    uint32_t *entries;  // row of the group << 20 | term << 10 | lowest ten bits of the id
+    uint32_t strips;
+};
+__global__ __launch_bounds__(256) void strips_kernel(const uint32_t *ids, uint32_t shift, const uint32_t *count, Strips to)
+{
+    __shared__ uint32_t at[kMostStrips], room[4];
+    const uint32_t first = blockIdx.x * kStripsRows;
+    if (first >= *count) return;
+    const uint32_t n = min(kStripsRows, *count - first) << shift, base = first << shift;
+    for (uint32_t s = threadIdx.x; s < to.strips; s += 256) at[s] = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n; i += 256) {
+        const uint32_t id = ids[base + i];
+        if (id != kNone) atomicAdd(&at[id / kStrip], 1u);
+    }
+    __syncthreads();
+    const uint32_t each = (to.strips + 255) / 256, from = min(threadIdx.x * each, to.strips), end = min(from + each, to.strips);
+    uint32_t sum = 0, all;
+    for (uint32_t s = from; s < end; ++s) sum += at[s];
+    uint32_t place = block_excl_scan<uint32_t, 4>(sum, &all, room);
+    uint32_t *starts = to.starts + uint64_t(blockIdx.x) * (to.strips + 1);
+    for (uint32_t s = from; s < end; ++s) {
+        const uint32_t have = at[s];
+        at[s] = place;
+        starts[s] = base + place;
+        place += have;
+    }
+    if (threadIdx.x == 0) starts[to.strips] = base + all;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n; i += 256) {
+        const uint32_t id = ids[base + i];
+        if (id != kNone) to.entries[base + atomicAdd(&at[id / kStrip], 1u)] = (i >> shift) << 20 | (i & ((1u << shift) - 1)) << 10 | (id & 1023);
+    }
+}
+
 // ------------------------------------------------------------------ ends of the products
 
 // A wave's sums in rows, eight neighbours at a time, by way of its strip: f(m, n, z) for rows under `rows` and columns, by eights, under
@@ -291,8 +334,9 @@ __device__ inline __attribute__((always_inline)) void in_rows(const f32x4 (&acc)
 }
 
 // Forward: of a row's scores in a wave's columns the largest, and the sum of 2^(score - largest), scores times log2(e) / T; and those of
-// its terms.  These are looked for among the terms' ids, 32 rows at a time, and where there is one the rows go through local memory.
-// (64 terms of 2048 rows of 4096: 446 us of the product that takes 393 without; by themselves, as products of two rows each, they took 164.)
+// its terms.  These come from lists by strips, or are looked for among the terms' ids, 32 rows at a time; where there is one the rows go
+// through local memory.  (us, lists / looked for, the whole call over 32000 by 4096, 2048 rows of 8, 64, 128 terms: 448, 457, 462 / 461, 474, 503, of one
+// term 442; 4096 rows of 768 over 50257, 64 terms: 381 / 445.  By themselves, as products of two rows each, 64 terms took 164.)
 struct Scores : Counted {
     static constexpr bool kCounted = true;
     float2 *stats;  // [strips of columns][rows]
@@ -302,8 +346,24 @@ struct Scores : Counted {
     float *scores;        // [rows][terms]
     uint32_t shift, terms, base;  // base: the id of the piece's first column
     float over;           // 1 / T
+    Strips lists;         // of groups of 32 rows, pieces of whole strips
     template <int RM, int RN>
     __device__ inline __attribute__((always_inline)) void put(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0, uint32_t) const
+    {
+        if (lists.starts) listed_terms(acc, strip, lane, m0, n0);
+        else searched_terms(acc, strip, lane, m0, n0);
+        float2 *to = stats + uint64_t(n0 / (RN * 16)) * rows;
+        const uint32_t c0 = n0 + 4 * (lane >> 4);
+        const bool whole = n0 + RN * 16 <= n;
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+            const uint32_t row = m0 + i * 16 + (lane & 15);
+            const float2 of = whole ? summed<true>(acc[i], c0) : summed<false>(acc[i], c0);
+            if (lane < 16 && row < m) to[row] = of;
+        }
+    }
+    template <int RM, int RN>
+    __device__ inline __attribute__((always_inline)) void searched_terms(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0) const
     {
         constexpr uint32_t kRow = RN * 16 + 4, kQuads = 8;  // quads of ids on their way
         const uint32_t first = base + n0, quads = 32u << (shift - 2);
@@ -356,14 +416,34 @@ struct Scores : Counted {
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        float2 *to = stats + uint64_t(n0 / (RN * 16)) * rows;
-        const uint32_t c0 = n0 + 4 * (lane >> 4);
-        const bool whole = n0 + RN * 16 <= n;
+    }
+    template <int RM, int RN>
+    __device__ inline __attribute__((always_inline)) void listed_terms(const f32x4 (&acc)[RM][RN], float *strip, uint32_t lane, uint32_t m0, uint32_t n0) const
+    {
+        constexpr uint32_t kRow = RN * 16 + 4;
+        static_assert(RN * 16 % kStrip == 0, "whole strips");
+        if (n0 >= n) return;
+        const uint32_t first = base + n0, s = first / kStrip, end_s = min(s + RN * 16 / kStrip, lists.strips);
+#pragma unroll 1
+        for (int i = 0; i < RM; i += 2) {
+            if (m0 + i * 16 >= m) break;
+            const uint32_t *starts = lists.starts + uint64_t((m0 + i * 16) / kStripsRows) * (lists.strips + 1);
+            const uint32_t from = __builtin_amdgcn_readfirstlane(starts[s]), end = __builtin_amdgcn_readfirstlane(starts[end_s]);
+            if (from == end) continue;
 #pragma unroll
-        for (int i = 0; i < RM; ++i) {
-            const uint32_t row = m0 + i * 16 + (lane & 15);
-            const float2 of = whole ? summed<true>(acc[i], c0) : summed<false>(acc[i], c0);
-            if (lane < 16 && row < m) to[row] = of;
+            for (int at = 0; at < RM; at += 2)
+                if (at == i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int j = 0; j < RN; ++j)
+                            *reinterpret_cast<f32x4 *>(strip + (16 * h + (lane & 15)) * kRow + 16 * j + 4 * (lane >> 4)) = acc[at + h][j];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (uint32_t e = from + lane; e < end; e += 64) {
+                const uint32_t entry = lists.entries[e], r = entry >> 20, k = entry >> 10 & 1023, c = (entry - first) & 1023;
+                scores[uint64_t(m0 + i * 16 + r) * terms + k] = strip[r * kRow + c] * over;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
     // of a row's scores in columns c0 + 16 j + (0 .. 3) of four lanes; WHOLE: all these columns are there
@@ -1006,10 +1086,21 @@ int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
     float2 *stats = w.take<float2>(up(piece, 256) / 32 * M);
     float2 *run = w.take<float2>(piece < V ? M : 0);
     float *scores = w.take<float>(M * l->terms);
+    Strips lists{};
+    lists.strips = uint32_t((V + kStrip - 1) / kStrip);
+    const bool listing = l->terms >= kListTerms && lists.strips <= kMostStrips;
+    if (listing) {
+        lists.starts = w.take<uint32_t>((M + kStripsRows - 1) / kStripsRows * (lists.strips + 1));
+        lists.entries = w.take<uint32_t>(M << listed.shift);
+    }
     if (!enqueue) return TAGC_OK;
 
     const bool at_once = ops.lay && piece >= V && V * D < kAtOnce;
     launch_rows<T>(terms, listed, gather<T>(l->x, l->ldx, M, D, x), at_once ? gather<T>(l->w, l->ldw, V, D, wq) : Gather{}, Rowwise{}, s);
+    if (listing) {
+        ProfileScope prof("loss_strips", s);
+        strips_kernel<<<uint32_t((M + kStripsRows - 1) / kStripsRows), 256, 0, s>>>(listed.ids, listed.shift, list.count, lists);
+    }
     for (uint64_t v = 0; v < V; v += piece) {
         const uint64_t n = V - v < piece ? V - v : piece;
         const T *from = static_cast<const T *>(l->w) + v * l->ldw;
@@ -1031,6 +1122,7 @@ int forward(const tagc_loss *l, Places &w, bool enqueue, hipStream_t s)
         a.terms = l->terms;
         a.base = uint32_t(v);
         a.over = terms.over;
+        a.lists = lists;
         {
             ProfileScope prof("loss_product", s);
             launch<T, false, false>(a, f, s);

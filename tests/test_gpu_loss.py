@@ -166,6 +166,28 @@ def test_most_terms():
     _check((19, 40, 3001), torch.bfloat16, 1024, 1.5, True, False, 3, 0)
 
 
+@pytest.mark.parametrize("K", [4, 5, 33])
+@pytest.mark.parametrize("shape", [(40, 24, 262_144), (40, 24, 262_177), (1500, 72, 1000)], ids=str)
+def test_terms_listed_and_looked_for(shape, K):
+    """On both sides of the terms, and of the vocabulary, up to which they are listed by strips."""
+    print("[case] terms", shape, K, flush=True)
+    _check(shape, torch.bfloat16, K, 1.0, True, False, 61, K == 5)
+
+
+def test_terms_in_one_place():
+    """All rows' terms in one strip, or all of them one token."""
+    from paper_2504_05638_amd.train import distill
+    M, D, V, K = 1300, 64, 9000, 128
+    x, w = _randn((M, D), 71, torch.bfloat16), _randn((V, D), 72, torch.bfloat16, D ** -0.5)
+    gen = torch.Generator(device="cuda").manual_seed(73)
+    logits = torch.randn((M, K), generator=gen, device="cuda")
+    for ids in (torch.randint(8970, 9000, (M, K), generator=gen, device="cuda"), torch.full((M, K), 8999, device="cuda"), torch.zeros((M, K), dtype=torch.int64, device="cuda")):
+        loss, saved = distill(x, w, ids, logits, save=True)
+        ref = Ref(x, w, ids, logits, 1.0)
+        _near(loss, *ref.loss(), torch.float32, "loss")
+        _near(saved[:, 1:], ref.mine, ref.mine_err, torch.float32, "scores")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_pieces_of_the_vocabulary_backward(dtype):
     """ds of 65536 rows: some thousand tokens at a time."""

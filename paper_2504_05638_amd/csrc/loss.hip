@@ -479,7 +479,7 @@ struct Slopes : Counted {
     uint64_t ld;
     uint32_t part;
     const float2 *row;
-    const uint32_t *ids;  // [rows][2^shift]: where a row has one term, whose weight is 1, or NULL: they are put right afterwards
+    const uint32_t *ids;  // [rows][4]: a row's target, whose weight is 1, or NULL: a teacher's terms are put right afterwards (also a single one: of a logit that is not finite its weight is NaN)
     uint32_t shift, base;
     float over2;
     template <int RM, int RN>
@@ -1192,7 +1192,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
             a.ld = ds.ld;
             a.part = ds.part;
             a.row = by.row;
-            a.ids = l->terms == 1 ? listed.ids : nullptr;
+            a.ids = l->logits ? nullptr : listed.ids;
             a.shift = listed.shift;
             a.base = uint32_t(v);
             a.over2 = float(kLog2e / l->temperature);
@@ -1209,7 +1209,7 @@ int backward(const tagc_loss_grad *l, Places &w, bool enqueue, hipStream_t s)
                     launch<T, false, false>(a, f, s);
                 }
             }
-            if (l->terms > 1) {
+            if (l->logits) {
                 ProfileScope prof("loss_terms", s);
                 const uint64_t each = listed.shift < 8 ? 256 >> listed.shift : 1;
                 terms_slope_kernel<T><<<uint32_t((M + each - 1) / each), 256, 0, s>>>(terms, list, listed.ids, listed.shift, by.row, l->saved, a.ds, ds.ld, ds.part, uint32_t(v),

@@ -229,7 +229,7 @@ enum { TAGC_NORM_LAYER = 0, TAGC_NORM_RMS = 1 };
 typedef struct tagc_norm {
     uint64_t rows, width;           /* rows < 2^31, width <= TAGC_MAX_NORM_WIDTH           */
     uint32_t dtype, kind;           /* TAGC_NORM_*                                        */
-    double eps;                     /* >= 0, finite                                       */
+    double eps;                     /* >= 0, finite in float32                            */
     const void *x; uint64_t ldx;    /* [rows, width]                                      */
     const void *w, *b;              /* [width] or NULL: 1 and 0; no b with TAGC_NORM_RMS   */
     void *y; uint64_t ldy;          /* [rows, width]                                      */

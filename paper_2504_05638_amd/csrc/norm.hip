@@ -474,7 +474,7 @@ int check(const tagc_norm *n)
     const int rc = check(n->rows, n->width, n->dtype, n->kind);
     if (rc) return rc;
     const uint64_t e = n->dtype == TAGC_F32 ? 4 : 2, M = n->rows, bytes = n->width * e;
-    if (!(n->eps >= 0) || !isfinite(n->eps) || (n->kind == TAGC_NORM_RMS && n->b)) return TAGC_EINVAL;
+    if (!(n->eps >= 0) || !isfinite(float(n->eps)) || (n->kind == TAGC_NORM_RMS && n->b)) return TAGC_EINVAL;
     if (M && n->width && (!n->x || !n->y)) return TAGC_EINVAL;
     if (!good(n->x, n->ldx, n->width, e) || !good(n->y, n->ldy, n->width, e) || !aligned_to(n->w, e) || !aligned_to(n->b, e) || !aligned_to(n->stats, 8))
         return TAGC_EINVAL;

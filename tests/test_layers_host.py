@@ -176,3 +176,9 @@ def test_loss_workspaces():
     assert _code(B.tagc_loss_forward, _loss(), None) == -1
     assert _code(B.tagc_loss_forward, _loss(), A + 128) == -1
     assert _code(B.tagc_loss_backward, _loss_grad(), None) == -1
+
+
+def test_norm_eps_that_float32_does_not_hold():
+    """It would count as an infinity, and rows as their bias."""
+    for eps in (1e39, 1e300):
+        assert _code(B.tagc_norm_forward, _norm(eps=eps)) == -1

@@ -152,3 +152,45 @@ def test_not_finite_rows_of_no_token_stay_out():
     dtable = torch.empty(7, 40, device="cuda")
     embedding_backward(dy, ids, dtable)
     assert torch.equal(dtable, torch.bincount(ids[ids >= 0], minlength=7)[:, None].float().expand(7, 40))
+
+
+def _checked_and_repeated(n, vocab, width, dtype, kind, add):
+    """The result that is compared with float64 is what a second call makes, too, bit for bit; what lies around it stays."""
+    from paper_2504_05638_amd.train import embedding_backward
+    ids, dy = _ids(n, vocab, 5, kind), _randn((n, width), 6, dtype)
+    bucket = _randn((1, 5 + vocab * width + 4), 7, dtype)[0]
+    was = bucket.clone()
+    dtable, old = bucket[5:5 + vocab * width].view(vocab, width), was[5:5 + vocab * width].view(vocab, width)
+    embedding_backward(dy, ids, dtable, accumulate=add)
+    first = bucket.clone()
+    bucket.copy_(was)
+    embedding_backward(dy, ids, dtable, accumulate=add)
+    assert torch.equal(bucket, first) and torch.equal(bucket[:5], was[:5]) and torch.equal(bucket[-4:], was[-4:])
+    there = (ids >= 0) & (ids < vocab)
+    at, rows = ids[there], dy[there].double()
+    count = torch.bincount(at, minlength=vocab)[:, None].double()
+
+    def sums(t):        # (float64's additions to one place go one behind the other: a hundred thousand take half a minute)
+        out = torch.zeros(vocab, width, device="cuda", dtype=torch.float64)
+        if kind not in ("one", "few"):
+            return out.index_add_(0, at, t)
+        for v in at.unique().tolist():
+            out[v] = t[at == v].sum(0)
+        return out
+
+    ref, size = sums(rows), sums(rows.abs())
+    if add:
+        ref = ref + old.double()
+    _near(dtable, ref, (count + 2) * E * size + E * ref.abs(), dtype, (n, vocab, width, kind))
+    untouched = count[:, 0] == 0
+    assert torch.equal(dtable[untouched], old[untouched] if add else torch.zeros_like(old[untouched]))
+
+
+@pytest.mark.parametrize("add", [False, True], ids=["written", "added"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", KINDS)
+def test_what_is_checked_repeats(kind, dtype, add):
+    """One launch, one chunk, a list merged of chunks, one of merged lists; zeros beside the sort, and behind it (from 16385 tokens on)."""
+    for n, vocab, width in ((100, 64, 70), (3000, 900, 130), (9000, 20000, 32), (16384, 700, 40), (16385, 701, 33), (70_000, 50257, 24), (150_001, 1000, 9)):
+        print("[case] embedding gradient, repeated", kind, dtype, add, n, vocab, width, flush=True)
+        _checked_and_repeated(n, vocab, width, T[dtype], kind, add)

@@ -19,6 +19,11 @@
  * allocated, nothing synchronised, all work enqueued in order on `stream`, argument errors
  * reported before anything is enqueued.  Every entry point but tagc_optim_upload may be
  * captured in a HIP graph.
+ *
+ * A layer's workspace holds for the very struct that its tagc_*_workspace function was asked with, on the same current device: it
+ * depends on sizes and types, on which pointers are NULL, on how operands are aligned and strided, and on whether
+ * a result is written in an operand's place.  A call does not see how large the memory is that it is given: a struct that differs in one
+ * of these is asked for anew.
  */
 #ifndef TAGC_TRAIN_H
 #define TAGC_TRAIN_H
@@ -256,7 +261,10 @@ typedef struct tagc_norm_grad {
 /* y = (x - mean) * r * w + b, r = 1 / sqrt(mean of (x - mean)^2 + eps), mean 0 with TAGC_NORM_RMS: in float32, rounded once. */
 int tagc_norm_forward(const tagc_norm *n, void *stream);
 
-/* Bytes of workspace (dev, 256-byte aligned, contents do not matter) that the call needs. */
+/*
+ * Bytes of workspace (dev, 256-byte aligned, contents do not matter) that this very call needs.  With few rows (at present up to 512) dw and
+ * db take none, but where dx is written over x or dy they do.
+ */
 int tagc_norm_backward_workspace(const tagc_norm_grad *n, uint64_t *bytes);
 
 /*
@@ -275,9 +283,10 @@ enum { TAGC_ID_I32 = 0, TAGC_ID_I64 = 1 };
  * one behind the other; one outside [0, vocab) is no token: its row of the table counts as zeros, and it has no part in a gradient.
  */
 typedef struct tagc_embedding {
-    uint64_t rows, width, vocab;    /* ids, features, rows of the table; each < 2^22       */
+    uint64_t rows, width, vocab;    /* ids, features, rows of the table; each < 2^22, rows * width up to 2^34
+                                       (above, TAGC_ESIZE is possible)                    */
     uint32_t dtype, id_type;        /* TAGC_F32 | TAGC_BF16; TAGC_ID_*                    */
-    double scale;                   /* finite                                             */
+    double scale;                   /* finite in float32                                  */
     const void *ids;                /* [rows]                                             */
     const void *table; uint64_t ldt; /* [vocab, width]                                    */
     const void *residual; uint64_t ldr; /* [rows, width] or NULL                          */
@@ -313,19 +322,22 @@ int tagc_embedding_backward(const tagc_embedding_grad *e, void *workspace, void 
 #define TAGC_MAX_TERMS 1024u
 
 /*
- * The loss of a layer's output x [rows, in] against a vocabulary w [vocab, in], both of one type (TAGC_F32 | TAGC_BF16), whose
- * scores s = x w^T / temperature are held nowhere as a whole.  Every row has `terms` tokens that its target distribution q is on:
+ * The loss of a layer's output x [rows, in] against a vocabulary w [vocab, in], both of one type (TAGC_F32 | TAGC_BF16).  The
+ * scores s = x w^T / temperature are no result, and take no memory that grows with rows times vocab, but for those of few rows over few
+ * tokens (at present up to 1024 rows and 2^23 scores), which the workspace holds in float32.  Every row has `terms` tokens that its
+ * target distribution q is on:
  *   logits NULL   one term, q = 1: softmax cross entropy
  *   logits given  q = softmax(logits / temperature) over the row's terms: distillation
  * A term outside [0, vocab), or one whose logit is -infinity, is none; a token that is a row's term twice has both weights.  A row
- * without a term has loss 0, `saved` 0 and no part in a gradient; its x is not looked at and may be anything.
+ * without a term has loss 0, `saved` 0 and no part in a gradient; its x has no influence on anything, and may be anything.
  */
 typedef struct tagc_loss {
-    uint64_t rows, in, vocab;       /* in, vocab >= 1; limits as for tagc_linear          */
-    uint32_t terms;                 /* 1 .. TAGC_MAX_TERMS; 1 without logits              */
+    uint64_t rows, in, vocab;       /* in, vocab >= 1; limits as for tagc_linear, and x and w, their sides rounded up to
+                                       multiples of 64, < 2^34 elements each              */
+    uint32_t terms;                 /* 1 .. TAGC_MAX_TERMS, rows * terms < 2^25; 1 without logits */
     uint32_t dtype, id_type;        /* TAGC_F32 | TAGC_BF16; TAGC_ID_*                    */
     uint32_t reserved;              /* must be 0                                          */
-    double temperature;             /* > 0, finite; 1 for plain cross entropy             */
+    double temperature;             /* > 0, finite, as its reciprocal is in float32; 1 for plain cross entropy */
     const void *x; uint64_t ldx;    /* [rows, in]                                         */
     const void *w; uint64_t ldw;    /* [vocab, in]                                        */
     const void *ids;                /* [rows, terms], contiguous                          */
@@ -359,8 +371,9 @@ int tagc_loss_backward_workspace(const tagc_loss_grad *l, uint64_t *bytes);
 int tagc_loss_forward(const tagc_loss *l, void *workspace, void *stream);
 
 /*
- * ds = dloss (e^(s - lse) - q) / temperature, by pieces of the vocabulary, each rounded to the operands' type once; dx = ds w;
- * dw (+)= ds^T x.  dx is summed in float32 over the pieces.  What is written shares no element with an operand or another result.
+ * ds = dloss (e^(s - lse) - q) / temperature, by pieces of the vocabulary, each rounded to the operands' type once (float32: held as the
+ * products' operands are, see tagc_linear_forward); dx = ds w; dw (+)= ds^T x.  dx is summed in float32 over the pieces.  What is written shares no
+ * element with an operand or another result.
  */
 int tagc_loss_backward(const tagc_loss_grad *l, void *workspace, void *stream);
 

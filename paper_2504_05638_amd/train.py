@@ -436,7 +436,7 @@ def _loss_backward(dloss, x, w, ids, logits, saved, temperature, dx, dw, accumul
 
 def cross_entropy(x, w, targets, save=False, stream=None):
     """(loss, saved): of every row of x [..., in] the softmax cross entropy of its scores x w^T over a vocabulary w [vocab, in] against
-    its target (int32 or int64), float32; the scores are kept nowhere.  A target outside [0, vocab) is ignored: loss 0, no gradient.
+    its target (int32 or int64), float32; the scores are no result, and held as a whole only where they are few.  A target outside [0, vocab) is ignored: loss 0, no gradient.
     `save`: saved, float32 [rows, 2] (the log-sum of the scores' exponentials, the target's score), for cross_entropy_backward (else
     None).  No autograd graph is recorded; `stream`: as for linear."""
     _no_graph("cross_entropy", x, w)

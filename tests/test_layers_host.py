@@ -182,3 +182,23 @@ def test_norm_eps_that_float32_does_not_hold():
     """It would count as an infinity, and rows as their bias."""
     for eps in (1e39, 1e300):
         assert _code(B.tagc_norm_forward, _norm(eps=eps)) == -1
+
+
+def test_sizes_that_are_allowed_together():
+    """On both sides of what the header says of products of sizes."""
+    wide = (1 << 22) - 1
+    for rows, width in ((wide, 4096), (4096, wide), (1 << 17, 1 << 17), (1, wide), (wide, 1)):
+        assert rows * width <= 1 << 34
+        # (a result over an operand, which is found behind sizes: nothing is launched)
+        assert _code(B.tagc_embedding_forward, _embed(rows=rows, width=width, y=A, ldt=width, ldr=width, ldy=width)) == -1
+        assert B.tagc_embedding_backward_workspace(_embed_grad(rows=rows, width=width, vocab=1, lddy=width, ldt=width, dtable=1 << 48)) >= 0
+    for terms, rows in ((1024, (1 << 15) - 1), (16, (1 << 21) - 1), (1000, 33554)):
+        assert rows * terms < 1 << 25 <= (rows + 1) * terms
+        assert B.tagc_loss_forward_workspace(_loss(rows=rows, terms=terms, logits=S, loss=1 << 48, saved=None)) > 0
+        assert _code(B.tagc_loss_forward_workspace, _loss(rows=rows + 1, terms=terms, logits=S, loss=1 << 48, saved=None)) == -2
+    for width, allowed in (((1 << 17) - 64, True), ((1 << 17) - 63, False), (1 << 17, False)):
+        a = _loss(rows=10, vocab=1 << 17, in_=width, ldx=width, ldw=width)
+        if allowed:
+            assert B.tagc_loss_forward_workspace(a) > 0
+        else:
+            assert _code(B.tagc_loss_forward_workspace, a) == -2

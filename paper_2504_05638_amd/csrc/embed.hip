@@ -369,7 +369,7 @@ __global__ __launch_bounds__(kSumThreads) void direct_kernel(Tokens a, Sums b)
 }
 
 // A workgroup sums a piece of sorted tokens, 256 * V columns of them; workgroups behind those write zeros.  Bound by the bytes of dy, of the rows that
-// are finished and of the partial sums: 16384 tokens of 4096 in bfloat16 35 us, 5.1 TB/s.
+// are finished and of the partial sums: 16384 tokens of 4096 in bfloat16 35 us for 134, 43 and 9 MB, 5.3 TB/s.
 template <typename T, uint32_t PIECE, int ROWS>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(Sums a)
 {
